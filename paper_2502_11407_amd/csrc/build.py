@@ -55,8 +55,9 @@ def generate():
         path = os.path.join(GEN, "%s_%03d.hip" % (kind, t // PER_TU))
         _write_if_changed(path, "\n".join(src))
         tus.append(path)
+    tus += generate_fused()
     for f in os.listdir(GEN):                      # units of an earlier lattice
-        if f.endswith(".hip") and os.path.join(GEN, f) not in tus and f != "registry.hip":
+        if f.endswith(".hip") and os.path.join(GEN, f) not in tus and f not in ("registry.hip", "fused_registry.hip"):
             os.remove(os.path.join(GEN, f))
             if os.path.exists(os.path.join(GEN, f[:-4] + ".o")):
                 os.remove(os.path.join(GEN, f[:-4] + ".o"))
@@ -66,17 +67,7 @@ def generate():
         if lattice.splittable(d):
             reg.append("hipError_t launch_split_%d(const KernelArgs&, hipStream_t);" % d["id"])
     reg.append("const InstanceDesc g_instances[] = {")
-    for d in L:
-        es = 4 if d["dt"] == "f32" else 2
-        kg = (64 // d["mb"]) * (16 // es)
-        a_bytes = d["bm"] * d["bk"] * es if d["asrc"] == "KC" else d["bk"] * (d["bm"] * es + (0 if d["direct"] else lattice.pad_m(d)))
-        b_bytes = d["bn"] * d["bk"] * es if (d["bsrc"] == "KC" or d["direct"]) else d["bk"] * (d["bn"] * es + lattice.pad_n(d))
-        lds = 0 if d["units"] or lattice.conv_rows(d) else (a_bytes + b_bytes) * d["stages"] + (b_bytes if lattice.alternate(d) else 0)
-        threads = (d["bm"] // d["wm"]) * (d["bn"] // d["wn"]) * 64
-        reg.append("  {%d, %d, %d, %d, %d, %d, %d, %d, %d, %d, %d, %d, %d, %d, %d, %d, %d, %d, %d, %d, launch_%d, %s}," % (
-            d["id"], lattice.DT[d["dt"]], lattice.DT[d["out"]], d["bm"], d["bn"], d["bk"], d["wm"], d["wn"], d["mb"],
-            d["vm"], d["vn"], lattice.BSRC[d["bsrc"]], lattice.ASRC[d["asrc"]], d["vec"], d["stages"], d["direct"], lds, threads, kg, d["units"], d["id"],
-            ("launch_split_%d" % d["id"]) if lattice.splittable(d) else "nullptr"))
+    reg += ["  {%s, launch_%d, %s}," % (instance_fields(d), d["id"], ("launch_split_%d" % d["id"]) if lattice.splittable(d) else "nullptr") for d in L]
     reg.append("};")
     reg.append("const int g_num_instances = %d;" % len(L))
     reg.append("}  // namespace gensor")
@@ -87,16 +78,57 @@ def generate():
     return tus
 
 
+def instance_fields(d):
+    """The members of an InstanceDesc in front of its launches."""
+    es = 4 if d["dt"] == "f32" else 2
+    kg = (64 // d["mb"]) * (16 // es)
+    a_bytes = d["bm"] * d["bk"] * es if d["asrc"] == "KC" else d["bk"] * (d["bm"] * es + (0 if d["direct"] else lattice.pad_m(d)))
+    b_bytes = d["bn"] * d["bk"] * es if (d["bsrc"] == "KC" or d["direct"]) else d["bk"] * (d["bn"] * es + lattice.pad_n(d))
+    lds = 0 if d["units"] or lattice.conv_rows(d) else (a_bytes + b_bytes) * d["stages"] + (b_bytes if lattice.alternate(d) else 0)
+    threads = (d["bm"] // d["wm"]) * (d["bn"] // d["wn"]) * 64
+    return ", ".join(str(x) for x in (
+        d["id"], lattice.DT[d["dt"]], lattice.DT[d["out"]], d["bm"], d["bn"], d["bk"], d["wm"], d["wn"], d["mb"],
+        d["vm"], d["vn"], lattice.BSRC[d["bsrc"]], lattice.ASRC[d["asrc"]], d["vec"], d["stages"], d["direct"], lds, threads, kg, d["units"]))
+
+
+def generate_fused():
+    """Units and table of the products that are consumed in place."""
+    L = lattice.fused()
+    tus = []
+    # (a unit holds tiles built with the same flags)
+    chains = [d for d in L if lattice.chains(d) > 1]
+    for kind, group in (("fused", [d for d in L if lattice.chains(d) == 1]), ("fusedchains", chains)):
+        for d in group:
+            src = ['#include "fused_registry.hpp"', "namespace gensor {", "typedef %s C_%d;" % (lattice.cfg_type(d), d["id"])]
+            src += ["hipError_t fused_%d_%s(const FusedArgs& a, hipStream_t st) { return launch_fused<C_%d, %s>(a, st); }"
+                    % (d["id"], k, d["id"], lattice.FUSED_KINDS[k]) for k in d["kinds"]]
+            src.append("}  // namespace gensor\n")
+            path = os.path.join(GEN, "%s_%03d.hip" % (kind, d["id"]))
+            _write_if_changed(path, "\n".join(src))
+            tus.append(path)
+    reg = ['#include "fused_registry.hpp"', "#if !defined(__HIP_DEVICE_COMPILE__)", "namespace gensor {"]
+    reg += ["hipError_t fused_%d_%s(const FusedArgs&, hipStream_t);" % (d["id"], k) for d in L for k in d["kinds"]]
+    reg.append("const FusedDesc g_fused[] = {")
+    reg += ["  {{%s, nullptr, nullptr}, {%s}}," % (instance_fields(d), ", ".join(
+        "fused_%d_%s" % (d["id"], k) if k in d["kinds"] else "nullptr" for k in lattice.FUSED_KINDS)) for d in L]
+    reg += ["};", "const int g_num_fused = %d;" % len(L), "}  // namespace gensor", "#endif\n"]
+    path = os.path.join(GEN, "fused_registry.hip")
+    _write_if_changed(path, "\n".join(reg))
+    return tus + [path]
+
+
 def _compile(src):
     obj = os.path.join(GEN, os.path.basename(src).rsplit(".", 1)[0] + ".o")
     deps = [src, os.path.join(HERE, "gemm_kernel.hpp"), os.path.join(HERE, "conv_kernel.hpp"), os.path.join(HERE, "conv_rows_kernel.hpp"), os.path.join(HERE, "registry.hpp"),
             os.path.join(HERE, "host_common.hpp"), os.path.join(PKG, "..", "include", "gensor.h")]
+    if "fused" in os.path.basename(src):
+        deps += [os.path.join(HERE, "fused_kernel.hpp"), os.path.join(HERE, "fused_registry.hpp"), os.path.join(PKG, "..", "include", "gensor_fused.h")]
     if os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps if os.path.exists(d)):
         return obj
     # host sources: no fused multiply-add contraction, so the constructor's double arithmetic
     # is the plain IEEE sequence its tests compare against
     extra = ["-ffp-contract=off"] if src.endswith(".cpp") else []
-    if os.path.basename(src).startswith(("conv_", "chains_")):
+    if os.path.basename(src).startswith(("conv_", "chains_", "fusedchains_")):
         extra += CONV_FLAGS
     cmd = [HIPCC] + FLAGS + extra + ["-x", "hip", "-c", src, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -110,7 +142,8 @@ def _compile(src):
 
 def build(force=False, jobs=None):
     tus = generate()
-    tus += [os.path.join(HERE, "gensor_api.cpp"), os.path.join(HERE, "constructor.cpp"), os.path.join(HERE, "scan_kernels.cpp")]
+    tus += [os.path.join(HERE, "gensor_api.cpp"), os.path.join(HERE, "constructor.cpp"), os.path.join(HERE, "scan_kernels.cpp"),
+            os.path.join(HERE, "gensor_fused.cpp")]
     probe = os.path.join(HERE, "probe.cpp")
     if force:
         for f in os.listdir(GEN):

@@ -569,6 +569,10 @@ void keep_choice(std::vector<Choice>* list, const Choice& x) {
 
 }  // namespace
 
+double fused_price(const InstanceDesc& d, const GemmView& v, int split) {
+  return predict(v, kMi355x, d.bm, d.bn, d.bk, d.wm, d.wn, d.kg, d.vm, d.vn, d.vec, d.stages, d.direct, split);
+}
+
 gensor_status construct_internal(const gensor_problem* p, const gensor_hw* hw, const gensor_construct_opts* opts,
                                  uint64_t seed, bool vec_ok, int view_mode, gensor_schedule* out, const LeadingDims* ld,
                                  std::vector<RankedSchedule>* ranked) {

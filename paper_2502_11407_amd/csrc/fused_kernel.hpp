@@ -1,0 +1,583 @@
+// Products whose result is consumed where it is produced: what the contraction kernel's workgroups do with their tile in
+// place of storing alpha * A * B (the F of contraction_kernel), and how they find their rows where the products are grouped.
+//
+//   END_LINEAR  C = act(alpha A B + bias) + residual, and the values before act kept; or C = (alpha A B) * act'(preact)
+//   END_LSE     rows are vocabulary entries, columns tokens: each wave reduces its rows' logits to a maximum and a sum of
+//               exponentials per token; nothing else is stored
+//   END_PROB    the same product again: C = scale * dloss[token] * (exp(logit - lse[token]) - (row == target[token]))
+//
+//   MOVE_NONE   one product
+//   MOVE_ROWS   group g owns rows [offsets[g], offsets[g+1]) of A and C and has its own B (and bias)
+//   MOVE_DEPTH  group g owns k rows [offsets[g], offsets[g+1]) of both operands and has its own C
+//
+// Activations.  gelu is the tanh form, 0.5 z (1 + tanh(u)) with u = sqrt(2/pi) (z + 0.044715 z^3).  Since
+// 0.5 (1 + tanh(u)) = sigmoid(2u), gelu and silu are both z * sigmoid(z (c1 + c2 z^2)), one exponential and one reciprocal,
+// without the difference 1 + tanh that loses the negative side's digits.
+#pragma once
+#include "gemm_kernel.hpp"
+
+namespace gensor {
+
+enum { END_LINEAR = 0, END_LSE = 1, END_PROB = 2 };
+enum { MOVE_NONE = 0, MOVE_ROWS = 1, MOVE_DEPTH = 2 };
+enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };       // gensor_act
+
+struct FusedArgs : KernelArgs {
+  int32_t store_m, store_n;        // rows and columns of C that exist (loads go by M and N)
+  // END_LINEAR
+  int32_t act, grad;               // grad: C = (alpha A B) * act'(preact)
+  const void* bias;                // of the input type, or null
+  void* preact;                    // of C's type: written (read if grad), or null
+  const void* residual;            // of C's type, or fp32 (residual_f32), or null
+  int64_t ld_preact, ld_residual;
+  int32_t residual_f32;
+  const float* scale;              // one more factor of alpha, on the device, or null
+  // groups
+  const int32_t* offsets;          // groups + 1 of them; any values: what they name is cut to the `rows` there are
+  int32_t groups, rows;
+  // END_LSE and END_PROB; a column is a token
+  const int64_t* targets;
+  int64_t ignore;
+  const float* lse;
+  const float* dloss;
+  float* part_max;                 // [slab of C::WM rows][tokens]
+  float* part_sum;
+  float* at_target;                // the logit of the token's target
+  int32_t tokens, row_first, vocab;        // row_first: vocabulary entry of row 0
+};
+
+// ---------------------------------------------------------------- activations
+struct ActForm {
+  float k1, k2, c1, c2;            // k = -log2(e) c
+  __device__ explicit ActForm(int act) {
+    constexpr float log2e = 1.44269504088896340736f;
+    c1 = act == ACT_GELU ? 1.59576912160573071176f : 1.f;              // 2 sqrt(2 / pi)
+    c2 = act == ACT_GELU ? 1.59576912160573071176f * 0.044715f : 0.f;
+    k1 = -log2e * c1;
+    k2 = -log2e * c2;
+  }
+  // (the square is held finite: 0 * inf would be NaN in silu's c2 z^2)
+  __device__ float sigmoid(float z, float& q) const {
+    q = fminf(z * z, 1e30f);
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * fmaf(k2, q, k1)));
+  }
+  __device__ float value(float z) const {
+    float q;
+    return z * sigmoid(z, q);
+  }
+  __device__ float slope(float z) const {
+    float q;
+    const float s = sigmoid(z, q);
+    return fmaf(z * s * (1.f - s), fmaf(3.f * c2, q, c1), s);
+  }
+};
+
+template <typename T> __device__ inline float from_bits(uint32_t u);
+template <> __device__ inline float from_bits<f32_t>(uint32_t u) { return as_f32(u); }
+template <> __device__ inline float from_bits<bf16_t>(uint32_t u) { return as_f32(u << 16); }
+template <> __device__ inline float from_bits<f16_t>(uint32_t u) { return (float)__builtin_bit_cast(_Float16, (uint16_t)u); }
+template <typename T> __device__ inline float from_pair(uint32_t u, int half);
+template <> __device__ inline float from_pair<bf16_t>(uint32_t u, int half) { return as_f32(half ? u & 0xffff0000u : u << 16); }
+template <> __device__ inline float from_pair<f16_t>(uint32_t u, int half) { return from_bits<f16_t>(half ? u >> 16 : u & 0xffffu); }
+
+// ---------------------------------------------------------------- sums of exponentials
+// sum = sum of exp(z - reference) with the maximum as the reference, or 0 where it is infinite (inf - inf): lse = reference + log(sum)
+__device__ inline float lse_reference(float top) { return fabsf(top) == INFINITY ? 0.f : top; }
+// ... joined with another part's.  (A part without terms has the maximum -inf and the sum 0: its factor must be no infinity.)
+__device__ inline void join_sums(float& top, float& sum, float top2, float sum2) {
+  constexpr float log2e = 1.44269504088896340736f;
+  const float both = fmaxf(top, top2), r = lse_reference(both);
+  const float f1 = fabsf(top) == INFINITY ? 1.f : __builtin_amdgcn_exp2f(log2e * (top - r));
+  const float f2 = fabsf(top2) == INFINITY ? 1.f : __builtin_amdgcn_exp2f(log2e * (top2 - r));
+  sum = sum * f1 + sum2 * f2;
+  top = both;
+}
+
+// ---------------------------------------------------------------- groups
+// Rows of group g: the offsets are device memory that the host never sees, so whatever they hold is cut to the rows there are.
+__device__ inline void group_rows(const FusedArgs& a, int g, int& first, int& count) {
+  first = min(max(a.offsets[g], 0), a.rows);
+  count = min(max(a.offsets[g + 1], first), a.rows) - first;
+}
+
+// ---------------------------------------------------------------- the ends
+template <int END, int MOVE>
+struct Fused {
+  typedef FusedArgs Args;
+  typedef std::conditional_t<MOVE != MOVE_NONE, FusedArgs, const FusedArgs&> Local;
+  static constexpr bool MOVES = MOVE != MOVE_NONE, OWN_END = true;
+
+  // The workgroup's tile; false: there is none for it.  The launch has as many workgroups as the row counts could
+  // need, ceil(rows / BM) of each group at worst; every wave counts the tiles there are by itself (64 groups at a time, one
+  // a lane), so nothing has to run before this launch and the host never waits for the counts.
+  template <typename C>
+  static __device__ __attribute__((always_inline)) bool place(FusedArgs& a, int& bidx, int& tile_m, int& tile_n) {
+    constexpr int ES = C::ES, OS = ElemSize<typename C::OutT>::value;
+    if constexpr (MOVE == MOVE_DEPTH) {
+      const int per = a.tiles_m * a.tiles_n;
+      const int wg = xcd_contiguous(blockIdx.x, per * a.batch);
+      bidx = wg / per;
+      tile_of(a, wg - bidx * per, tile_m, tile_n);
+      int first, count;
+      group_rows(a, bidx, first, count);
+      a.A = (const char*)a.A + (int64_t)first * a.lda * ES;
+      a.B = (const char*)a.B + (int64_t)first * a.ldb * ES;
+      a.C = (char*)a.C + (int64_t)bidx * a.strideC * OS;
+      a.K = count;
+      if (count > 0) return true;
+      // nothing to add up: zeros
+      const int m0 = tile_m * C::BM, n0 = tile_n * C::BN;
+      const int rows = min(C::BM, a.store_m - m0), cols = min(C::BN, a.store_n - n0);
+      for (int i = threadIdx.x; i < rows * C::BN; i += C::THREADS) {
+        const int r = i / C::BN, k = i % C::BN;
+        if (k < cols) store_out<typename C::OutT>(a.C, (int64_t)(m0 + r) * a.ldc + n0 + k, 0.f);
+      }
+      return false;
+    } else {
+      const int lane = threadIdx.x & 63;
+      auto tiles_at = [&](int g) {
+        int first, count = 0;
+        if (g < a.groups) group_rows(a, g, first, count);
+        return (count + C::BM - 1) / C::BM;
+      };
+      auto running = [&](int x) {                    // inclusive sum over the lanes
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+          const int y = __shfl_up(x, d, 64);
+          if (lane >= d) x += y;
+        }
+        return x;
+      };
+      int total = 0, mine = 0;
+      for (int g0 = 0; g0 < a.groups; g0 += 64) {
+        mine = running(tiles_at(g0 + lane));
+        total += __builtin_amdgcn_readlane(mine, 63);
+      }
+      total *= a.tiles_n;
+      if ((int)blockIdx.x >= total) return false;
+      const int t = xcd_contiguous(blockIdx.x, total);
+      int before = 0;                                // tile rows of the groups before this chunk of them
+      for (int g0 = 0; g0 < a.groups; g0 += 64) {
+        if (a.groups > 64) mine = running(tiles_at(g0 + lane));
+        const uint64_t beyond = __ballot((before + mine) * a.tiles_n > t);
+        if (beyond != 0) {
+          const int at = __builtin_ctzll(beyond);
+          const int end = __builtin_amdgcn_readlane(mine, at);
+          const int start = at > 0 ? __builtin_amdgcn_readlane(mine, at - 1) : 0;
+          const int g = g0 + at;
+          int first, count;
+          group_rows(a, g, first, count);
+          first = __builtin_amdgcn_readfirstlane(first);
+          count = __builtin_amdgcn_readfirstlane(count);
+          bidx = g;
+          a.M = a.store_m = count;
+          a.tiles_m = end - start;
+          a.panel = min(a.panel, a.tiles_m);
+          tile_of(a, t - (before + start) * a.tiles_n, tile_m, tile_n);
+          a.A = (const char*)a.A + (int64_t)first * a.lda * ES;
+          a.C = (char*)a.C + (int64_t)first * a.ldc * OS;
+          if (a.preact) a.preact = (char*)a.preact + (int64_t)first * a.ld_preact * OS;
+          if (a.residual) a.residual = (const char*)a.residual + (int64_t)first * a.ld_residual * OS;
+          if (a.bias) a.bias = (const char*)a.bias + (int64_t)g * a.N * ES;
+          return true;
+        }
+        before += __builtin_amdgcn_readlane(mine, 63);
+      }
+      return false;
+    }
+  }
+
+  template <typename C, typename Acc>
+  static __device__ __attribute__((always_inline)) void finish(const FusedArgs& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p) {
+    if constexpr (END == END_LSE) finish_lse<C>(a, acc, p);
+    else if constexpr (END == END_PROB) finish_prob<C>(a, acc, p);
+    else finish_linear<C, true>(a, acc, p);
+  }
+
+  // Row of element v of a block, less the lane group's part (4 rows apart)
+  template <typename C> static constexpr __device__ int row_of(int v) { return C::MB == 32 ? 8 * (v / 4) + v % 4 : v; }
+
+  // ---- C = act(alpha A B + bias) + residual, or (alpha A B) * act'(preact); FULL = false: C = acc as it is.
+  // Bound by what it moves beside C: the values kept or read again, and the residual.  An element access moves two bytes a
+  // lane of 16-bit types, so where rows allow it (`paired`) pairs of rows of a column are traded with the neighbour lane for
+  // pairs of columns of a row, as the plain epilogue does: the exchange is its own inverse, so what is read goes the
+  // same way backwards.  What a block reads is requested while the block before it is computed.
+  template <typename C, bool FULL, typename Acc>
+  static __device__ __attribute__((always_inline)) void finish_linear(const FusedArgs& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p) {
+    typedef typename C::OutT OutT;
+    constexpr int OS = ElemSize<OutT>::value, ES = C::ES, MB = C::MB, NACC = MB * MB / 64;
+    constexpr uint32_t FLAGS = 0x00020000u, OOB = 0x80000000u;
+    const int lane = p.lane, frow = lane % MB, fgrp = lane / MB;
+    const int rows_valid = min(C::BM, a.store_m - p.m0), cols_valid = min(C::BN, a.store_n - p.n0);
+    auto records = [&](int64_t ld, int size) -> uint32_t {
+      const int64_t bytes = ((int64_t)(rows_valid - 1) * ld + cols_valid) * size;
+      return bytes <= 0 ? 0u : bytes > 0x7fffffffll ? 0x7fffffffu : (uint32_t)bytes;
+    };
+    const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void*)((char*)a.C + ((int64_t)p.m0 * a.ldc + p.n0) * OS), 0, records(a.ldc, OS), FLAGS);
+    const uint32_t pitch = (uint32_t)a.ldc * OS;
+    const bool has_z = FULL && a.preact != nullptr, has_r = FULL && a.residual != nullptr;
+    const int xs = has_r && a.residual_f32 ? 4 : OS;                   // size of what is read
+    const bool reads = has_r || (has_z && a.grad);
+    const char* x_base = has_r ? (const char*)a.residual : (const char*)a.preact;
+    const int64_t x_ld = has_r ? a.ld_residual : a.ld_preact;
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)(reads ? x_base + ((int64_t)p.m0 * x_ld + p.n0) * xs : (const char*)a.C), 0,
+                                                                        reads ? records(x_ld, xs) : 0u, FLAGS);
+    const uint32_t x_pitch = (uint32_t)x_ld * xs;
+    const bool keeps = has_z && !a.grad;
+    const __amdgpu_buffer_rsrc_t rz = __builtin_amdgcn_make_buffer_rsrc((void*)(keeps ? (char*)a.preact + ((int64_t)p.m0 * a.ld_preact + p.n0) * OS : (char*)a.C), 0,
+                                                                        keeps ? records(a.ld_preact, OS) : 0u, FLAGS);
+    const uint32_t z_pitch = (uint32_t)a.ld_preact * OS;
+    const float alpha = FULL ? a.alpha * (a.scale ? *a.scale : 1.f) : 1.f;
+    const int act = FULL ? a.act : ACT_NONE;
+    const bool grad = FULL && a.grad;
+    const ActForm form(act);
+
+    // ---- bias: one value a lane and block column
+    float bias[C::NBLK];
+#pragma unroll
+    for (int bj = 0; bj < C::NBLK; ++bj) {
+      const int col = p.n0 + p.col + bj * MB + frow;
+      bias[bj] = FULL && a.bias && col < a.store_n ? to_float<typename C::T>(a.bias, col) : 0.f;
+    }
+    // the values of a block, x what was read for it; z: the values before the activation
+    auto compute = [&](int bi, int bj, const float* x, float* z, float* y) {
+#pragma unroll
+      for (int v = 0; v < NACC; ++v) z[v] = FULL ? fmaf(alpha, acc[bi][bj][v], bias[bj]) : acc[bi][bj][v];
+      if (act == ACT_NONE) {
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) y[v] = z[v];
+      } else if (grad) {
+        if (act == ACT_RELU) {
+#pragma unroll
+          for (int v = 0; v < NACC; ++v) y[v] = x[v] > 0.f ? z[v] : 0.f;
+        } else {
+#pragma unroll
+          for (int v = 0; v < NACC; ++v) y[v] = z[v] * form.slope(x[v]);
+        }
+      } else if (act == ACT_RELU) {
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) y[v] = z[v] < 0.f ? 0.f : z[v];
+      } else {
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) y[v] = form.value(z[v]);
+      }
+      if (has_r) {
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) y[v] += x[v];
+      }
+    };
+    constexpr bool HALF_LINES = C::WN % 64 != 0;
+    constexpr int GB = (HALF_LINES ? 32 : 64) / MB;                    // blocks side by side that are stored together
+    constexpr bool PAIRS = OS == 2 && GB >= 2 && C::NBLK % GB == 0;
+    if (PAIRS && a.paired) {
+      if constexpr (PAIRS) {
+        const uint32_t pick = (lane & 1) ? 0x03020706u : 0x05040100u;
+        auto trade = [&](uint32_t own) -> uint32_t {
+          const uint32_t other = (uint32_t)__builtin_amdgcn_mov_dpp((int)own, 0xB1, 0xF, 0xF, true);      // quad_perm [1,0,3,2]
+          return __builtin_amdgcn_perm(other, own, pick);
+        };
+        constexpr int RS = GB == 4 ? 4 : 2;                            // stores of a pair of rows of GB blocks
+        // w[i]: block i's pairs of rows v, v + 1; swapped into the order of the stores, whose rows are row_at(i) further down
+        auto swap_in = [&](uint32_t* w) {
+          if constexpr (MB == 32) {
+            const auto q = __builtin_amdgcn_permlane32_swap(w[0], w[1], false, false);
+            w[0] = q[0]; w[1] = q[1];
+          } else if constexpr (GB == 2) {
+            const auto q = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false);
+            w[0] = q[0]; w[1] = q[1];
+          } else {
+            const auto s = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false);
+            const auto t = __builtin_amdgcn_permlane16_swap(w[2], w[3], false, false);
+            const auto c = __builtin_amdgcn_permlane32_swap(s[0], t[0], false, false);
+            const auto d = __builtin_amdgcn_permlane32_swap(s[1], t[1], false, false);
+            w[0] = c[0]; w[1] = d[0]; w[2] = c[1]; w[3] = d[1];
+          }
+        };
+        auto swap_out = [&](uint32_t* w) {
+          if constexpr (MB == 32) {
+            const auto q = __builtin_amdgcn_permlane32_swap(w[0], w[1], false, false);
+            w[0] = q[0]; w[1] = q[1];
+          } else if constexpr (GB == 2) {
+            const auto q = __builtin_amdgcn_permlane16_swap(w[0], w[1], false, false);
+            w[0] = q[0]; w[1] = q[1];
+          } else {
+            const auto c = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+            const auto d = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+            const auto s = __builtin_amdgcn_permlane16_swap(c[0], d[0], false, false);
+            const auto t = __builtin_amdgcn_permlane16_swap(c[1], d[1], false, false);
+            w[0] = s[0]; w[1] = s[1]; w[2] = t[0]; w[3] = t[1];
+          }
+        };
+        constexpr int UNITS = C::MBLK * (C::NBLK / GB), HALVES = NACC / 2;
+        uint32_t in[2][HALVES][RS];
+        auto column = [&](int bj) { return p.col + bj * MB + (lane % (GB * MB) & ~1); };
+        auto row = [&](int bi) { return p.row + bi * MB + (lane & 1) + (HALF_LINES ? 8 * (lane >> 5) : 0); };
+        auto request = [&](int u, int set) {
+          const int bi = u % C::MBLK, bj = u / C::MBLK * GB;
+          const uint32_t at = column(bj) < cols_valid ? (uint32_t)(column(bj) * OS) + (uint32_t)row(bi) * x_pitch : OOB;
+#pragma unroll
+          for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+            for (int i = 0; i < RS; ++i) in[set][h][i] = __builtin_amdgcn_raw_buffer_load_b32(rx, at + (uint32_t)(row_of<C>(2 * h) + 4 * i) * x_pitch, 0, 0);
+        };
+        if (reads) request(0, 0);
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+          const int bi = u % C::MBLK, bj = u / C::MBLK * GB;
+          if (reads && u + 1 < UNITS) request(u + 1, (u + 1) & 1);
+          float x[GB][NACC], z[GB][NACC], y[GB][NACC];
+          if (reads) {
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) {
+              uint32_t w[RS];
+#pragma unroll
+              for (int i = 0; i < RS; ++i) w[i] = in[u & 1][h][i];
+              swap_out(w);
+#pragma unroll
+              for (int g = 0; g < GB; ++g) {
+                const uint32_t t = trade(w[g]);
+                if constexpr (OS == 2) {
+                  x[g][2 * h] = from_pair<OutT>(t, 0);
+                  x[g][2 * h + 1] = from_pair<OutT>(t, 1);
+                }
+              }
+            }
+          }
+#pragma unroll
+          for (int g = 0; g < GB; ++g) compute(bi, bj + g, x[g], z[g], y[g]);
+          auto put = [&](const float (&val)[GB][NACC], const __amdgpu_buffer_rsrc_t& r, uint32_t row_pitch) {
+            const uint32_t at = column(bj) < cols_valid ? (uint32_t)(column(bj) * OS) + (uint32_t)row(bi) * row_pitch : OOB;
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) {
+              uint32_t w[RS];
+#pragma unroll
+              for (int g = 0; g < GB; ++g) w[g] = trade(pack_out<OutT>(val[g][2 * h], val[g][2 * h + 1]));
+              swap_in(w);
+#pragma unroll
+              for (int i = 0; i < RS; ++i) {
+                const uint32_t off = at + (uint32_t)(row_of<C>(2 * h) + 4 * i) * row_pitch;
+                if (a.through) __builtin_amdgcn_raw_buffer_store_b32(w[i], r, off, 0, 16);
+                else __builtin_amdgcn_raw_buffer_store_b32(w[i], r, off, 0, 0);
+              }
+            }
+          };
+          if (keeps) put(z, rz, z_pitch);
+          put(y, rc, pitch);
+        }
+      }
+      return;
+    }
+    // ---- element accesses
+    constexpr int BLOCKS = C::MBLK * C::NBLK;
+    uint32_t in[2][NACC];
+    auto column = [&](int bj) { return p.col + bj * MB + frow; };
+    auto row = [&](int bi) { return p.row + bi * MB + 4 * fgrp; };
+    auto request = [&](int b, int set) {
+      const int bi = b % C::MBLK, bj = b / C::MBLK;
+      const uint32_t at = column(bj) < cols_valid ? (uint32_t)(column(bj) * xs) + (uint32_t)row(bi) * x_pitch : OOB;
+      if (xs == 4) {
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) in[set][v] = __builtin_amdgcn_raw_buffer_load_b32(rx, at + (uint32_t)row_of<C>(v) * x_pitch, 0, 0);
+      } else {
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) in[set][v] = __builtin_amdgcn_raw_buffer_load_b16(rx, at + (uint32_t)row_of<C>(v) * x_pitch, 0, 0);
+      }
+    };
+    if (reads) request(0, 0);
+#pragma unroll
+    for (int b = 0; b < BLOCKS; ++b) {
+      const int bi = b % C::MBLK, bj = b / C::MBLK;
+      if (reads && b + 1 < BLOCKS) request(b + 1, (b + 1) & 1);
+      float x[NACC], z[NACC], y[NACC];
+      if (reads) {
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) x[v] = OS == 4 || xs == 4 ? as_f32(in[b & 1][v]) : from_bits<OutT>(in[b & 1][v]);
+      }
+      compute(bi, bj, x, z, y);
+      auto put = [&](const float* val, const __amdgpu_buffer_rsrc_t& r, uint32_t row_pitch, auto policy_tag) {
+        constexpr int policy = decltype(policy_tag)::value;
+        const uint32_t at = column(bj) < cols_valid ? (uint32_t)(column(bj) * OS) + (uint32_t)row(bi) * row_pitch : OOB;
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) {
+          const uint32_t off = at + (uint32_t)row_of<C>(v) * row_pitch;
+          if constexpr (OS == 4) {
+            __builtin_amdgcn_raw_buffer_store_b32(as_u32(val[v]), r, off, 0, policy);
+          } else {
+            uint16_t bits;
+            store_out<OutT>(&bits, 0, val[v]);
+            __builtin_amdgcn_raw_buffer_store_b16(bits, r, off, 0, policy);
+          }
+        }
+      };
+      if (a.through) {
+        if (keeps) put(z, rz, z_pitch, std::integral_constant<int, 16>{});
+        put(y, rc, pitch, std::integral_constant<int, 16>{});
+      } else {
+        if (keeps) put(z, rz, z_pitch, std::integral_constant<int, 0>{});
+        put(y, rc, pitch, std::integral_constant<int, 0>{});
+      }
+    }
+  }
+
+  // ---- the logits of a wave's rows (vocabulary entries) reduced for each column (token).  A lane's registers are rows of one
+  // column, so the reduction stays inside the lane but for the two or four lane groups of a block at the end: with the tokens
+  // as rows it would cross 32 lanes for every row.
+  template <typename C, typename Acc>
+  static __device__ __attribute__((always_inline)) void finish_lse(const FusedArgs& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p) {
+    constexpr int MB = C::MB, NACC = MB * MB / 64;
+    constexpr float log2e = 1.44269504088896340736f;
+    const int lane = p.lane, frow = lane % MB, fgrp = lane / MB;
+    const int first = p.m0 + p.row;                                  // the wave's first row
+    const int rows = min(C::WM, a.store_m - first);
+    const int slab = first / C::WM;
+#pragma unroll
+    for (int bj = 0; bj < C::NBLK; ++bj) {
+      const int token = p.n0 + p.col + bj * MB + frow;
+      const bool there = token < a.store_n;
+      float top = -INFINITY;
+      if (rows < C::WM) {
+#pragma unroll
+        for (int bi = 0; bi < C::MBLK; ++bi)
+#pragma unroll
+          for (int v = 0; v < NACC; ++v)
+            if (bi * MB + row_of<C>(v) + 4 * fgrp >= rows) acc[bi][bj][v] = -INFINITY;
+      }
+#pragma unroll
+      for (int bi = 0; bi < C::MBLK; ++bi)
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) top = fmaxf(top, acc[bi][bj][v]);
+      const float ref = lse_reference(top);
+      float sum = 0.f;
+#pragma unroll
+      for (int bi = 0; bi < C::MBLK; ++bi) {
+        float part = 0.f;
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) part += __builtin_amdgcn_exp2f(log2e * (acc[bi][bj][v] - ref));
+        sum += part;
+      }
+#pragma unroll
+      for (int d = MB; d < 64; d *= 2) {
+        const float t2 = __shfl_xor(top, d, 64), s2 = __shfl_xor(sum, d, 64);
+        join_sums(top, sum, t2, s2);
+      }
+      if (there && fgrp == 0 && rows > 0) {
+        a.part_max[(int64_t)slab * a.tokens + token] = top;
+        a.part_sum[(int64_t)slab * a.tokens + token] = sum;
+      }
+      if (a.targets) {
+        const int64_t target = there ? a.targets[token] : -1;
+        const int at = target != a.ignore && target >= first && target < (int64_t)first + rows ? (int)(target - first) - 4 * fgrp : -1;
+        if (__any(at >= 0)) {
+#pragma unroll
+          for (int bi = 0; bi < C::MBLK; ++bi)
+#pragma unroll
+            for (int v = 0; v < NACC; ++v)
+              if (at == bi * MB + row_of<C>(v)) a.at_target[token] = acc[bi][bj][v];
+        }
+      }
+    }
+  }
+
+  // exp(d).  In fp32 the exponent's rounding (2^-24 of up to a hundred) is carried as a factor; 16-bit results round a thousand times
+  // coarser than it.
+  template <typename C> static __device__ float exponential(float d) {
+    constexpr float log2e = 1.44269504088896340736f;
+    const float t = log2e * d;
+    if constexpr (C::ES == 2) return __builtin_amdgcn_exp2f(t);
+    const float r = fmaf(log2e, d, -t) + 1.92596299e-8f * d;           // (log2(e) - log2e)
+    const float e = __builtin_amdgcn_exp2f(t);
+    return d > -100.f ? fmaf(e, 0.69314718f * r, e) : e;                // (-inf: inf - inf)
+  }
+
+  // ---- scale * dloss * (softmax - one at the target), in the input type, a product's operand next.  Columns beyond the tokens,
+  // up to whole vectors (store_n), are written as zeros.
+  template <typename C, typename Acc>
+  static __device__ __attribute__((always_inline)) void finish_prob(const FusedArgs& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p) {
+    constexpr int MB = C::MB, NACC = MB * MB / 64;
+    const int lane = p.lane, frow = lane % MB, fgrp = lane / MB;
+    const int first = p.m0 + p.row + a.row_first;
+    const float scale = a.scale ? *a.scale : 1.f;
+#pragma unroll
+    for (int bj = 0; bj < C::NBLK; ++bj) {
+      const int token = p.n0 + p.col + bj * MB + frow;
+      const bool there = token < a.tokens;
+      const int64_t target = there ? a.targets[token] : -1;
+      const bool counts = there && target != a.ignore && target >= 0 && target < a.vocab;
+      const float lse = counts ? a.lse[token] : INFINITY, g = counts ? a.dloss[token] * scale : 0.f;
+#pragma unroll
+      for (int bi = 0; bi < C::MBLK; ++bi)
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) acc[bi][bj][v] = g * exponential<C>(acc[bi][bj][v] - lse);
+      const int at = counts && target >= first && target < (int64_t)first + C::WM ? (int)(target - first) - 4 * fgrp : -1;
+      if (__any(at >= 0)) {
+#pragma unroll
+        for (int bi = 0; bi < C::MBLK; ++bi)
+#pragma unroll
+          for (int v = 0; v < NACC; ++v)
+            if (at == bi * MB + row_of<C>(v)) acc[bi][bj][v] -= g;
+      }
+    }
+    finish_linear<C, false>(a, acc, p);
+  }
+};
+
+// A split tile: the sum of its slots, through the same end.  (The slots' order and the reasons for a second launch stand at
+// split_reduce.)
+template <typename T, typename OutT>
+__global__ __launch_bounds__(256) void fused_split_reduce(const FusedArgs args, int bm, int bn, int wm, int wn, int mb) {
+  const int threads = (bm / wm) * (bn / wn) * 64;
+  const int groups = bm * bn / 4, blocks = groups >> 8;
+  const int u = blockIdx.x / blocks, r = (blockIdx.x - u * blocks) * 256 + threadIdx.x;
+  const int g = r / threads, tid = r - g * threads;
+  const int lane = tid & 63, wave = tid >> 6, waves_n = bn / wn, nblk = wn / mb;
+  const int per_block = mb == 32 ? 4 : 1;
+  const int b = g / per_block, q = g - b * per_block;
+  const int row = (wave / waves_n) * wm + (b / nblk) * mb + 8 * q + 4 * (lane / mb);
+  const int col = (wave % waves_n) * wn + (b % nblk) * mb + lane % mb;
+  const __amdgpu_buffer_rsrc_t slots = __builtin_amdgcn_make_buffer_rsrc((void*)((const f32x4*)args.partials + (int64_t)u * args.split * groups), 0,
+                                                                        (uint32_t)(args.split * groups * 16), 0x00020000u);
+  f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+  auto add = [&](auto n_tag) {
+    constexpr int n = decltype(n_tag)::value;
+    u32x4 v[n];
+#pragma unroll
+    for (int i = 0; i < n; ++i) v[i] = __builtin_amdgcn_raw_buffer_load_b128(slots, (uint32_t)((i * groups + r) * 16), 0, 2 /* nt */);
+#pragma unroll
+    for (int i = 0; i < n; ++i)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) sum[x] += as_f32(v[i][x]);
+  };
+  if (args.split <= 2) add(std::integral_constant<int, 2>{});
+  else if (args.split <= 4) add(std::integral_constant<int, 4>{});
+  else if (args.split <= 8) add(std::integral_constant<int, 8>{});
+  else add(std::integral_constant<int, 16>{});
+  int tile_m, tile_n;
+  tile_of(args, args.whole + u, tile_m, tile_n);
+  const int m = tile_m * bm + row, n = tile_n * bn + col;
+  if (n >= args.store_n) return;
+  const float alpha = args.alpha * (args.scale ? *args.scale : 1.f);
+  const float bias = args.bias ? to_float<T>(args.bias, n) : 0.f;
+  const ActForm form(args.act);
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    if (m + x >= args.store_m) break;
+    const float z = fmaf(alpha, sum[x], bias);
+    float y = z;
+    if (args.preact && args.grad) {
+      const float at = to_float<OutT>(args.preact, (int64_t)(m + x) * args.ld_preact + n);
+      if (args.act == ACT_RELU) y = at > 0.f ? z : 0.f;
+      else if (args.act != ACT_NONE) y = z * form.slope(at);
+    } else {
+      if (args.preact) store_out<OutT>(args.preact, (int64_t)(m + x) * args.ld_preact + n, z);
+      if (args.act == ACT_RELU) y = z < 0.f ? 0.f : z;
+      else if (args.act != ACT_NONE) y = form.value(z);
+    }
+    if (args.residual) {
+      const int64_t i = (int64_t)(m + x) * args.ld_residual + n;
+      y += args.residual_f32 ? to_float<f32_t>(args.residual, i) : to_float<OutT>(args.residual, i);
+    }
+    store_out<OutT>(args.C, (int64_t)(m + x) * args.ldc + n, y);
+  }
+}
+
+}  // namespace gensor

@@ -322,12 +322,30 @@ __device__ inline void tile_of(const KernelArgs& args, int t, int& tile_m, int& 
   tile_n = r / rows_here;
 }
 
+// What a launch does with the tile of a workgroup: `Args` are the kernel's arguments, `Local` what the kernel sees of them (a
+// copy, where a workgroup moves the operands to its own rows), MOVES whether `place` finds the workgroup's tile and moves
+// them, OWN_END whether `finish` takes the place of the plain epilogue.  This is the plain product.
+struct PlainOutput {
+  typedef KernelArgs Args;
+  typedef const KernelArgs& Local;
+  static constexpr bool MOVES = false, OWN_END = false;
+};
+
+// A wave's place in its workgroup's tile, for an epilogue of its own.
+struct TilePlace {
+  int m0, n0;                      // first row and column of the tile
+  int row, col;                    // ... and of the wave's tile inside it
+  int lane;
+};
+
 // ---------------------------------------------------------------- the kernel
 // SPLIT: the launch has split tiles (KernelArgs::split > 1); without it the kernel knows at compile time
 // that every workgroup owns a whole tile.  AHEAD: workgroups read the next batch's operands ahead (KernelArgs::ahead_a;
 // carrying the unused load through every launch cost the small batched ones 1-2 %).  MORE_SUMS: Cfg::DEEP_CHAINS.
-template <typename C, bool SPLIT = false, bool AHEAD = false, bool MORE_SUMS = false>
-__global__ __launch_bounds__(C::THREADS) void contraction_kernel(const KernelArgs args) {
+// F: what is done with the tile (PlainOutput).
+template <typename C, bool SPLIT = false, bool AHEAD = false, bool MORE_SUMS = false, typename F = PlainOutput>
+__global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename F::Args passed) {
+  typename F::Local args = passed;
   typedef typename C::T T;
   typedef Mfma<T, C::MB> MF;
   typedef typename MF::Acc Acc;
@@ -363,9 +381,13 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const KernelArg
     kpart = u / tiles;
     wg = args.whole + u - kpart * tiles;
   }
-  const int bidx = wg / tiles_per_batch;
-  int tile_m, tile_n;
-  tile_of(args, wg - bidx * tiles_per_batch, tile_m, tile_n);
+  int bidx, tile_m, tile_n;
+  if constexpr (F::MOVES) {
+    if (!F::template place<C>(args, bidx, tile_m, tile_n)) return;
+  } else {
+    bidx = wg / tiles_per_batch;
+    tile_of(args, wg - bidx * tiles_per_batch, tile_m, tile_n);
+  }
   const int m0 = tile_m * BM;
   const int n0 = tile_n * BN;
 
@@ -1459,6 +1481,11 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const KernelArg
       __builtin_amdgcn_raw_buffer_store_b128(v, slot, (uint32_t)((g * C::THREADS + tid) * 16), 0, WRITE_THROUGH);
       if (g % 8 == 7) __builtin_amdgcn_sched_barrier(0);
     }
+    return;
+  }
+
+  if constexpr (F::OWN_END) {
+    F::template finish<C>(args, acc, TilePlace{m0, n0, wave_m * C::WM, wave_n * C::WN, lane});
     return;
   }
 

@@ -90,6 +90,13 @@ inline bool narrow_tiles(const GemmView& v, int64_t compute_units) {
 struct LeadingDims { int64_t a, b, c; };
 bool offsets_fit(const InstanceDesc& d, const GemmView& v, const LeadingDims& ld);
 
+// Can the operands be read in whole 16-byte vectors?
+bool vector_ok(const GemmView& v, const void* A, int64_t lda, int64_t strideA, const void* B, int64_t ldb, int64_t strideB);
+
+// The cost model's time of a tile on a product whose result is consumed in place (that is, of the product), microseconds; not
+// positive: the tile does not serve.
+double fused_price(const InstanceDesc& d, const GemmView& v, int split);
+
 // gensor_construct with more inputs: whether the operands allow 16-byte vector accesses, the view (ViewMode) a
 // pointwise convolution is taken in, and, where only tiles whose offsets reach are wanted, the leading dimensions.
 // `ranked`: beside the best schedule, the best ones for less workspace than it needs, in order, down to one that needs none.

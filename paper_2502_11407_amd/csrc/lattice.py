@@ -315,6 +315,36 @@ def lattice():
     return out
 
 
+# Products that are consumed in place: END and MOVE of fused_kernel.hpp, and whether tiles may be split
+FUSED_KINDS = {"linear": "END_LINEAR, MOVE_NONE", "linear_split": "END_LINEAR, MOVE_NONE, true", "rows": "END_LINEAR, MOVE_ROWS",
+               "depth": "END_LINEAR, MOVE_DEPTH", "lse": "END_LSE, MOVE_NONE", "prob": "END_PROB, MOVE_NONE"}
+
+
+def fused():
+    """Their tiles: of the lattice above those that take any K, from the largest to the smallest, aligned and at any alignment.  Every tile
+    exists for the operand layouts and ends that some operator has: A k-contiguous with either B (activations times weights, grouped
+    or not), A m-contiguous with an n-contiguous B (sums over rows: weight gradients), both k-contiguous (logits)."""
+    tiles16 = [(256, 256, 64, 128, 64, 16, 1, 2, 1), (256, 128, 64, 64, 64, 16, 1, 3, 1), (128, 256, 64, 64, 64, 16, 1, 3, 1),
+               (128, 128, 64, 64, 32, 16, 1, 4, 1), (64, 64, 64, 32, 32, 32, 1, 2, 0), (32, 32, 128, 16, 16, 16, 1, 2, 0),
+               (128, 128, 64, 64, 32, 32, 0, 2, 0), (64, 64, 64, 32, 32, 32, 0, 2, 0), (32, 32, 128, 16, 16, 16, 0, 2, 0)]
+    tiles32 = [(128, 128, 32, 64, 64, 32, 1, 2, 0), (64, 64, 32, 32, 32, 32, 1, 2, 0), (32, 32, 64, 16, 16, 16, 1, 2, 0),
+               (128, 128, 32, 64, 64, 32, 0, 2, 0), (64, 64, 32, 32, 32, 32, 0, 2, 0), (32, 32, 64, 16, 16, 16, 0, 2, 0)]
+    out = []
+    for dt in ("f16", "bf16", "f32"):
+        for (bm, bn, bk, wm, wn, mb, vec, stages, direct) in (tiles32 if dt == "f32" else tiles16):
+            for odt in ((dt,) if dt == "f32" else ("f32", dt)):
+                for asrc, bsrc in (("KC", "KC"), ("KC", "NC"), ("MC", "NC")):
+                    d = _inst(dt, odt, bm, bn, bk, wm, wn, mb, bsrc=bsrc, vec=vec, stages=stages, direct=direct, asrc=asrc)
+                    kinds = ["linear", "linear_split", "rows" if asrc == "KC" else "depth"]
+                    if asrc == "KC" and bsrc == "KC" and odt == dt:
+                        kinds += ["lse", "prob"]
+                    d["kinds"] = kinds
+                    out.append(d)
+    for i, d in enumerate(out):
+        d["id"] = i
+    return out
+
+
 def cfg_type(d):
     if conv_rows(d):
         return "ConvRowsCfg<%s, %s, %d, %d, %d, %d>" % (CT[d["dt"]], CT[d["out"]], d["bm"], d["bn"], d["wm"], d["wn"])
