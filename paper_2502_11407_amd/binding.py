@@ -336,84 +336,103 @@ def to_host_f64(t) -> np.ndarray:
 
 # ---- products that are consumed where they are produced.  Shapes and types are checked here against the problem, because the library
 # sees addresses only.
-_NAMES = None
+_TORCH = None        # torch's type of a gensor_dtype, and the other way round, once torch is imported
+_CODE = None
 
 
-def _dtype_name(t) -> str:
-    global _NAMES
-    if _NAMES is None:
-        import torch
-        _NAMES = {torch.float32: "f32", torch.float16: "f16", torch.bfloat16: "bf16"}
-    return _NAMES.get(t.dtype, str(t.dtype))
+def _torch_types():
+    global _TORCH, _CODE
+    import torch
+    _TORCH = (torch.float32, torch.float16, torch.bfloat16)
+    _CODE = {t: i for i, t in enumerate(_TORCH)}
 
 
-def _matrix(t, rows: int, cols: int, dtype: int, what: str) -> int:
+def _code(t, what: str) -> int:
+    """The gensor_dtype of a tensor."""
+    if _CODE is None:
+        _torch_types()
+    code = _CODE.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what}: f32, f16 and bf16 are served, got {t.dtype}")
+    return code
+
+
+def _matrix(t, rows: int, cols: int, dtype, what: str) -> int:
     """Checks a device matrix with unit inner stride against what the problem says it is; its leading dimension."""
-    if tuple(t.shape) != (rows, cols) or DTYPE.get(_dtype_name(t)) != dtype or not t.is_cuda:
-        raise ValueError(f"{what}: a device matrix of {rows} x {cols} of dtype {dtype} is wanted, got {tuple(t.shape)} {t.dtype} on {t.device}")
-    ld, inner = t.stride()
-    if (cols > 1 and inner != 1) or (rows > 1 and ld < cols):
+    if t.shape == (rows, cols) and t.dtype is dtype and t.is_cuda:
+        ld, inner = t.stride()
+        if inner == 1 and ld >= cols:
+            return ld
+        if (cols == 1 or inner == 1) and (rows == 1 or ld >= cols):
+            return ld if rows > 1 else cols
         raise ValueError(f"{what}: contiguous rows that do not overlap are wanted, got strides {t.stride()}")
-    return ld if rows > 1 else cols
+    raise ValueError(f"{what}: a device matrix of {rows} x {cols} {dtype} is wanted, got {tuple(t.shape)} {t.dtype} on {t.device}")
 
 
 def _vector(t, n: int, dtype: str, what: str) -> int:
-    if tuple(t.shape) != (n,) or not t.is_contiguous() or not t.is_cuda or str(t.dtype) != "torch." + dtype:
+    if t.shape != (n,) or not t.is_contiguous() or not t.is_cuda or str(t.dtype) != dtype:
         raise ValueError(f"{what}: a contiguous device vector of {n} {dtype} is wanted, got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
-def _stack(t, groups: int, rows: int, cols: int, dtype: int, what: str):
+def _stack(t, groups: int, rows: int, cols: int, dtype, what: str):
     """The same for a stack of matrices: (leading dimension, distance between matrices)."""
-    if t.dim() != 3 or t.shape[0] != groups:
-        raise ValueError(f"{what}: {groups} matrices are wanted, got {tuple(t.shape)}")
-    return _matrix(t[0], rows, cols, dtype, what), t.stride(0) if groups > 1 else 0
+    if t.shape == (groups, rows, cols) and t.dtype is dtype and t.is_cuda:
+        far, ld, inner = t.stride()
+        if (cols == 1 or inner == 1) and (rows == 1 or ld >= cols):
+            return ld if rows > 1 else cols, far if groups > 1 else 0
+        raise ValueError(f"{what}: contiguous rows that do not overlap are wanted, got strides {t.stride()}")
+    raise ValueError(f"{what}: a device stack of {groups} matrices of {rows} x {cols} {dtype} is wanted, got {tuple(t.shape)} {t.dtype} on {t.device}")
 
 
-def _epilogue(p: Problem, rows: int, bias, act: str, preact, residual, grad: int):
+def _epilogue(rows: int, N: int, bias_shape, dtype, out, bias, act: str, preact, residual, grad: int):
     """The epilogue's structure, or None for the plain product."""
-    if act not in ACT:
+    code = ACT.get(act)
+    if code is None:
         raise ValueError(f"act: one of {sorted(ACT)} is wanted, got {act!r}")
-    if bias is None and preact is None and residual is None and act == "none" and not grad:
+    if bias is None and preact is None and residual is None and code == 0 and not grad:
         return None
-    e = Epilogue()
-    e.act, e.grad = ACT[act], grad
+    e = Epilogue(code, grad)
     if bias is not None:
-        shape = (p.batch, p.N) if p.op == OP_BMM else (p.N,)
-        if tuple(bias.shape) != shape or not bias.is_contiguous() or DTYPE.get(_dtype_name(bias)) != p.in_dtype or not bias.is_cuda:
-            raise ValueError(f"bias: a contiguous device tensor of {shape} in the input type is wanted, got {tuple(bias.shape)} {bias.dtype} on {bias.device}")
+        if bias.shape != bias_shape or not bias.is_contiguous() or bias.dtype is not dtype or not bias.is_cuda:
+            raise ValueError(f"bias: a contiguous device tensor of {bias_shape} {dtype} is wanted, got {tuple(bias.shape)} {bias.dtype} on {bias.device}")
         e.bias = bias.data_ptr()
     if preact is not None:
-        e.ld_preact = _matrix(preact, rows, p.N, p.out_dtype, "preact")
+        e.ld_preact = _matrix(preact, rows, N, out, "preact")
         e.preact = preact.data_ptr()
     if residual is not None:
-        e.ld_residual = _matrix(residual, rows, p.N, p.out_dtype, "residual")
+        e.ld_residual = _matrix(residual, rows, N, out, "residual")
         e.residual = residual.data_ptr()
-    return e
+    return C.byref(e)
 
 
 def gemm_fused_workspace_bytes(p: Problem) -> int:
     return int(lib.gensor_gemm_fused_workspace_bytes(C.byref(p)))
 
 
-def _gemm_fused(p, A, B, Cout, e, alpha, workspace, stream):
-    lda = _matrix(A, *((p.K, p.M) if p.transA else (p.M, p.K)), p.in_dtype, "A")
-    ldb = _matrix(B, *((p.N, p.K) if p.transB else (p.K, p.N)), p.in_dtype, "B")
-    ldc = _matrix(Cout, p.M, p.N, p.out_dtype, "C")
-    ws_ptr, ws_len = _ws(workspace)
-    _check(lib.gensor_gemm_fused(C.byref(p), _sref(e), alpha, A.data_ptr(), lda, B.data_ptr(), ldb, Cout.data_ptr(), ldc, ws_ptr, ws_len,
-                                 _stream_ptr(stream)), "gensor_gemm_fused")
+def _gemm_fused(p, A, B, Cout, bias, act, preact, residual, grad, alpha, workspace, stream):
+    if _TORCH is None:
+        _torch_types()
+    M, N, K, dtype, out = p.M, p.N, p.K, _TORCH[p.in_dtype], _TORCH[p.out_dtype]
+    e = _epilogue(M, N, (N,), dtype, out, bias, act, preact, residual, grad)
+    lda = _matrix(A, K, M, dtype, "A") if p.transA else _matrix(A, M, K, dtype, "A")
+    ldb = _matrix(B, N, K, dtype, "B") if p.transB else _matrix(B, K, N, dtype, "B")
+    ldc = _matrix(Cout, M, N, out, "C")
+    ws_ptr, ws_len = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    st = lib.gensor_gemm_fused(C.byref(p), e, alpha, A.data_ptr(), lda, B.data_ptr(), ldb, Cout.data_ptr(), ldc, ws_ptr, ws_len, _stream_ptr(stream))
+    if st:
+        _check(st, "gensor_gemm_fused")
 
 
 def gemm_fused(p: Problem, A, B, Cout, bias=None, act: str = "none", preact=None, residual=None, alpha: float = 1.0, stream=None, workspace=None):
     """C = act(Z) + residual with Z = alpha op(A) op(B) + bias; `preact`, if given, receives Z.  act: none, relu, gelu (tanh form), silu.
     `workspace`: device tensor of gemm_fused_workspace_bytes(p) bytes, or less, or None."""
-    _gemm_fused(p, A, B, Cout, _epilogue(p, p.M, bias, act, preact, residual, 0), alpha, workspace, stream)
+    _gemm_fused(p, A, B, Cout, bias, act, preact, residual, 0, alpha, workspace, stream)
 
 
 def gemm_act_grad(p: Problem, A, B, preact, Cout, act: str, alpha: float = 1.0, stream=None, workspace=None):
     """C = (alpha op(A) op(B)) * act'(preact): the gradient that reaches an activation's input, from the product behind it."""
-    _gemm_fused(p, A, B, Cout, _epilogue(p, p.M, None, act, preact, None, 1), alpha, workspace, stream)
+    _gemm_fused(p, A, B, Cout, None, act, preact, None, 1, alpha, workspace, stream)
 
 
 def grouped_problem(dtype: str, groups: int, rows: int, N: int, K: int, transB: int = 0, out_dtype: str = "f32") -> Problem:
@@ -423,35 +442,42 @@ def grouped_problem(dtype: str, groups: int, rows: int, N: int, K: int, transB: 
     return p
 
 
+def _grouped_gemm(p, offsets, A, B, Cout, bias, act, preact, residual, grad, alpha, stream):
+    if _TORCH is None:
+        _torch_types()
+    G, M, N, K, dtype, out = p.batch, p.M, p.N, p.K, _TORCH[p.in_dtype], _TORCH[p.out_dtype]
+    off = _vector(offsets, G + 1, "torch.int32", "offsets")
+    lda, ldc = _matrix(A, M, K, dtype, "A"), _matrix(Cout, M, N, out, "C")
+    ldb, stride = _stack(B, G, N, K, dtype, "B") if p.transB else _stack(B, G, K, N, dtype, "B")
+    e = _epilogue(M, N, (G, N), dtype, out, bias, act, preact, residual, grad)
+    if M == 0:                                     # (nothing to do, and an empty tensor has no address)
+        return
+    st = lib.gensor_grouped_gemm(C.byref(p), off, e, alpha, A.data_ptr(), lda, B.data_ptr(), ldb, stride, Cout.data_ptr(), ldc, _stream_ptr(stream))
+    if st:
+        _check(st, "gensor_grouped_gemm")
+
+
 def grouped_gemm(p: Problem, offsets, A, B, Cout, bias=None, act: str = "none", preact=None, residual=None, alpha: float = 1.0, stream=None):
     """Rows offsets[g] .. offsets[g+1] of C = act(alpha A B[g] + bias[g]) + residual.  offsets: groups + 1 int32 on the device."""
-    off = _vector(offsets, p.batch + 1, "int32", "offsets")
-    lda, ldc = _matrix(A, p.M, p.K, p.in_dtype, "A"), _matrix(Cout, p.M, p.N, p.out_dtype, "C")
-    ldb, stride = _stack(B, p.batch, *((p.N, p.K) if p.transB else (p.K, p.N)), p.in_dtype, "B")
-    e = _epilogue(p, p.M, bias, act, preact, residual, 0)
-    if p.M > 0:
-        _check(lib.gensor_grouped_gemm(C.byref(p), off, _sref(e), alpha, A.data_ptr(), lda, B.data_ptr(), ldb, stride, Cout.data_ptr(), ldc,
-                                       _stream_ptr(stream)), "gensor_grouped_gemm")
+    _grouped_gemm(p, offsets, A, B, Cout, bias, act, preact, residual, 0, alpha, stream)
 
 
 def grouped_act_grad(p: Problem, offsets, A, B, preact, Cout, act: str, alpha: float = 1.0, stream=None):
     """Rows offsets[g] .. offsets[g+1] of C = (alpha A B[g]) * act'(preact)."""
-    off = _vector(offsets, p.batch + 1, "int32", "offsets")
-    lda, ldc = _matrix(A, p.M, p.K, p.in_dtype, "A"), _matrix(Cout, p.M, p.N, p.out_dtype, "C")
-    ldb, stride = _stack(B, p.batch, *((p.N, p.K) if p.transB else (p.K, p.N)), p.in_dtype, "B")
-    e = _epilogue(p, p.M, None, act, preact, None, 1)
-    if p.M > 0:
-        _check(lib.gensor_grouped_gemm(C.byref(p), off, _sref(e), alpha, A.data_ptr(), lda, B.data_ptr(), ldb, stride, Cout.data_ptr(), ldc,
-                                       _stream_ptr(stream)), "gensor_grouped_gemm")
+    _grouped_gemm(p, offsets, A, B, Cout, None, act, preact, None, 1, alpha, stream)
 
 
 def grouped_wgrad(p: Problem, offsets, A, dY, dW, stream=None):
     """dW[g] = A_g^T dY_g over the rows of g, laid out like the B of `p`: the gradient of grouped_gemm's B for the same problem."""
-    off = _vector(offsets, p.batch + 1, "int32", "offsets")
-    lda, lddy = _matrix(A, p.M, p.K, p.in_dtype, "A"), _matrix(dY, p.M, p.N, p.in_dtype, "dY")
-    lddw, stride = _stack(dW, p.batch, *((p.N, p.K) if p.transB else (p.K, p.N)), p.out_dtype, "dW")
-    _check(lib.gensor_grouped_wgrad(C.byref(p), off, A.data_ptr(), lda, dY.data_ptr(), lddy, dW.data_ptr(), lddw, stride, _stream_ptr(stream)),
-           "gensor_grouped_wgrad")
+    if _TORCH is None:
+        _torch_types()
+    G, M, N, K, dtype, out = p.batch, p.M, p.N, p.K, _TORCH[p.in_dtype], _TORCH[p.out_dtype]
+    off = _vector(offsets, G + 1, "torch.int32", "offsets")
+    lda, lddy = _matrix(A, M, K, dtype, "A"), _matrix(dY, M, N, dtype, "dY")
+    lddw, stride = _stack(dW, G, N, K, out, "dW") if p.transB else _stack(dW, G, K, N, out, "dW")
+    st = lib.gensor_grouped_wgrad(C.byref(p), off, A.data_ptr(), lda, dY.data_ptr(), lddy, dW.data_ptr(), lddw, stride, _stream_ptr(stream))
+    if st:
+        _check(st, "gensor_grouped_wgrad")
 
 
 def bias_grad_workspace_bytes(groups: int, rows: int, N: int, dtype: str = "bf16") -> int:
@@ -461,17 +487,16 @@ def bias_grad_workspace_bytes(groups: int, rows: int, N: int, dtype: str = "bf16
 def bias_grad(dY, db, offsets=None, stream=None, workspace=None):
     """db = column sums of dY [rows][N]; with offsets (groups + 1 int32 on the device) db[g] = column sums of the rows of g."""
     rows, N = dY.shape
-    dt, out = _dtype_name(dY), _dtype_name(db)
-    if dt not in DTYPE or out not in DTYPE:
-        raise ValueError(f"bias_grad: f32, f16 and bf16 are served, got {dY.dtype} and {db.dtype}")
+    dt, out = _code(dY, "dY"), _code(db, "db")
     groups = 1 if offsets is None else offsets.shape[0] - 1
-    off = None if offsets is None else _vector(offsets, groups + 1, "int32", "offsets")
-    if tuple(db.shape) != ((N,) if offsets is None else (groups, N)) or not db.is_contiguous() or not db.is_cuda:
+    off = None if offsets is None else _vector(offsets, groups + 1, "torch.int32", "offsets")
+    if db.shape != ((N,) if offsets is None else (groups, N)) or not db.is_contiguous() or not db.is_cuda:
         raise ValueError(f"db: a contiguous device tensor of {(N,) if offsets is None else (groups, N)} is wanted, got {tuple(db.shape)} on {db.device}")
-    ld = _matrix(dY, rows, N, DTYPE[dt], "dY")
-    ws_ptr, ws_len = _ws(workspace)
-    _check(lib.gensor_bias_grad(DTYPE[dt], DTYPE[out], groups, rows, N, dY.data_ptr(), ld, off, db.data_ptr(), ws_ptr, ws_len, _stream_ptr(stream)),
-           "gensor_bias_grad")
+    ld = _matrix(dY, rows, N, dY.dtype, "dY")
+    ws_ptr, ws_len = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    st = lib.gensor_bias_grad(dt, out, groups, rows, N, dY.data_ptr(), ld, off, db.data_ptr(), ws_ptr, ws_len, _stream_ptr(stream))
+    if st:
+        _check(st, "gensor_bias_grad")
 
 
 def xent_workspace_bytes(dtype: str, T: int, V: int, D: int, backward: bool = False) -> int:
@@ -482,24 +507,24 @@ def xent_forward(X, W, targets, loss, lse, ignore_index: int = -100, stream=None
     """loss[t] = lse[t] - z[t][targets[t]] and lse[t] = log sum exp z[t] of the logits z = X W^T, which are never stored: X [T][D], W [V][D] of
     one type, targets [T] int64, loss and lse [T] fp32 (either may be None).  `workspace`: xent_workspace_bytes(...) bytes."""
     (T, D), (V, _) = X.shape, W.shape
-    dt = DTYPE.get(_dtype_name(X), -1)
-    ldx, ldw = _matrix(X, T, D, dt, "X"), _matrix(W, V, D, dt, "W")
-    ws_ptr, ws_len = _ws(workspace)
+    dt, dtype = _code(X, "X"), X.dtype
+    ldx, ldw = _matrix(X, T, D, dtype, "X"), _matrix(W, V, D, dtype, "W")
+    ws_ptr, ws_len = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
     _check(lib.gensor_xent_forward(dt, T, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw,
-                                   None if targets is None else _vector(targets, T, "int64", "targets"), ignore_index,
-                                   None if loss is None else _vector(loss, T, "float32", "loss"),
-                                   None if lse is None else _vector(lse, T, "float32", "lse"), ws_ptr, ws_len, _stream_ptr(stream)), "gensor_xent_forward")
+                                   None if targets is None else _vector(targets, T, "torch.int64", "targets"), ignore_index,
+                                   None if loss is None else _vector(loss, T, "torch.float32", "loss"),
+                                   None if lse is None else _vector(lse, T, "torch.float32", "lse"), ws_ptr, ws_len, _stream_ptr(stream)), "gensor_xent_forward")
 
 
 def xent_backward(X, W, targets, lse, dloss, dX, dW, ignore_index: int = -100, stream=None, workspace=None):
     """dX = G W and dW = G^T X with G[t][v] = dloss[t] (exp(z[t][v] - lse[t]) - (v == targets[t])); dX or dW may be None.
     `workspace`: xent_workspace_bytes(..., backward=True) bytes, or less for smaller pieces of the vocabulary."""
     (T, D), (V, _) = X.shape, W.shape
-    dt = DTYPE.get(_dtype_name(X), -1)
-    ldx, ldw = _matrix(X, T, D, dt, "X"), _matrix(W, V, D, dt, "W")
-    ws_ptr, ws_len = _ws(workspace)
-    _check(lib.gensor_xent_backward(dt, T, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, _vector(targets, T, "int64", "targets"), ignore_index,
-                                    _vector(lse, T, "float32", "lse"), _vector(dloss, T, "float32", "dloss"),
-                                    None if dX is None else dX.data_ptr(), 0 if dX is None else _matrix(dX, T, D, dt, "dX"),
-                                    None if dW is None else dW.data_ptr(), 0 if dW is None else _matrix(dW, V, D, dt, "dW"),
+    dt, dtype = _code(X, "X"), X.dtype
+    ldx, ldw = _matrix(X, T, D, dtype, "X"), _matrix(W, V, D, dtype, "W")
+    ws_ptr, ws_len = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    _check(lib.gensor_xent_backward(dt, T, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, _vector(targets, T, "torch.int64", "targets"), ignore_index,
+                                    _vector(lse, T, "torch.float32", "lse"), _vector(dloss, T, "torch.float32", "dloss"),
+                                    None if dX is None else dX.data_ptr(), 0 if dX is None else _matrix(dX, T, D, dtype, "dX"),
+                                    None if dW is None else dW.data_ptr(), 0 if dW is None else _matrix(dW, V, D, dtype, "dW"),
                                     ws_ptr, ws_len, _stream_ptr(stream)), "gensor_xent_backward")

@@ -106,6 +106,8 @@ struct Fused {
   typedef FusedArgs Args;
   typedef std::conditional_t<MOVE != MOVE_NONE, FusedArgs, const FusedArgs&> Local;
   static constexpr bool MOVES = MOVE != MOVE_NONE, OWN_END = true;
+  // Stores of a wave that `finish` issues at least (a pair of 16-bit values is one); the logits' reduction stores next to nothing
+  template <typename C> static constexpr int MIN_STORES = END == END_LSE ? 0 : C::WM * C::WN / 64 / (ElemSize<typename C::OutT>::value == 2 ? 2 : 1);
 
   // The workgroup's tile; false: there is none for it.  The launch has as many workgroups as the row counts could
   // need, ceil(rows / BM) of each group at worst; every wave counts the tiles there are by itself (64 groups at a time, one
@@ -114,11 +116,21 @@ struct Fused {
   static __device__ __attribute__((always_inline)) bool place(FusedArgs& a, int& bidx, int& tile_m, int& tile_n) {
     constexpr int ES = C::ES, OS = ElemSize<typename C::OutT>::value;
     if constexpr (MOVE == MOVE_DEPTH) {
+      // The tiles of the group with the most rows start first, then the next one's: a tile's time is its group's rows, and a long
+      // one started last would run alone.  Each group's tiles are dealt over all XCDs in contiguous ranges.  (Of more than 64
+      // groups the order is kept among 64 at a time.)
       const int per = a.tiles_m * a.tiles_n;
-      const int wg = xcd_contiguous(blockIdx.x, per * a.batch);
-      bidx = wg / per;
-      tile_of(a, wg - bidx * per, tile_m, tile_n);
-      int first, count;
+      const int turn = blockIdx.x / per, g0 = turn & ~63, lane = threadIdx.x & 63;
+      int first, count = -1;
+      if (g0 + lane < a.groups) group_rows(a, g0 + lane, first, count);
+      int before = 0;
+#pragma unroll 8
+      for (int i = 0; i < 64; ++i) {
+        const int other = __builtin_amdgcn_readlane(count, i);
+        before += other > count || (other == count && i < lane);
+      }
+      bidx = g0 + __builtin_ctzll(__ballot(before == (turn & 63)));
+      tile_of(a, xcd_contiguous(blockIdx.x - turn * per, per), tile_m, tile_n);
       group_rows(a, bidx, first, count);
       a.A = (const char*)a.A + (int64_t)first * a.lda * ES;
       a.B = (const char*)a.B + (int64_t)first * a.ldb * ES;
@@ -187,9 +199,10 @@ struct Fused {
     }
   }
 
-  template <typename C, typename Acc>
-  static __device__ __attribute__((always_inline)) void finish(const FusedArgs& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p) {
-    if constexpr (END == END_LSE) finish_lse<C>(a, acc, p);
+  // before_stores: called where everything is computed and only stores follow (END_LSE)
+  template <typename C, typename Acc, typename Hook>
+  static __device__ __attribute__((always_inline)) void finish(const FusedArgs& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p, Hook&& before_stores) {
+    if constexpr (END == END_LSE) finish_lse<C>(a, acc, p, before_stores);
     else if constexpr (END == END_PROB) finish_prob<C>(a, acc, p);
     else finish_linear<C, true>(a, acc, p);
   }
@@ -309,7 +322,8 @@ struct Fused {
           }
         };
         constexpr int UNITS = C::MBLK * (C::NBLK / GB), HALVES = NACC / 2;
-        uint32_t in[2][HALVES][RS];
+        constexpr int AHEAD = UNITS * HALVES * RS <= 32 ? UNITS : 32 / (HALVES * RS);
+        uint32_t in[AHEAD][HALVES][RS];
         auto column = [&](int bj) { return p.col + bj * MB + (lane % (GB * MB) & ~1); };
         auto row = [&](int bi) { return p.row + bi * MB + (lane & 1) + (HALF_LINES ? 8 * (lane >> 5) : 0); };
         auto request = [&](int u, int set) {
@@ -320,18 +334,20 @@ struct Fused {
 #pragma unroll
             for (int i = 0; i < RS; ++i) in[set][h][i] = __builtin_amdgcn_raw_buffer_load_b32(rx, at + (uint32_t)(row_of<C>(2 * h) + 4 * i) * x_pitch, 0, 0);
         };
-        if (reads) request(0, 0);
+        if (reads) {
+#pragma unroll
+          for (int u = 0; u < AHEAD; ++u) request(u, u);
+        }
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
           const int bi = u % C::MBLK, bj = u / C::MBLK * GB;
-          if (reads && u + 1 < UNITS) request(u + 1, (u + 1) & 1);
           float x[GB][NACC], z[GB][NACC], y[GB][NACC];
           if (reads) {
 #pragma unroll
             for (int h = 0; h < HALVES; ++h) {
               uint32_t w[RS];
 #pragma unroll
-              for (int i = 0; i < RS; ++i) w[i] = in[u & 1][h][i];
+              for (int i = 0; i < RS; ++i) w[i] = in[u % AHEAD][h][i];
               swap_out(w);
 #pragma unroll
               for (int g = 0; g < GB; ++g) {
@@ -343,6 +359,7 @@ struct Fused {
               }
             }
           }
+          if (reads && u + AHEAD < UNITS) request(u + AHEAD, u % AHEAD);
 #pragma unroll
           for (int g = 0; g < GB; ++g) compute(bi, bj + g, x[g], z[g], y[g]);
           auto put = [&](const float (&val)[GB][NACC], const __amdgpu_buffer_rsrc_t& r, uint32_t row_pitch) {
@@ -369,7 +386,8 @@ struct Fused {
     }
     // ---- element accesses
     constexpr int BLOCKS = C::MBLK * C::NBLK;
-    uint32_t in[2][NACC];
+    constexpr int AHEAD = BLOCKS * NACC <= 32 ? BLOCKS : 32 / NACC;
+    uint32_t in[AHEAD][NACC];
     auto column = [&](int bj) { return p.col + bj * MB + frow; };
     auto row = [&](int bi) { return p.row + bi * MB + 4 * fgrp; };
     auto request = [&](int b, int set) {
@@ -383,16 +401,19 @@ struct Fused {
         for (int v = 0; v < NACC; ++v) in[set][v] = __builtin_amdgcn_raw_buffer_load_b16(rx, at + (uint32_t)row_of<C>(v) * x_pitch, 0, 0);
       }
     };
-    if (reads) request(0, 0);
+    if (reads) {
+#pragma unroll
+      for (int b = 0; b < AHEAD; ++b) request(b, b);
+    }
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b) {
       const int bi = b % C::MBLK, bj = b / C::MBLK;
-      if (reads && b + 1 < BLOCKS) request(b + 1, (b + 1) & 1);
       float x[NACC], z[NACC], y[NACC];
       if (reads) {
 #pragma unroll
-        for (int v = 0; v < NACC; ++v) x[v] = OS == 4 || xs == 4 ? as_f32(in[b & 1][v]) : from_bits<OutT>(in[b & 1][v]);
+        for (int v = 0; v < NACC; ++v) x[v] = OS == 4 || xs == 4 ? as_f32(in[b % AHEAD][v]) : from_bits<OutT>(in[b % AHEAD][v]);
       }
+      if (reads && b + AHEAD < BLOCKS) request(b + AHEAD, b % AHEAD);
       compute(bi, bj, x, z, y);
       auto put = [&](const float* val, const __amdgpu_buffer_rsrc_t& r, uint32_t row_pitch, auto policy_tag) {
         constexpr int policy = decltype(policy_tag)::value;
@@ -422,14 +443,16 @@ struct Fused {
   // ---- the logits of a wave's rows (vocabulary entries) reduced for each column (token).  A lane's registers are rows of one
   // column, so the reduction stays inside the lane but for the two or four lane groups of a block at the end: with the tokens
   // as rows it would cross 32 lanes for every row.
-  template <typename C, typename Acc>
-  static __device__ __attribute__((always_inline)) void finish_lse(const FusedArgs& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p) {
+  template <typename C, typename Acc, typename Hook>
+  static __device__ __attribute__((always_inline)) void finish_lse(const FusedArgs& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p, Hook&& before_stores) {
     constexpr int MB = C::MB, NACC = MB * MB / 64;
     constexpr float log2e = 1.44269504088896340736f;
     const int lane = p.lane, frow = lane % MB, fgrp = lane / MB;
     const int first = p.m0 + p.row;                                  // the wave's first row
     const int rows = min(C::WM, a.store_m - first);
     const int slab = first / C::WM;
+    float tops[C::NBLK], sums[C::NBLK], at_target[C::NBLK];
+    bool hit[C::NBLK];
 #pragma unroll
     for (int bj = 0; bj < C::NBLK; ++bj) {
       const int token = p.n0 + p.col + bj * MB + frow;
@@ -446,24 +469,35 @@ struct Fused {
       for (int bi = 0; bi < C::MBLK; ++bi)
 #pragma unroll
         for (int v = 0; v < NACC; ++v) top = fmaxf(top, acc[bi][bj][v]);
+      // exp(z - ref) in three operations: the product log2e * ref is rounded, which multiplies every term by the same factor 2^off; it is taken
+      // out of the sum, so that the maximum's own term is 1.  (Where that product would not be finite: four operations.)
       const float ref = lse_reference(top);
       float sum = 0.f;
+      if (__any(fabsf(ref) > 1e37f)) {
 #pragma unroll
-      for (int bi = 0; bi < C::MBLK; ++bi) {
-        float part = 0.f;
+        for (int bi = 0; bi < C::MBLK; ++bi)
 #pragma unroll
-        for (int v = 0; v < NACC; ++v) part += __builtin_amdgcn_exp2f(log2e * (acc[bi][bj][v] - ref));
-        sum += part;
+          for (int v = 0; v < NACC; ++v) sum += __builtin_amdgcn_exp2f(log2e * (acc[bi][bj][v] - ref));
+      } else {
+        const float base = -(log2e * ref), off = fmaf(log2e, ref, base);
+#pragma unroll
+        for (int bi = 0; bi < C::MBLK; ++bi) {
+          float part = 0.f;
+#pragma unroll
+          for (int v = 0; v < NACC; ++v) part += __builtin_amdgcn_exp2f(fmaf(log2e, acc[bi][bj][v], base));
+          sum += part;
+        }
+        sum *= __builtin_amdgcn_exp2f(-off);
       }
 #pragma unroll
       for (int d = MB; d < 64; d *= 2) {
         const float t2 = __shfl_xor(top, d, 64), s2 = __shfl_xor(sum, d, 64);
         join_sums(top, sum, t2, s2);
       }
-      if (there && fgrp == 0 && rows > 0) {
-        a.part_max[(int64_t)slab * a.tokens + token] = top;
-        a.part_sum[(int64_t)slab * a.tokens + token] = sum;
-      }
+      tops[bj] = top;
+      sums[bj] = sum;
+      hit[bj] = false;
+      at_target[bj] = 0.f;
       if (a.targets) {
         const int64_t target = there ? a.targets[token] : -1;
         const int at = target != a.ignore && target >= first && target < (int64_t)first + rows ? (int)(target - first) - 4 * fgrp : -1;
@@ -472,9 +506,22 @@ struct Fused {
           for (int bi = 0; bi < C::MBLK; ++bi)
 #pragma unroll
             for (int v = 0; v < NACC; ++v)
-              if (at == bi * MB + row_of<C>(v)) a.at_target[token] = acc[bi][bj][v];
+              if (at == bi * MB + row_of<C>(v)) {
+                hit[bj] = true;
+                at_target[bj] = acc[bi][bj][v];
+              }
         }
       }
+    }
+    before_stores();
+#pragma unroll
+    for (int bj = 0; bj < C::NBLK; ++bj) {
+      const int token = p.n0 + p.col + bj * MB + frow;
+      if (token < a.store_n && fgrp == 0 && rows > 0) {
+        a.part_max[(int64_t)slab * a.tokens + token] = tops[bj];
+        a.part_sum[(int64_t)slab * a.tokens + token] = sums[bj];
+      }
+      if (hit[bj]) a.at_target[token] = at_target[bj];
     }
   }
 
@@ -521,6 +568,29 @@ struct Fused {
   }
 };
 
+// One element of C from its product's sum, through the linear end.
+template <typename T, typename OutT>
+__device__ inline void finish_element(const FusedArgs& args, int m, int n, float sum) {
+  const float alpha = args.alpha * (args.scale ? *args.scale : 1.f);
+  const float z = fmaf(alpha, sum, args.bias ? to_float<T>(args.bias, n) : 0.f);
+  const ActForm form(args.act);
+  float y = z;
+  if (args.preact && args.grad) {
+    const float at = to_float<OutT>(args.preact, (int64_t)m * args.ld_preact + n);
+    if (args.act == ACT_RELU) y = at > 0.f ? z : 0.f;
+    else if (args.act != ACT_NONE) y = z * form.slope(at);
+  } else {
+    if (args.preact) store_out<OutT>(args.preact, (int64_t)m * args.ld_preact + n, z);
+    if (args.act == ACT_RELU) y = z < 0.f ? 0.f : z;
+    else if (args.act != ACT_NONE) y = form.value(z);
+  }
+  if (args.residual) {
+    const int64_t i = (int64_t)m * args.ld_residual + n;
+    y += args.residual_f32 ? to_float<f32_t>(args.residual, i) : to_float<OutT>(args.residual, i);
+  }
+  store_out<OutT>(args.C, (int64_t)m * args.ldc + n, y);
+}
+
 // A split tile: the sum of its slots, through the same end.  (The slots' order and the reasons for a second launch stand at
 // split_reduce.)
 template <typename T, typename OutT>
@@ -555,29 +625,9 @@ __global__ __launch_bounds__(256) void fused_split_reduce(const FusedArgs args, 
   tile_of(args, args.whole + u, tile_m, tile_n);
   const int m = tile_m * bm + row, n = tile_n * bn + col;
   if (n >= args.store_n) return;
-  const float alpha = args.alpha * (args.scale ? *args.scale : 1.f);
-  const float bias = args.bias ? to_float<T>(args.bias, n) : 0.f;
-  const ActForm form(args.act);
 #pragma unroll
-  for (int x = 0; x < 4; ++x) {
-    if (m + x >= args.store_m) break;
-    const float z = fmaf(alpha, sum[x], bias);
-    float y = z;
-    if (args.preact && args.grad) {
-      const float at = to_float<OutT>(args.preact, (int64_t)(m + x) * args.ld_preact + n);
-      if (args.act == ACT_RELU) y = at > 0.f ? z : 0.f;
-      else if (args.act != ACT_NONE) y = z * form.slope(at);
-    } else {
-      if (args.preact) store_out<OutT>(args.preact, (int64_t)(m + x) * args.ld_preact + n, z);
-      if (args.act == ACT_RELU) y = z < 0.f ? 0.f : z;
-      else if (args.act != ACT_NONE) y = form.value(z);
-    }
-    if (args.residual) {
-      const int64_t i = (int64_t)(m + x) * args.ld_residual + n;
-      y += args.residual_f32 ? to_float<f32_t>(args.residual, i) : to_float<OutT>(args.residual, i);
-    }
-    store_out<OutT>(args.C, (int64_t)(m + x) * args.ldc + n, y);
-  }
+  for (int x = 0; x < 4; ++x)
+    if (m + x < args.store_m) finish_element<T, OutT>(args, m + x, n, sum[x]);
 }
 
 }  // namespace gensor

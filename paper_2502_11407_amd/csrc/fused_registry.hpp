@@ -29,7 +29,9 @@ hipError_t launch_fused(const FusedArgs& a, hipStream_t st) {
   hipError_t e = allow_dynamic_lds(contraction_kernel<C, SPLIT, false, false, F>, C::LDS_BYTES, done);
   if (e != hipSuccess) return e;
   const unsigned tiles = (unsigned)a.tiles_m * (unsigned)a.tiles_n * (unsigned)a.batch;
-  const unsigned grid = SPLIT ? (unsigned)a.whole + (tiles - (unsigned)a.whole) * (unsigned)a.split : tiles;
+  // (workgroups of the alternating tiles stay for further tiles: one to a compute unit)
+  const unsigned most = C::ALTERNATE && MOVE == MOVE_NONE ? 256u : 0xffffffffu;
+  const unsigned grid = SPLIT ? (unsigned)a.whole + (tiles - (unsigned)a.whole) * (unsigned)a.split : tiles < most ? tiles : most;
   hipLaunchKernelGGL((contraction_kernel<C, SPLIT, false, false, F>), dim3(grid), dim3(C::THREADS), C::LDS_BYTES, st, a);
   return hipGetLastError();
 }

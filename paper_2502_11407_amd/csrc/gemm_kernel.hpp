@@ -329,6 +329,7 @@ struct PlainOutput {
   typedef KernelArgs Args;
   typedef const KernelArgs& Local;
   static constexpr bool MOVES = false, OWN_END = false;
+  template <typename C> static constexpr int MIN_STORES = 0;       // of a wave, that `finish` issues at least
 };
 
 // A wave's place in its workgroup's tile, for an epilogue of its own.
@@ -388,8 +389,8 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
     bidx = wg / tiles_per_batch;
     tile_of(args, wg - bidx * tiles_per_batch, tile_m, tile_n);
   }
-  const int m0 = tile_m * BM;
-  const int n0 = tile_n * BN;
+  int m0 = tile_m * BM;
+  int n0 = tile_n * BN;
 
   // k range of this workgroup: the whole of K, or k tiles [kpart * nk / kparts, (kpart + 1) * nk / kparts) of a split
   // tile.  The operand bases move to the first k of the range and Kx is its length, so everything below
@@ -437,8 +438,8 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
   auto clamp_records = [](int64_t bytes) -> uint32_t {
     return bytes <= 0 ? 0u : (bytes > 0x7fffffffll ? 0x7fffffffu : (uint32_t)bytes);
   };
-  const int rows_valid = min(BM, args.M - m0);
-  const int cols_valid = min(BN, args.N - n0);
+  int rows_valid = min(BM, args.M - m0);
+  int cols_valid = min(BN, args.N - n0);
   const char* a_tile = (C::ASRC == A_KC) ? Ab + (int64_t)m0 * args.lda * ES : Ab + (int64_t)m0 * ES;
   const char* b_tile = (C::BSRC == B_KC) ? Bb + (int64_t)n0 * args.ldb * ES : (C::BSRC == B_NCS2 ? Bb : Bb + (int64_t)n0 * ES);
   // Operands without VEC start anywhere: the descriptor begins at the 16-byte granule that holds the tile's first
@@ -1156,11 +1157,42 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
     constexpr std::integral_constant<int, NBR> but_b{};
     constexpr std::integral_constant<int, NA + NBR> but_ab{};
     constexpr std::integral_constant<int, NA + 2 * NBR> but_ab2{};
+    // Products that are consumed in place keep their workgroups: one to a compute unit, each with every gridDim.x'th tile.  The first
+    // requests of the next tile go out before the epilogue of this one, which covers their latency (and a workgroup's start); they have landed
+    // once no more operations are outstanding than the epilogue's stores behind them.  Group 0 begins its epilogue while group 1
+    // multiplies the last k tile: all fragments have been read by then, so the stages are free.
+    constexpr bool STAYS = F::OWN_END && !F::MOVES && !SPLIT;
+    constexpr int BEHIND = F::template MIN_STORES<C> == 0 || F::template MIN_STORES<C> > 63 ? 63 : F::template MIN_STORES<C>;
     int t = 0, t3 = 0;                                         // k tile, and t % 3
-    request_a(0);
-    request_b(0, 0);
+    int turn = blockIdx.x;
+    auto first_requests = [&]() {
+      // (nothing of the addresses is computed once for all tiles: a request that waits for its spilled address waits for those before it)
+      asm volatile("" : "+v"(va[0]), "+v"(va[1]), "+v"(vb[0]), "+v"(vb[1]), "+v"(vb[VB - 1]));
+      request_a(0);
+      request_b(0, 0);
+      if (group == 0) {
+        if (nk > 1) request_b(1, 1);
+      } else if (nk > 1) {
+        request_a(1);
+        request_b(1, 1);
+      }
+      pin();
+    };
+    if constexpr (STAYS) first_requests();
+    bool again = false;
+    do {
+    if constexpr (!STAYS) {
+      request_a(0);
+      request_b(0, 0);
+    } else {
+      t = t3 = 0;
+    }
     if (group == 0) {
-      if (nk > 1) {
+      if constexpr (STAYS) {
+        if (again) landed(std::integral_constant<int, BEHIND>{});
+        else if (nk > 1) landed(but_b);
+        else landed(all);
+      } else if (nk > 1) {
         request_b(1, 1);
         landed(but_b);
       } else {
@@ -1192,9 +1224,13 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
       }
       multiply();
       end_slot();
-      end_slot();
+      if constexpr (!STAYS) end_slot();
     } else {
-      if (nk > 1) {
+      if constexpr (STAYS) {
+        if (again) landed(std::integral_constant<int, BEHIND>{});
+        else if (nk > 1) landed(but_ab);
+        else landed(all);
+      } else if (nk > 1) {
         request_a(1);
         request_b(1, 1);
         landed(but_ab);
@@ -1211,9 +1247,39 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
       for (; t < nk; ++t, t3 = third(t3, 1)) {
         read_slot(t, t3, no, 0, no, 0, 0, all);
         multiply();
-        end_slot();
+        if (!STAYS || t + 1 < nk) end_slot();
       }
     }
+    if constexpr (STAYS) {
+      int own = lane;
+      asm volatile("" : "+v"(own));                            // (what the epilogue derives from it is not computed once for all tiles: no registers)
+      const TilePlace here{m0, n0, wave_m * C::WM, wave_n * C::WN, own};
+      turn += gridDim.x;
+      again = turn < total;
+      if (again) {
+        tile_of(args, xcd_contiguous(turn, total), tile_m, tile_n);
+        m0 = tile_m * BM;
+        n0 = tile_n * BN;
+        rows_valid = min(BM, args.M - m0);
+        cols_valid = min(BN, args.N - n0);
+        a_tile = Ab + (C::ASRC == A_KC ? (int64_t)m0 * args.lda : (int64_t)m0) * ES;
+        b_tile = Bb + (C::BSRC == B_KC ? (int64_t)n0 * args.ldb : (int64_t)n0) * ES;
+        first_requests();
+      }
+      // (a reduction stores next to nothing behind the requests: it waits for them before it stores, and nobody waits for its stores)
+      F::template finish<C>(args, acc, here, [&]() { if (F::template MIN_STORES<C> == 0) landed(all); });
+      pin();
+      if (again) {
+#pragma unroll
+        for (int i = 0; i < C::MBLK; ++i)
+#pragma unroll
+          for (int j = 0; j < C::NBLK; ++j)
+#pragma unroll
+            for (int v = 0; v < MF::NACC; ++v) acc[i][j][v] = 0.f;
+      }
+    }
+    } while (again);
+    if constexpr (STAYS) return;
   } else if constexpr (DEEP) {
     // By the barrier in front of step 2 every wave has read (and received) steps 2 and 3 of this
     // tile, so its stage is free: the loads of tile kt+2 go out right behind the barrier, over
@@ -1485,7 +1551,7 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
   }
 
   if constexpr (F::OWN_END) {
-    F::template finish<C>(args, acc, TilePlace{m0, n0, wave_m * C::WM, wave_n * C::WN, lane});
+    F::template finish<C>(args, acc, TilePlace{m0, n0, wave_m * C::WM, wave_n * C::WN, lane}, []() {});
     return;
   }
 

@@ -46,6 +46,18 @@ std::map<std::array<int64_t, 14>, std::vector<FusedChoice>> g_choices;
 const size_t kChoiceLimit = 4096;
 const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16};
 
+// The cost model's time.  A group's tiles of a product over ragged rows take as long as its rows are many, and groups are rarely even: a launch
+// is no shorter than one group of three times the mean's rows alone.  (8 groups of 2048 rows on average, the largest 5000, 768 x 3072 each:
+// 256x256 tiles 121 us, 256x128 103; 32 groups of 512: 125 and 149.)
+double tile_price(const FusedDesc& f, const GemmView& v, int kind, int split) {
+  const double us = fused_price(f.d, v, split);
+  if (kind != FUSED_DEPTH || us <= 0 || v.batch == 1) return us;
+  GemmView one = v;
+  one.batch = 1;
+  one.K = std::min<int64_t>(3 * v.K, INT32_MAX - 256);
+  return std::max(us, fused_price(f.d, one, 1));
+}
+
 gensor_status choose(const GemmView& v, int kind, bool vec_ok, const LeadingDims& ld, size_t room, FusedChoice* out) {
   const std::array<int64_t, 14> key = {kind, v.in_dtype, v.out_dtype, v.asrc, v.bsrc, vec_ok, v.M, v.N, v.K, v.batch, ld.a, ld.b, ld.c, 0};
   std::lock_guard<std::mutex> lock(g_choice_mutex);
@@ -55,9 +67,10 @@ gensor_status choose(const GemmView& v, int kind, bool vec_ok, const LeadingDims
     for (int i = 0; i < g_num_fused; ++i) {
       const FusedDesc& f = g_fused[i];
       if (!f.launch[kind] || !instance_serves(f.d, v) || (f.d.vec && !vec_ok) || !offsets_fit(f.d, v, ld)) continue;
+      if (f.d.direct && !f.d.any_k() && (kind == FUSED_DEPTH || v.K % f.d.bk != 0)) continue;
       for (int split : kSplits) {
         if (split > 1 && (kind != FUSED_LINEAR || (v.K + f.d.bk - 1) / f.d.bk < split)) break;
-        const double us = fused_price(f.d, v, split);
+        const double us = tile_price(f, v, kind, split);
         if (us <= 0) continue;
         const SplitPlan sp = split_plan(f.d, v, split, 0);
         if (split > 1 && sp.split == 1) continue;
@@ -302,15 +315,15 @@ extern "C" gensor_status gensor_grouped_wgrad(const gensor_problem* p, const int
 
 // ------------------------------------------------------------------------------------ column sums
 // db[g][n] = sum of dY[r][n] over the rows of g, fp32 sums.  Bound by reading dY once.  A workgroup takes 64 vectors' columns and one of `parts`
-// equal shares of a group's rows; its four waves take turns at the rows and add up in LDS.  The shares' sums go to the workspace
-// and a second launch adds them in order, so the result does not depend on when a share finished.
+// equal shares of a group's rows; its eight waves take turns at the rows, eight rows requested together, and add up in LDS.  The shares'
+// sums go to the workspace and a second launch adds them in order, so the result does not depend on when a share finished.
 namespace gensor {
 
 template <typename T, typename OutT, bool VEC>
-__global__ __launch_bounds__(256) void column_sums_kernel(const char* Y, int64_t ld, int rows, int N, const int32_t* offsets, int groups, int parts,
+__global__ __launch_bounds__(512) void column_sums_kernel(const char* Y, int64_t ld, int rows, int N, const int32_t* offsets, int groups, int parts,
                                                           float* partial, void* out) {
-  constexpr int ES = ElemSize<T>::value, EPC = 16 / ES, UNROLL = 4;
-  __shared__ float sums[4][64 * EPC];
+  constexpr int ES = ElemSize<T>::value, EPC = 16 / ES, UNROLL = VEC ? 8 : 4, WAVES = 8;
+  __shared__ float sums[WAVES][64 * EPC];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int g = blockIdx.z, part = blockIdx.y;
   int first = 0, count = rows;
@@ -325,13 +338,13 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const char* Y, int64_t
   for (int e = 0; e < EPC; ++e) acc[e] = 0.f;
   // element e of a lane is column col0 + EPC * lane + e (vectors) or col0 + lane + 64 * e
   const int mine = VEC ? col0 + lane * EPC : col0 + lane;
-  for (int r = r0 + wave; r < r1; r += 4 * UNROLL) {
+  for (int r = r0 + wave; r < r1; r += WAVES * UNROLL) {
     if constexpr (VEC) {
       u32x4 v[UNROLL];
 #pragma unroll
       for (int u = 0; u < UNROLL; ++u) {
         v[u] = u32x4{0u, 0u, 0u, 0u};
-        if (r + 4 * u < r1 && mine < N) v[u] = *(const u32x4*)(Y + ((int64_t)(r + 4 * u) * ld + mine) * ES);
+        if (r + WAVES * u < r1 && mine < N) v[u] = *(const u32x4*)(Y + ((int64_t)(r + WAVES * u) * ld + mine) * ES);
       }
 #pragma unroll
       for (int u = 0; u < UNROLL; ++u)
@@ -345,43 +358,52 @@ __global__ __launch_bounds__(256) void column_sums_kernel(const char* Y, int64_t
       for (int u = 0; u < UNROLL; ++u)
 #pragma unroll
         for (int e = 0; e < EPC; ++e)
-          if (r + 4 * u < r1 && mine + 64 * e < N) acc[e] += to_float<T>(Y, (int64_t)(r + 4 * u) * ld + mine + 64 * e);
+          if (r + WAVES * u < r1 && mine + 64 * e < N) acc[e] += to_float<T>(Y, (int64_t)(r + WAVES * u) * ld + mine + 64 * e);
     }
   }
 #pragma unroll
   for (int e = 0; e < EPC; ++e) sums[wave][VEC ? lane * EPC + e : lane + 64 * e] = acc[e];
   __syncthreads();
-  for (int i = threadIdx.x; i < 64 * EPC; i += 256) {
+  for (int i = threadIdx.x; i < 64 * EPC; i += 512) {
     const int col = col0 + i;
     if (col >= N) continue;
-    const float s = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
+    float s = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) s += sums[w][i];
     if (parts == 1) store_out<OutT>(out, (int64_t)g * N + col, s);
     else partial[((int64_t)g * parts + part) * N + col] = s;
   }
 }
 
 template <typename OutT>
-__global__ __launch_bounds__(256) void column_parts_kernel(const float* partial, int parts, int N, void* out) {
-  const int col = blockIdx.x * 64 + (threadIdx.x & 63), wave = threadIdx.x >> 6;
-  __shared__ float sums[4][64];
+__global__ __launch_bounds__(1024) void column_parts_kernel(const float* partial, int parts, int N, void* out) {
+  constexpr int WAVES = 16, UNROLL = 8;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+  __shared__ float sums[WAVES][64];
   float s = 0.f;
-  if (col < N)
-    for (int p = wave; p < parts; p += 4) s += partial[((int64_t)blockIdx.y * parts + p) * N + col];
-  sums[wave][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (wave == 0 && col < N) {
-    const int i = threadIdx.x;
-    store_out<OutT>(out, (int64_t)blockIdx.y * N + col, (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]));
+  for (int p = wave; p < parts; p += WAVES * UNROLL) {
+    float v[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) v[u] = col < N && p + WAVES * u < parts ? partial[((int64_t)blockIdx.y * parts + p + WAVES * u) * N + col] : 0.f;
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) s += v[u];
   }
+  sums[wave][lane] = s;
+  __syncthreads();
+  if (wave != 0 || col >= N) return;
+  s = 0.f;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) s += sums[w][lane];
+  store_out<OutT>(out, (int64_t)blockIdx.y * N + col, s);
 }
 
 }  // namespace gensor
 
 namespace {
-// Shares of a group's rows: enough that the launch has about four workgroups a compute unit, none of fewer than 32 rows on average.
+// Shares of a group's rows: enough that the launch has about two workgroups a compute unit, none of fewer than 64 rows on average.
 int64_t column_parts(int64_t groups, int64_t rows, int64_t N, int esize) {
   const int64_t blocks = (N + 64 * (16 / esize) - 1) / (64 * (16 / esize)) * groups;
-  const int64_t want = (4 * 256 + blocks - 1) / blocks, most = std::max<int64_t>(1, rows / groups / 32);
+  const int64_t want = (2 * 256 + blocks - 1) / blocks, most = std::max<int64_t>(1, rows / groups / 64);
   return std::min<int64_t>(std::min(want, most), 1024);
 }
 
@@ -391,12 +413,12 @@ gensor_status launch_columns(const void* dY, int64_t ld, int64_t rows, int64_t N
   const int64_t per = 64 * (16 / ElemSize<T>::value);
   const dim3 grid((unsigned)((N + per - 1) / per), (unsigned)parts, (unsigned)groups);
   if (vec)
-    hipLaunchKernelGGL((column_sums_kernel<T, OutT, true>), grid, dim3(256), 0, st, (const char*)dY, ld, (int)rows, (int)N, offsets, (int)groups, (int)parts, partial, out);
+    hipLaunchKernelGGL((column_sums_kernel<T, OutT, true>), grid, dim3(512), 0, st, (const char*)dY, ld, (int)rows, (int)N, offsets, (int)groups, (int)parts, partial, out);
   else
-    hipLaunchKernelGGL((column_sums_kernel<T, OutT, false>), grid, dim3(256), 0, st, (const char*)dY, ld, (int)rows, (int)N, offsets, (int)groups, (int)parts, partial, out);
+    hipLaunchKernelGGL((column_sums_kernel<T, OutT, false>), grid, dim3(512), 0, st, (const char*)dY, ld, (int)rows, (int)N, offsets, (int)groups, (int)parts, partial, out);
   if (hipGetLastError() != hipSuccess) return GENSOR_ERR_DEVICE;
   if (parts == 1) return GENSOR_OK;
-  hipLaunchKernelGGL((column_parts_kernel<OutT>), dim3((unsigned)((N + 63) / 64), (unsigned)groups), dim3(256), 0, st, partial, (int)parts, (int)N, out);
+  hipLaunchKernelGGL((column_parts_kernel<OutT>), dim3((unsigned)((N + 63) / 64), (unsigned)groups), dim3(1024), 0, st, partial, (int)parts, (int)N, out);
   return launched(hipGetLastError());
 }
 }  // namespace
@@ -530,9 +552,57 @@ struct XentPlan {
   size_t pad_bytes, sum_bytes, part_bytes, piece_bytes, total;
 };
 
-// G of a piece stays in the 256 MiB Infinity Cache beside what its products read, so pieces of 128 MiB at most.
-const size_t kPieceBytes = (size_t)128 << 20;
-const size_t kPartBytes = (size_t)32 << 20;
+// A piece's G at most: larger pieces fill the chip in more whole rounds and split dX's sum less often (50257 entries, 4096 tokens, 768 wide, bf16: pieces
+// of 64 MiB 1215 us, 128 1051, 256 956), but the logits of a batch are not to be kept.
+const size_t kPieceBytes = (size_t)256 << 20;
+const size_t kPartBytes = (size_t)64 << 20;
+
+// The cheapest whole or split tile's price, not remembered.
+double best_price(const GemmView& v, int kind, bool vec, size_t room) {
+  const LeadingDims ld = {v.asrc == A_KC ? v.K : v.M, v.bsrc == B_KC ? v.K : v.N, v.N};
+  double best = 1e30;
+  for (int i = 0; i < g_num_fused; ++i) {
+    const FusedDesc& f = g_fused[i];
+    if (!f.launch[kind] || f.d.vec != (vec ? 1 : 0) || !instance_serves(f.d, v) || !offsets_fit(f.d, v, ld)) continue;
+    for (int split : kSplits) {
+      if (split > 1 && (kind != FUSED_LINEAR || (v.K + f.d.bk - 1) / f.d.bk < split)) break;
+      const double us = tile_price(f, v, kind, split);
+      if (us > 0 && us < best && split_plan(f.d, v, split, 0).bytes <= room) best = us;
+    }
+  }
+  return best;
+}
+
+GemmView prob_view(int dtype, int64_t rows, int64_t T, int64_t D) { return product_view(dtype, dtype, rows, T, D, A_KC, B_KC); }
+GemmView dw_view(int dtype, int64_t rows, int64_t pitch, int64_t D) { return product_view(dtype, dtype, rows, D, pitch, A_KC, B_NC); }
+GemmView dx_view(int dtype, int64_t rows, int64_t pitch, int64_t D, bool last) {
+  return product_view(dtype, last ? dtype : (int)GENSOR_F32, pitch, D, rows, A_MC, B_NC);
+}
+
+std::map<std::array<int64_t, 6>, int64_t> g_piece_sizes;         // guarded by g_choice_mutex
+
+// Entries of a piece where V of them do not fit one of `most`: all pieces but the last have as many.  A piece's products each end in a partly
+// filled round of tiles, so the sizes in steps of a tile are priced: 50257 entries for 4096 tokens in pieces of 12800 (four rounds
+// of 256x256 tiles, the last almost empty) 1051 us, of 25344 956.
+int64_t piece_size(int dtype, int64_t T, int64_t V, int64_t D, int64_t pitch, int64_t most) {
+  const bool vec = D % (16 / size_of(dtype)) == 0;
+  auto price = [&](int64_t rows, bool last) {
+    return best_price(prob_view(dtype, rows, T, D), FUSED_PROB, vec, 0) + best_price(dw_view(dtype, rows, pitch, D), FUSED_LINEAR, vec, kPartBytes) +
+           best_price(dx_view(dtype, rows, pitch, D, last), FUSED_LINEAR, vec, kPartBytes);
+  };
+  const int64_t least = (V + most - 1) / most;             // pieces
+  int64_t best = most, step = 256;
+  while (most / step > 64) step *= 2;                      // at most 64 sizes of each count are priced
+  double best_us = 1e30;
+  for (int64_t n = least; n <= least + 1; ++n)
+    for (int64_t size = (V / n + 255) / 256 * 256; size <= most && (n - 1) * size < V; size += step) {
+      const int64_t last = V - (n - 1) * size;
+      if (last > most) continue;
+      const double us = (double)(n - 1) * price(size, false) + price(last, true);
+      if (us < best_us) { best_us = us; best = size; }
+    }
+  return best;
+}
 
 bool plan_xent(int dtype, int64_t T, int64_t V, int64_t D, size_t room, XentPlan* pl) {
   const int es = size_of(dtype), epc = 16 / es;
@@ -540,34 +610,46 @@ bool plan_xent(int dtype, int64_t T, int64_t V, int64_t D, size_t room, XentPlan
   pl->pad = pl->pitch != T;
   pl->pad_bytes = pl->pad ? round_up((size_t)(pl->pitch * D * es), 256) : 0;
   const size_t row = (size_t)(pl->pitch * es);
-  int64_t most = (int64_t)(kPieceBytes / row) / 256 * 256;
-  if (most < 256) most = 256;
-  auto layout = [&](int64_t piece) {
-    if (piece >= V) piece = V;
-    pl->pieces = (V + piece - 1) / piece;
-    pl->piece = pl->pieces == 1 ? V : std::min<int64_t>(V, ((V + pl->pieces - 1) / pl->pieces + 255) / 256 * 256);
+  int64_t most = std::max<int64_t>(256, (int64_t)(kPieceBytes / row) / 256 * 256);
+  auto layout = [&]() {
+    pl->piece = V;
+    if (V > most) {
+      const std::array<int64_t, 6> key = {dtype, T, V, D, pl->pitch, most};
+      std::lock_guard<std::mutex> lock(g_choice_mutex);
+      auto it = g_piece_sizes.find(key);
+      if (it == g_piece_sizes.end()) {
+        if (g_piece_sizes.size() >= kChoiceLimit) g_piece_sizes.clear();
+        it = g_piece_sizes.emplace(key, piece_size(dtype, T, V, D, pl->pitch, most)).first;
+      }
+      pl->piece = it->second;
+    }
     pl->pieces = (V + pl->piece - 1) / pl->piece;
+    // (a last piece that is larger than the others: what it has more would be a small piece of its own)
+    while (pl->pieces > 1 && V - (pl->pieces - 2) * pl->piece <= most) --pl->pieces;
+    const int64_t largest = std::max(pl->piece, V - (pl->pieces - 1) * pl->piece);
     pl->sum_bytes = pl->pieces > 1 && dtype != GENSOR_F32 ? round_up((size_t)(T * D * 4), 256) : 0;
-    pl->piece_bytes = round_up((size_t)pl->piece * row, 256);
+    pl->piece_bytes = round_up((size_t)largest * row, 256);
     // the room the products' partial tiles would like, within a limit
     size_t parts = 0;
-    const GemmView dw = product_view(dtype, dtype, pl->piece, D, pl->pitch, A_KC, B_NC), dx = product_view(dtype, dtype == GENSOR_F32 || pl->pieces == 1 ? dtype : (int)GENSOR_F32, pl->pitch, D, pl->piece, A_MC, B_NC);
-    for (const GemmView* v : {&dw, &dx})
-      for (int vec = 0; vec < 2; ++vec) {
-        FusedChoice c;
-        const LeadingDims ld = {pl->pitch, D, D};
-        if (choose(*v, FUSED_LINEAR, vec != 0, ld, kPartBytes, &c) == GENSOR_OK) parts = std::max(parts, c.bytes);
-      }
+    for (int64_t rows : {pl->piece, V - (pl->pieces - 1) * pl->piece}) {
+      const bool last = rows != pl->piece || pl->pieces == 1;
+      const GemmView dw = dw_view(dtype, rows, pl->pitch, D), dx = dx_view(dtype, rows, pl->pitch, D, last);
+      for (const GemmView* v : {&dw, &dx})
+        for (int vec = 0; vec < 2; ++vec) {
+          FusedChoice c;
+          const LeadingDims ld = {pl->pitch, D, D};
+          if (choose(*v, FUSED_LINEAR, vec != 0, ld, kPartBytes, &c) == GENSOR_OK) parts = std::max(parts, c.bytes);
+        }
+    }
     pl->part_bytes = round_up(parts, 256);
     pl->total = 256 + pl->pad_bytes + pl->sum_bytes + pl->part_bytes + pl->piece_bytes;
   };
-  layout(most);
-  // less room: smaller pieces
-  while (pl->total > room && most > 256) {
+  layout();
+  while (pl->total > room && most > 256) {                 // less room: smaller pieces
     most = std::max<int64_t>(256, most / 2 / 256 * 256);
-    layout(most);
+    layout();
   }
-  if (pl->total > room) {                    // and no partial tiles
+  if (pl->total > room) {                                  // and no partial tiles
     pl->total -= pl->part_bytes;
     pl->part_bytes = 0;
   }
@@ -576,7 +658,7 @@ bool plan_xent(int dtype, int64_t T, int64_t V, int64_t D, size_t room, XentPlan
 
 gensor_status choose_logits(int dtype, int kind, int64_t rows, int64_t T, int64_t D, const void* W, int64_t ldw, const void* X, int64_t ldx, int64_t ldc,
                             GemmView* v, FusedChoice* c) {
-  *v = product_view(dtype, dtype, rows, T, D, A_KC, B_KC);
+  *v = prob_view(dtype, rows, T, D);
   const LeadingDims ld = {ldw, ldx, ldc};
   return choose(*v, kind, vector_ok(*v, W, ldw, 0, X, ldx, 0), ld, 0, c);
 }
@@ -630,9 +712,9 @@ extern "C" gensor_status gensor_xent_forward(gensor_dtype dtype, int64_t T, int6
   a.at_target = (float*)workspace;
   a.part_max = (float*)((char*)workspace + head);
   a.part_sum = (float*)((char*)workspace + head + each);
+  hipStream_t s = (hipStream_t)hip_stream;
   tiles_of(&a, v, c, V, T);
   if ((int64_t)a.tiles_m * a.tiles_n > INT32_MAX) return GENSOR_ERR_UNSUPPORTED;
-  hipStream_t s = (hipStream_t)hip_stream;
   hipError_t e = c.f->launch[FUSED_LSE](a, s);
   if (e != hipSuccess) return GENSOR_ERR_DEVICE;
   int per = 1;
@@ -671,19 +753,19 @@ extern "C" gensor_status gensor_xent_backward(gensor_dtype dtype, int64_t T, int
   for (int64_t i = 0; i < pl.pieces; ++i) {
     Piece& q = pieces[(size_t)i];
     q.first = i * pl.piece;
-    q.rows = std::min(pl.piece, V - q.first);
+    q.rows = i + 1 == pl.pieces ? V - q.first : pl.piece;
     const char* Wp = (const char*)W + q.first * ldw * es;
     st = choose_logits(dtype, FUSED_PROB, q.rows, T, D, Wp, ldw, X, ldx, pl.pitch, &q.vp, &q.cp);
     if (st != GENSOR_OK) return st;
     if (dW) {
-      q.vw = product_view(dtype, dtype, q.rows, D, pl.pitch, A_KC, B_NC);
+      q.vw = dw_view(dtype, q.rows, pl.pitch, D);
       const LeadingDims ld = {pl.pitch, ldxs, lddw};
       st = choose(q.vw, FUSED_LINEAR, vector_ok(q.vw, G, pl.pitch, 0, Xs, ldxs, 0), ld, pl.part_bytes, &q.cw);
       if (st != GENSOR_OK) return st;
     }
     if (dX) {
       const bool last = i + 1 == pl.pieces;
-      q.vx = product_view(dtype, last ? dtype : (int)GENSOR_F32, pl.pitch, D, q.rows, A_MC, B_NC);
+      q.vx = dx_view(dtype, q.rows, pl.pitch, D, last);
       const LeadingDims ld = {pl.pitch, ldw, std::max(lddx, D) * (last && dtype != GENSOR_F32 ? 2 : 1)};
       st = choose(q.vx, FUSED_LINEAR, vector_ok(q.vx, G, pl.pitch, 0, Wp, ldw, 0), ld, pl.part_bytes, &q.cx);
       if (st != GENSOR_OK) return st;

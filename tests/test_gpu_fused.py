@@ -4,6 +4,7 @@ definitions in 64 bits.
 Tolerances.  u = 2^-24 is the unit roundoff of fp32.  A product's sum of K terms in any order is off by at most (K + 1) u sum|a||b| (first
 order); the activations have slopes of at most 1.13 and are evaluated to within 16 u |z| (gelu and silu: an exponential whose argument is
 off by 4 u |argument|, the sigmoid's derivative times its argument stays below 0.3); a result is rounded once to its type."""
+import gc
 import math
 
 import numpy as np
@@ -21,7 +22,8 @@ TINY = {"f32": 1e-37, "f16": 2.0 ** -25, "bf16": 1e-37}      # half a subnormal 
 @pytest.fixture(scope="module")
 def gs():
     from paper_2502_11407_amd import binding
-    return binding
+    yield binding
+    gc.collect()                                 # (other modules count the device memory that is in use)
 
 
 def draw(shape, dtype, seed, sigma=1.0, pad=0):

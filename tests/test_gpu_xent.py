@@ -4,6 +4,7 @@ Tolerances.  u = 2^-24.  A logit is off by at most e_z = (D + 1) u sum|x||w|; ls
 rounding of the exponentials' arguments and sums, at most 2e-6 + u |lse| here (exponents below 30, slabs and joins of a few thousand terms);
 loss by both.  A probability is then off by a factor 1 + 2 e_z + 4e-6 + u |lse|; G is rounded to the type (f16: after scaling, whose
 subnormal step is 2^-39 of the largest |dloss|); a product's sums of n terms are off by (n + 1) u sum|G||w|; results are rounded once."""
+import gc
 import math
 
 import pytest
@@ -21,7 +22,8 @@ IGNORE = -100
 @pytest.fixture(scope="module")
 def gs():
     from paper_2502_11407_amd import binding
-    return binding
+    yield binding
+    gc.collect()                                 # (other modules count the device memory that is in use)
 
 
 def draw(shape, dtype, seed, sigma=1.0, pad=0):
@@ -116,12 +118,10 @@ def test_pieces(gs, dtype, T):
         dX, dW = torch.empty((T, D), dtype=TORCH[dtype], device="cuda"), torch.empty((V, D), dtype=TORCH[dtype], device="cuda")
         gs.xent_backward(X, W, t, lse, dloss, dX, dW, workspace=workspace(room))
         check_gradient(dtype, X, W, t, lse, dloss, dX, dW)
-    with pytest.raises(gs.GensorError) as e:
+    with pytest.raises(gs.GensorError, match="WORKSPACE"):
         gs.xent_backward(X, W, t, lse, dloss, dX, dW, workspace=workspace(256 * pitch * es))
-    assert e.value.status == 4
-    with pytest.raises(gs.GensorError) as e:
+    with pytest.raises(gs.GensorError, match="WORKSPACE"):
         gs.xent_forward(X, W, t, None, lse, workspace=workspace(256))
-    assert e.value.status == 4
 
 
 def test_one_gradient_of_the_two(gs):
