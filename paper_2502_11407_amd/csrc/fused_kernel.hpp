@@ -19,7 +19,7 @@
 namespace gensor {
 
 enum { END_LINEAR = 0, END_LSE = 1, END_PROB = 2 };
-enum { MOVE_NONE = 0, MOVE_ROWS = 1, MOVE_DEPTH = 2 };
+enum { MOVE_NONE = PLACE_ALL, MOVE_ROWS = PLACE_ROWS, MOVE_DEPTH = PLACE_DEPTH };
 enum { ACT_NONE = 0, ACT_RELU = 1, ACT_GELU = 2, ACT_SILU = 3 };       // gensor_act
 
 struct FusedArgs : KernelArgs {
@@ -104,54 +104,64 @@ __device__ inline void group_rows(const FusedArgs& a, int g, int& first, int& co
 template <int END, int MOVE>
 struct Fused {
   typedef FusedArgs Args;
-  typedef std::conditional_t<MOVE != MOVE_NONE, FusedArgs, const FusedArgs&> Local;
-  static constexpr bool MOVES = MOVE != MOVE_NONE, OWN_END = true;
-  // Stores of a wave that `finish` issues at least (a pair of 16-bit values is one); the logits' reduction stores next to nothing
-  template <typename C> static constexpr int MIN_STORES = END == END_LSE ? 0 : C::WM * C::WN / 64 / (ElemSize<typename C::OutT>::value == 2 ? 2 : 1);
+  static constexpr int MOVES = MOVE;
+  static constexpr bool OWN_END = true;
+  static constexpr bool STAYS = END == END_LSE;
+  // The rows of the first 64 groups, one a lane.
+  static __device__ __attribute__((always_inline)) GroupRows own_group(const FusedArgs& a) {
+    GroupRows r{0, -1};
+    const int lane = threadIdx.x & 63;
+    if (lane < a.groups) group_rows(a, lane, r.first, r.count);
+    return r;
+  }
 
-  // The workgroup's tile; false: there is none for it.  The launch has as many workgroups as the row counts could
-  // need, ceil(rows / BM) of each group at worst; every wave counts the tiles there are by itself (64 groups at a time, one
-  // a lane), so nothing has to run before this launch and the host never waits for the counts.
+  // Tile `id` of a launch; false: there is none.  The launch numbers as many as the row counts could need, ceil(rows / BM) of each group at
+  // worst; every wave counts the tiles there are by itself (64 groups at a time, one a lane), so nothing has to run before this
+  // launch and the host never waits for the counts.
   template <typename C>
-  static __device__ __attribute__((always_inline)) bool place(FusedArgs& a, int& bidx, int& tile_m, int& tile_n) {
-    constexpr int ES = C::ES, OS = ElemSize<typename C::OutT>::value;
+  static __device__ __attribute__((always_inline)) bool place(const FusedArgs& a, int id, const GroupRows& own, GroupPlace& w) {
+    const int lane = threadIdx.x & 63;
     if constexpr (MOVE == MOVE_DEPTH) {
       // The tiles of the group with the most rows start first, then the next one's: a tile's time is its group's rows, and a long
       // one started last would run alone.  Each group's tiles are dealt over all XCDs in contiguous ranges.  (Of more than 64
       // groups the order is kept among 64 at a time.)
       const int per = a.tiles_m * a.tiles_n;
-      const int turn = blockIdx.x / per, g0 = turn & ~63, lane = threadIdx.x & 63;
-      int first, count = -1;
-      if (g0 + lane < a.groups) group_rows(a, g0 + lane, first, count);
+      const int turn = id / per, g0 = turn & ~63;
+      int first, count = own.count;
+      if (g0 > 0) {
+        count = -1;
+        if (g0 + lane < a.groups) group_rows(a, g0 + lane, first, count);
+      }
       int before = 0;
 #pragma unroll 8
       for (int i = 0; i < 64; ++i) {
         const int other = __builtin_amdgcn_readlane(count, i);
         before += other > count || (other == count && i < lane);
       }
-      bidx = g0 + __builtin_ctzll(__ballot(before == (turn & 63)));
-      tile_of(a, xcd_contiguous(blockIdx.x - turn * per, per), tile_m, tile_n);
-      group_rows(a, bidx, first, count);
-      a.A = (const char*)a.A + (int64_t)first * a.lda * ES;
-      a.B = (const char*)a.B + (int64_t)first * a.ldb * ES;
-      a.C = (char*)a.C + (int64_t)bidx * a.strideC * OS;
-      a.K = count;
-      if (count > 0) return true;
+      w.group = g0 + __builtin_ctzll(__ballot(before == (turn & 63)));
+      tile_of(a, xcd_contiguous(id - turn * per, per), w.tile_m, w.tile_n);
+      group_rows(a, w.group, w.first, w.count);
+      if (w.count > 0) return true;
       // nothing to add up: zeros
-      const int m0 = tile_m * C::BM, n0 = tile_n * C::BN;
+      typedef typename C::OutT OutT;
+      char* c = (char*)a.C + (int64_t)w.group * a.strideC * ElemSize<OutT>::value;
+      const int m0 = w.tile_m * C::BM, n0 = w.tile_n * C::BN;
       const int rows = min(C::BM, a.store_m - m0), cols = min(C::BN, a.store_n - n0);
       for (int i = threadIdx.x; i < rows * C::BN; i += C::THREADS) {
         const int r = i / C::BN, k = i % C::BN;
-        if (k < cols) store_out<typename C::OutT>(a.C, (int64_t)(m0 + r) * a.ldc + n0 + k, 0.f);
+        if (k < cols) store_out<OutT>(c, (int64_t)(m0 + r) * a.ldc + n0 + k, 0.f);
       }
       return false;
     } else {
-      const int lane = threadIdx.x & 63;
-      auto tiles_at = [&](int g) {
-        int first, count = 0;
-        if (g < a.groups) group_rows(a, g, first, count);
-        return (count + C::BM - 1) / C::BM;
+      auto rows_at = [&](int g0) {
+        GroupRows r = own;
+        if (g0 > 0) {
+          r.count = 0;
+          if (g0 + lane < a.groups) group_rows(a, g0 + lane, r.first, r.count);
+        }
+        return r;
       };
+      auto tiles_at = [&](int g0) { return (max(rows_at(g0).count, 0) + C::BM - 1) / C::BM; };
       auto running = [&](int x) {                    // inclusive sum over the lanes
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -162,41 +172,69 @@ struct Fused {
       };
       int total = 0, mine = 0;
       for (int g0 = 0; g0 < a.groups; g0 += 64) {
-        mine = running(tiles_at(g0 + lane));
+        mine = running(tiles_at(g0));
         total += __builtin_amdgcn_readlane(mine, 63);
       }
       total *= a.tiles_n;
-      if ((int)blockIdx.x >= total) return false;
-      const int t = xcd_contiguous(blockIdx.x, total);
+      if (id >= total) return false;
+      const int t = xcd_contiguous(id, total);
       int before = 0;                                // tile rows of the groups before this chunk of them
       for (int g0 = 0; g0 < a.groups; g0 += 64) {
-        if (a.groups > 64) mine = running(tiles_at(g0 + lane));
+        if (a.groups > 64) mine = running(tiles_at(g0));
         const uint64_t beyond = __ballot((before + mine) * a.tiles_n > t);
         if (beyond != 0) {
           const int at = __builtin_ctzll(beyond);
           const int end = __builtin_amdgcn_readlane(mine, at);
           const int start = at > 0 ? __builtin_amdgcn_readlane(mine, at - 1) : 0;
-          const int g = g0 + at;
-          int first, count;
-          group_rows(a, g, first, count);
-          first = __builtin_amdgcn_readfirstlane(first);
-          count = __builtin_amdgcn_readfirstlane(count);
-          bidx = g;
-          a.M = a.store_m = count;
-          a.tiles_m = end - start;
-          a.panel = min(a.panel, a.tiles_m);
-          tile_of(a, t - (before + start) * a.tiles_n, tile_m, tile_n);
-          a.A = (const char*)a.A + (int64_t)first * a.lda * ES;
-          a.C = (char*)a.C + (int64_t)first * a.ldc * OS;
-          if (a.preact) a.preact = (char*)a.preact + (int64_t)first * a.ld_preact * OS;
-          if (a.residual) a.residual = (const char*)a.residual + (int64_t)first * a.ld_residual * OS;
-          if (a.bias) a.bias = (const char*)a.bias + (int64_t)g * a.N * ES;
+          w.group = g0 + at;
+          const GroupRows r = rows_at(g0);
+          w.first = __builtin_amdgcn_readlane(r.first, at);
+          w.count = __builtin_amdgcn_readlane(r.count, at);
+          // the tiles of a group: panels of tile rows, walked column by column
+          const int tile_rows = end - start, panel = min(a.panel, tile_rows), inside = t - (before + start) * a.tiles_n;
+          const int pi = inside / (panel * a.tiles_n), rows_here = min(panel, tile_rows - pi * panel), q = inside - pi * panel * a.tiles_n;
+          w.tile_m = pi * panel + q % rows_here;
+          w.tile_n = q / rows_here;
           return true;
         }
         before += __builtin_amdgcn_readlane(mine, 63);
       }
       return false;
     }
+  }
+
+  // Reads two of the lines that the tile's epilogue will read, so that they lie in the L2 by then (8192 x 768 x 3072 with a residual of 50
+  // MB: the product alone 41 us, with a residual that was first asked for in the epilogue 63).  p.lane: the thread.
+  template <typename C>
+  static __device__ __attribute__((always_inline)) void touch(const FusedArgs& a, const TilePlace& p, uint32_t (&value)[2]) {
+    if constexpr (END == END_LINEAR) {
+      if (!a.residual && !a.grad) return;
+      const EndPlace e = end_place<C>(a, p);
+      const int size = a.residual && a.residual_f32 ? 4 : ElemSize<typename C::OutT>::value;
+      const int64_t ld = a.residual ? a.ld_residual : a.ld_preact;
+      const char* base = (const char*)(a.residual ? a.residual : a.preact) + (e.row0 * ld + p.n0) * size;
+      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, e.records(ld, size), 0x00020000u);
+      const int per_row = (C::BN * size + 255) / 256;                  // threads a row; two lines each
+      for (int at = p.lane; at < C::BM * per_row; at += C::THREADS) {
+        const uint32_t off = (uint32_t)(at / per_row) * (uint32_t)(ld * size) + (uint32_t)(at % per_row) * 256u;
+        value[0] = __builtin_amdgcn_raw_buffer_load_b32(r, off & ~3u, 0, 0);
+        value[1] = __builtin_amdgcn_raw_buffer_load_b32(r, (off + 128u) & ~3u, 0, 0);
+      }
+    }
+  }
+
+  // Where the tile lies in C (and in what is read and kept beside it): its first row, and its rows and columns that exist.
+  struct EndPlace {
+    int64_t row0;
+    int rows, cols, group;
+    __device__ uint32_t records(int64_t ld, int size) const {
+      const int64_t bytes = ((int64_t)(rows - 1) * ld + cols) * size;
+      return bytes <= 0 ? 0u : bytes > 0x7fffffffll ? 0x7fffffffu : (uint32_t)bytes;
+    }
+  };
+  template <typename C>
+  static __device__ __attribute__((always_inline)) EndPlace end_place(const FusedArgs& a, const TilePlace& p) {
+    return {(MOVE == MOVE_ROWS ? p.first : 0) + (int64_t)p.m0, min(C::BM, (MOVE == MOVE_ROWS ? p.count : a.store_m) - p.m0), min(C::BN, a.store_n - p.n0), p.group};
   }
 
   // before_stores: called where everything is computed and only stores follow (END_LSE)
@@ -214,31 +252,30 @@ struct Fused {
   // Bound by what it moves beside C: the values kept or read again, and the residual.  An element access moves two bytes a
   // lane of 16-bit types, so where rows allow it (`paired`) pairs of rows of a column are traded with the neighbour lane for
   // pairs of columns of a row, as the plain epilogue does: the exchange is its own inverse, so what is read goes the
-  // same way backwards.  What a block reads is requested while the block before it is computed.
+  // same way backwards.  (Four columns a lane, in half as many stores, were 3 us slower on 8192 x 3072 x 768: 41.3 -> 44.4.)
+  // What is read is requested as far ahead as 32 registers hold: a load's wait counts the stores before it, too.
   template <typename C, bool FULL, typename Acc>
   static __device__ __attribute__((always_inline)) void finish_linear(const FusedArgs& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p) {
     typedef typename C::OutT OutT;
     constexpr int OS = ElemSize<OutT>::value, ES = C::ES, MB = C::MB, NACC = MB * MB / 64;
     constexpr uint32_t FLAGS = 0x00020000u, OOB = 0x80000000u;
     const int lane = p.lane, frow = lane % MB, fgrp = lane / MB;
-    const int rows_valid = min(C::BM, a.store_m - p.m0), cols_valid = min(C::BN, a.store_n - p.n0);
-    auto records = [&](int64_t ld, int size) -> uint32_t {
-      const int64_t bytes = ((int64_t)(rows_valid - 1) * ld + cols_valid) * size;
-      return bytes <= 0 ? 0u : bytes > 0x7fffffffll ? 0x7fffffffu : (uint32_t)bytes;
-    };
-    const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void*)((char*)a.C + ((int64_t)p.m0 * a.ldc + p.n0) * OS), 0, records(a.ldc, OS), FLAGS);
+    const EndPlace e = end_place<C>(a, p);
+    const int cols_valid = e.cols;
+    char* c_base = (char*)a.C + ((MOVE == MOVE_DEPTH ? (int64_t)e.group * a.strideC : 0) + e.row0 * a.ldc + p.n0) * OS;
+    const __amdgpu_buffer_rsrc_t rc = __builtin_amdgcn_make_buffer_rsrc((void*)c_base, 0, e.records(a.ldc, OS), FLAGS);
     const uint32_t pitch = (uint32_t)a.ldc * OS;
     const bool has_z = FULL && a.preact != nullptr, has_r = FULL && a.residual != nullptr;
     const int xs = has_r && a.residual_f32 ? 4 : OS;                   // size of what is read
     const bool reads = has_r || (has_z && a.grad);
     const char* x_base = has_r ? (const char*)a.residual : (const char*)a.preact;
     const int64_t x_ld = has_r ? a.ld_residual : a.ld_preact;
-    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)(reads ? x_base + ((int64_t)p.m0 * x_ld + p.n0) * xs : (const char*)a.C), 0,
-                                                                        reads ? records(x_ld, xs) : 0u, FLAGS);
+    const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)(reads ? x_base + (e.row0 * x_ld + p.n0) * xs : c_base), 0,
+                                                                        reads ? e.records(x_ld, xs) : 0u, FLAGS);
     const uint32_t x_pitch = (uint32_t)x_ld * xs;
     const bool keeps = has_z && !a.grad;
-    const __amdgpu_buffer_rsrc_t rz = __builtin_amdgcn_make_buffer_rsrc((void*)(keeps ? (char*)a.preact + ((int64_t)p.m0 * a.ld_preact + p.n0) * OS : (char*)a.C), 0,
-                                                                        keeps ? records(a.ld_preact, OS) : 0u, FLAGS);
+    const __amdgpu_buffer_rsrc_t rz = __builtin_amdgcn_make_buffer_rsrc((void*)(keeps ? (char*)a.preact + (e.row0 * a.ld_preact + p.n0) * OS : c_base), 0,
+                                                                        keeps ? e.records(a.ld_preact, OS) : 0u, FLAGS);
     const uint32_t z_pitch = (uint32_t)a.ld_preact * OS;
     const float alpha = FULL ? a.alpha * (a.scale ? *a.scale : 1.f) : 1.f;
     const int act = FULL ? a.act : ACT_NONE;
@@ -250,7 +287,7 @@ struct Fused {
 #pragma unroll
     for (int bj = 0; bj < C::NBLK; ++bj) {
       const int col = p.n0 + p.col + bj * MB + frow;
-      bias[bj] = FULL && a.bias && col < a.store_n ? to_float<typename C::T>(a.bias, col) : 0.f;
+      bias[bj] = FULL && a.bias && col < a.store_n ? to_float<typename C::T>(a.bias, (MOVE == MOVE_ROWS ? (int64_t)e.group * a.N : 0) + col) : 0.f;
     }
     // the values of a block, x what was read for it; z: the values before the activation
     auto compute = [&](int bi, int bj, const float* x, float* z, float* y) {
@@ -525,12 +562,12 @@ struct Fused {
     }
   }
 
-  // exp(d).  In fp32 the exponent's rounding (2^-24 of up to a hundred) is carried as a factor; 16-bit results round a thousand times
-  // coarser than it.
-  template <typename C> static __device__ float exponential(float d) {
+  // exp(z - lse), base = -log2(e) lse.  For 16-bit results, which round a thousand times coarser than the product and the exponent are rounded, in two
+  // operations; in fp32 the exponent's rounding (2^-24 of up to a hundred) is carried as a factor.
+  template <typename C> static __device__ float probability(float z, float lse, float base) {
     constexpr float log2e = 1.44269504088896340736f;
-    const float t = log2e * d;
-    if constexpr (C::ES == 2) return __builtin_amdgcn_exp2f(t);
+    if constexpr (C::ES == 2) return __builtin_amdgcn_exp2f(fmaf(log2e, z, base));
+    const float d = z - lse, t = log2e * d;
     const float r = fmaf(log2e, d, -t) + 1.92596299e-8f * d;           // (log2(e) - log2e)
     const float e = __builtin_amdgcn_exp2f(t);
     return d > -100.f ? fmaf(e, 0.69314718f * r, e) : e;                // (-inf: inf - inf)
@@ -550,11 +587,11 @@ struct Fused {
       const bool there = token < a.tokens;
       const int64_t target = there ? a.targets[token] : -1;
       const bool counts = there && target != a.ignore && target >= 0 && target < a.vocab;
-      const float lse = counts ? a.lse[token] : INFINITY, g = counts ? a.dloss[token] * scale : 0.f;
+      const float lse = counts ? a.lse[token] : INFINITY, base = -1.44269504088896340736f * lse, g = counts ? a.dloss[token] * scale : 0.f;
 #pragma unroll
       for (int bi = 0; bi < C::MBLK; ++bi)
 #pragma unroll
-        for (int v = 0; v < NACC; ++v) acc[bi][bj][v] = g * exponential<C>(acc[bi][bj][v] - lse);
+        for (int v = 0; v < NACC; ++v) acc[bi][bj][v] = g * probability<C>(acc[bi][bj][v], lse, base);
       const int at = counts && target >= first && target < (int64_t)first + C::WM ? (int)(target - first) - 4 * fgrp : -1;
       if (__any(at >= 0)) {
 #pragma unroll

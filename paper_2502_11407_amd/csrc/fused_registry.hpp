@@ -30,7 +30,7 @@ hipError_t launch_fused(const FusedArgs& a, hipStream_t st) {
   if (e != hipSuccess) return e;
   const unsigned tiles = (unsigned)a.tiles_m * (unsigned)a.tiles_n * (unsigned)a.batch;
   // (workgroups of the alternating tiles stay for further tiles: one to a compute unit)
-  const unsigned most = C::ALTERNATE && MOVE == MOVE_NONE ? 256u : 0xffffffffu;
+  const unsigned most = C::ALTERNATE && F::STAYS ? 256u : 0xffffffffu;
   const unsigned grid = SPLIT ? (unsigned)a.whole + (tiles - (unsigned)a.whole) * (unsigned)a.split : tiles < most ? tiles : most;
   hipLaunchKernelGGL((contraction_kernel<C, SPLIT, false, false, F>), dim3(grid), dim3(C::THREADS), C::LDS_BYTES, st, a);
   return hipGetLastError();

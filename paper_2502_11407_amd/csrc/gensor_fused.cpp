@@ -44,7 +44,8 @@ struct FusedChoice {
 std::mutex g_choice_mutex;
 std::map<std::array<int64_t, 14>, std::vector<FusedChoice>> g_choices;
 const size_t kChoiceLimit = 4096;
-const int kSplits[] = {1, 2, 3, 4, 6, 8, 12, 16};
+// (five parts: 48 tiles of 256x256, a gradient of 4096 x 768 over a piece of the vocabulary, fill 240 of 256 units)
+const int kSplits[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16};
 
 // The cost model's time.  A group's tiles of a product over ragged rows take as long as its rows are many, and groups are rarely even: a launch
 // is no shorter than one group of three times the mean's rows alone.  (8 groups of 2048 rows on average, the largest 5000, 768 x 3072 each:

@@ -273,7 +273,7 @@ def test_grouped_activation_gradient_and_residual(gs):
 def test_grouped_large_tiles(gs):
     """Groups of many tiles, whose large tiles are taken, and one that ends inside a tile."""
     for dtype in ("f16", "bf16"):
-        sizes, N, K = [2048, 1000, 0, 3100], 1536, 768
+        sizes, N, K = [2048, 1000, 0, 7100], 1536, 768
         G, rows = len(sizes), sum(sizes)
         off = offsets_of(sizes)
         A, W, dY = draw((rows, K), dtype, 1), draw((G, K, N), dtype, 2, 1 / math.sqrt(K)), draw((rows, N), dtype, 3)
@@ -288,6 +288,27 @@ def test_grouped_large_tiles(gs):
             close(C[at:at + n], act64(z, "silu"), 1.13 * (K + 4) * U * (a.abs() @ w.abs()) + 16 * U * z.abs(), dtype, g)
             close(dW[g], a.t() @ d, (n + 4) * U * (a.abs().t() @ d.abs()), dtype, g)
             at += n
+
+
+@pytest.mark.parametrize("dtype,out", [("f16", "f16"), ("bf16", "bf16"), ("f16", "f32")])
+@pytest.mark.parametrize("M,N,K", [(8192, 3072, 768), (8001, 4096, 520), (4100, 5124, 328), (8192, 768, 3072)])
+def test_large_tiles(gs, dtype, out, M, N, K):
+    """The tiles of large products (256 and 192 columns, whole and split), whose epilogues store in whole lines, with everything read and kept."""
+    for tb in (0, 1):
+        A, B, a, b = problem_operands(dtype, M, N, K, 0, tb, 0, M + tb)
+        p = gs.gemm_problem(dtype, M, N, K, 0, tb, out_dtype=out)
+        ws = workspace(gs.gemm_fused_workspace_bytes(p))
+        d, e = a @ b, (K + 4) * U * (a.abs() @ b.abs())
+        bias, R, Z = draw((N,), dtype, 5, 0.5), draw((M, N), out, 6), draw((M, N), out, 7)
+        C, fine = guarded((M, N), out)
+        kept, kept_fine = guarded((M, N), out)
+        gs.gemm_fused(p, A, B, C, bias=bias, act="gelu", preact=kept, residual=R, workspace=ws)
+        z, ez = d + bias.double(), e + (K + 4) * U * bias.double().abs()
+        close(kept, z, ez, out, "kept")
+        close(C, act64(z, "gelu") + R.double(), 1.13 * ez + 16 * U * z.abs() + U * R.double().abs(), out, "forward")
+        gs.gemm_act_grad(p, A, B, Z, C, "silu", workspace=ws)
+        close(C, d * slope64(Z.double(), "silu"), 1.13 * e + 64 * U * d.abs(), out, "gradient")
+        fine(), kept_fine()
 
 
 def test_offsets_outside_the_rows_are_cut(gs):

@@ -124,6 +124,20 @@ def test_pieces(gs, dtype, T):
         gs.xent_forward(X, W, t, None, lse, workspace=workspace(256))
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("D", [64, 128, 192, 256, 328, 768])
+def test_more_tiles_than_compute_units(gs, dtype, D):
+    """Workgroups that take several tiles of the logits: one to many k tiles, the last tiles ragged in both directions."""
+    T, V = 2310, 9000
+    X, W, t = inputs(dtype, T, V, D, 0, D)
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    gs.xent_forward(X, W, t, loss, lse, workspace=workspace(gs.xent_workspace_bytes(dtype, T, V, D)))
+    _, lse64, loss64, _, _, e_z = reference(X, W, t)
+    limit = e_z + 2e-6 + 2 * U * lse64.abs()
+    assert bool(((lse.double() - lse64).abs() <= limit).all()), float(((lse.double() - lse64).abs() / limit).max())
+    assert bool(((loss.double() - loss64).abs() <= 2 * limit).all())
+
+
 def test_one_gradient_of_the_two(gs):
     T, V, D = 100, 1500, 128
     X, W, t = inputs("bf16", T, V, D, 0, 5)
