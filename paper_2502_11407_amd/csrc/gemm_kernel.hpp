@@ -1178,11 +1178,11 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
     constexpr std::integral_constant<int, NA + NBR> but_ab{};
     constexpr std::integral_constant<int, NA + 2 * NBR> but_ab2{};
     // STAYS: a workgroup to a compute unit, each with every gridDim.x'th tile.  The first requests of the next tile go out before the
-    // epilogue of this one, which covers their latency (and a workgroup's start) and waits for them before it stores.  Group 0
-    // begins its epilogue while group 1 multiplies the last k tile: all fragments have been read by then, so the stages
-    // are free.  For epilogues that store next to nothing only: where the requests of the second k tile wait, in order, for the stores in
+    // epilogue of this one, which covers their latency (and a workgroup's start) and waits for them before it stores.  For epilogues that store next to nothing only: where the requests of the second k tile wait, in order, for the stores in
     // front of them, a new workgroup, whose counters are its own, is faster (16384 x 3072 x 768 85 against 79 us).
     constexpr bool STAYS = F::STAYS && !SPLIT;
+    // OWN_END: group 0 begins its epilogue while group 1 multiplies the last k tile: all fragments have been read by then, so the stages
+    // are free, and no barrier follows.
     int t = 0, t3 = 0;                                         // k tile, and t % 3
     int turn = blockIdx.x;
     auto first_requests = [&]() {
@@ -1247,7 +1247,7 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
       }
       multiply();
       end_slot();
-      if constexpr (!STAYS) end_slot();
+      if constexpr (!F::OWN_END) end_slot();
     } else {
       if constexpr (STAYS) {
         if (again) pin();
@@ -1270,7 +1270,7 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
       for (; t < nk; ++t, t3 = third(t3, 1)) {
         read_slot(t, t3, no, 0, no, 0, 0, all);
         multiply();
-        if (!STAYS || t + 1 < nk) end_slot();
+        if (!F::OWN_END || t + 1 < nk) end_slot();
       }
     }
     if constexpr (F::OWN_END && !SPLIT) asm volatile("" ::"v"(touched[0]), "v"(touched[1]));
