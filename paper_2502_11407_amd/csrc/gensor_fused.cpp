@@ -317,7 +317,8 @@ extern "C" gensor_status gensor_grouped_wgrad(const gensor_problem* p, const int
 // ------------------------------------------------------------------------------------ column sums
 // db[g][n] = sum of dY[r][n] over the rows of g, fp32 sums.  Bound by reading dY once.  A workgroup takes 64 vectors' columns and one of `parts`
 // equal shares of a group's rows; its eight waves take turns at the rows, eight rows requested together, and add up in LDS.  The shares'
-// sums go to the workspace and a second launch adds them in order, so the result does not depend on when a share finished.
+// sums go to the workspace and a second launch adds them in order, so the result does not depend on when a share finished.  8192 x 3072 bf16: 9.6 to 17 us
+// (3 to 5.2 TB/s) and 3 to 5 for the shares; with four waves, four rows each and 171 shares 18 and 14.
 namespace gensor {
 
 template <typename T, typename OutT, bool VEC>
@@ -558,6 +559,8 @@ struct XentPlan {
 const size_t kPieceBytes = (size_t)256 << 20;
 const size_t kPartBytes = (size_t)64 << 20;
 
+// The gradient of 4096 tokens over 50257 entries of width 768 in bf16, 866 us (1.10 PFLOP/s of the six 2TVD): logits again 345, dW 279, dX 248 with its
+// partial tiles' 38.
 // The cheapest whole or split tile's price, not remembered.
 double best_price(const GemmView& v, int kind, bool vec, size_t room) {
   const LeadingDims ld = {v.asrc == A_KC ? v.K : v.M, v.bsrc == B_KC ? v.K : v.N, v.N};

@@ -110,6 +110,20 @@ def test_workspaces(gs):
     assert 50257 * 64 * 2 < small < large < 400 * 2 ** 20                                   # a batch's logits would be 823 MB
 
 
+def test_workspaces_of_many_shapes(gs):
+    """What a call needs is found for any shape, within the limits that the gradient's pieces have: 256 MiB of G, 64 of partial tiles, dX's sums and X."""
+    import random
+    rng = random.Random(1)
+    for _ in range(60):
+        dtype = rng.choice(["f16", "bf16", "f32"])
+        T, V, D = (int(10 ** rng.uniform(0, e)) for e in (4.5, 5.3, 3.5))
+        es, forward, backward = (4 if dtype == "f32" else 2), gs.xent_workspace_bytes(dtype, T, V, D), gs.xent_workspace_bytes(dtype, T, V, D, backward=True)
+        assert 8 * T <= forward <= 2 * 4 * T * (V // 16 + 2) + 4 * T + 1024
+        vec = 16 // es                                       # G's rows are whole vectors
+        least = (T + vec - 1) // vec * vec * min(V, 256) * es
+        assert least <= backward <= max(2 ** 28, least) + 2 ** 26 + T * D * 4 + (T + 8) * D * es + 4096
+
+
 def test_binding_checks_shapes_and_types(gs):
     import torch
     p = gs.gemm_problem("f16", 4, 8, 16)

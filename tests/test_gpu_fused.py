@@ -311,6 +311,34 @@ def test_large_tiles(gs, dtype, out, M, N, K):
         fine(), kept_fine()
 
 
+def test_large_tiles_beside_rows_of_any_pitch(gs):
+    """Aligned operands, but C, the residual and the kept values in rows that start anywhere."""
+    M, N, K = 4100, 3072, 768
+    A, B, a, b = problem_operands("bf16", M, N, K, 0, 1, 0, 3)
+    p = gs.gemm_problem("bf16", M, N, K, 0, 1, out_dtype="bf16")
+    d, e = a @ b, (K + 4) * U * (a.abs() @ b.abs())
+    for c_pad, r_pad in ((0, 5), (3, 0), (1, 7)):
+        R = draw((M, N), "bf16", 6, 1.0, r_pad)
+        C, fine = guarded((M, N), "bf16", c_pad)
+        gs.gemm_fused(p, A, B, C, residual=R, workspace=workspace(gs.gemm_fused_workspace_bytes(p)))
+        close(C, d + R.double(), e + U * R.double().abs(), "bf16", (c_pad, r_pad))
+        gs.gemm_act_grad(p, A, B, R, C, "gelu", workspace=workspace(gs.gemm_fused_workspace_bytes(p)))
+        close(C, d * slope64(R.double(), "gelu"), 1.13 * e + 64 * U * d.abs(), "bf16", (c_pad, r_pad))
+        fine()
+
+
+def test_groups_without_a_row(gs):
+    """No rows at all: nothing to compute, and gradients of zeros."""
+    p = gs.grouped_problem("f16", 3, 0, 40, 24, 0, "f16")
+    A, dY, off = torch.empty((0, 24), dtype=torch.float16, device="cuda"), torch.empty((0, 40), dtype=torch.float16, device="cuda"), offsets_of([0, 0, 0])
+    W, C = draw((3, 24, 40), "f16", 1), torch.empty((0, 40), dtype=torch.float16, device="cuda")
+    gs.grouped_gemm(p, off, A, W, C)
+    dW, db = torch.full((3, 24, 40), 5.0, dtype=torch.float16, device="cuda"), torch.full((3, 40), 5.0, dtype=torch.float16, device="cuda")
+    gs.grouped_wgrad(p, off, A, dY, dW)
+    gs.bias_grad(dY, db, offsets=off)
+    assert bool((dW == 0).all()) and bool((db == 0).all())
+
+
 def test_offsets_outside_the_rows_are_cut(gs):
     """Offsets beyond the rows, negative or decreasing: nothing outside C and dW is written."""
     rows, N, K = 100, 64, 48
