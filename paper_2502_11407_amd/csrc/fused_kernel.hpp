@@ -254,7 +254,7 @@ struct Fused {
   // pairs of columns of a row, as the plain epilogue does: the exchange is its own inverse, so what is read goes the
   // same way backwards.  (Four columns a lane, in half as many stores, were 3 us slower on 8192 x 3072 x 768: 41.3 -> 44.4.)
   // What is read is requested as far ahead as 32 registers hold: a load's wait counts the stores before it, too.
-  // 8192 x 3072 x 768, us, on 16-bit types: nothing 42 (0.92 PFLOP/s), gelu 47, gelu with Z kept 58 (118 MB, 2.0 TB/s), a residual 57, the gradient through
+  // 8192 x 3072 x 768, us, on 16-bit types: nothing 42 (0.92 PFLOP/s), gelu 47, gelu with Z kept 57 (118 MB, 2.1 TB/s), a residual 57, the gradient through
   // gelu 62.  The products of all units and their stores take turns (two rounds of tiles in step), so the times add up: 28 of
   // products, 10 for each 50 MB moved, 5 for gelu's two transcendental operations a value.
   template <typename C, bool FULL, typename Acc>
