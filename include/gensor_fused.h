@@ -8,7 +8,7 @@
  * and rounded once, where a result is stored.  Types are those of gensor_gemm: operands of in_dtype, results of out_dtype, which is
  * GENSOR_F32 or in_dtype.  Rows may start anywhere; operands on 16-byte boundaries with rows of whole 16-byte vectors run the fastest
  * tiles, and 16-bit results (and what is read and kept beside them) on dword boundaries with even rows are stored in whole lines.  UNSUPPORTED: leading
- * dimensions so large that no tile's rows stay within 32-bit offsets (64-row tiles reach 2^31 / 65 bytes), or extents above
+ * dimensions so large that no tile's rows stay within 32-bit offsets (32-row tiles reach 2^31 / 33 bytes), or extents above
  * INT32_MAX - 256.
  */
 #ifndef GENSOR_FUSED_H

@@ -327,6 +327,29 @@ def test_large_tiles_beside_rows_of_any_pitch(gs):
         fine()
 
 
+def test_elements_beyond_32_bits(gs):
+    """Results of more than 2^31 elements: the last rows of a product with everything beside it, and of a grouped one."""
+    M, N, K = 70000, 32768, 64
+    A, B, bias = draw((M, K), "bf16", 1), draw((N, K), "bf16", 2, 0.1), draw((N,), "bf16", 3)
+    p = gs.gemm_problem("bf16", M, N, K, 0, 1, out_dtype="bf16")
+    C, kept = torch.empty((M, N), dtype=torch.bfloat16, device="cuda"), torch.empty((M, N), dtype=torch.bfloat16, device="cuda")
+    C[-300:] = 0.25
+    gs.gemm_fused(p, A, B, C, bias=bias, act="relu", preact=kept, residual=C)
+    rows = slice(M - 300, M)
+    z, e = A[rows].double() @ B.double().t() + bias.double(), (K + 4) * U * (A[rows].double().abs() @ B.double().abs().t() + bias.double().abs())
+    close(kept[rows], z, e, "bf16")
+    close(C[rows], act64(z, "relu") + 0.25, e + U * z.abs(), "bf16")
+    sizes = [40000, 29990, 10]
+    W = draw((3, N, K), "bf16", 4, 0.1)
+    gs.grouped_gemm(gs.grouped_problem("bf16", 3, M, N, K, 1, "bf16"), offsets_of(sizes), A, W, C)
+    for g, r in ((1, slice(69700, 69990)), (2, slice(69990, 70000))):
+        a, w = A[r].double(), W[g].double().t()
+        close(C[r], a @ w, (K + 4) * U * (a.abs() @ w.abs()), "bf16")
+    db = torch.empty((3, N), dtype=torch.float32, device="cuda")
+    gs.bias_grad(kept, db, offsets=offsets_of(sizes))
+    close(db[2], kept[69990:].double().sum(0), 14 * U * kept[69990:].double().abs().sum(0), "f32")
+
+
 def test_groups_without_a_row(gs):
     """No rows at all: nothing to compute, and gradients of zeros."""
     p = gs.grouped_problem("f16", 3, 0, 40, 24, 0, "f16")
