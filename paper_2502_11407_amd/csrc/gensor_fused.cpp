@@ -726,7 +726,7 @@ extern "C" gensor_status gensor_xent_forward(gensor_dtype dtype, int64_t T, int6
   hipError_t e = c.f->launch[FUSED_LSE](a, s);
   if (e != hipSuccess) return GENSOR_ERR_DEVICE;
   int per = 1;
-  while (per < 16 && per < T) per *= 2;
+  while (per < 32 && per < T) per *= 2;          // whole lines (of 8192 tokens: 3 us of 612 less than with 16, 15 less than with 8)
   hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)((T + per - 1) / per)), dim3(1024), 0, s, a.part_max, a.part_sum, (int)((V + wm - 1) / wm), (int)T, per,
                      targets, ignore_index, (int)V, a.at_target, loss, lse);
   return launched(hipGetLastError());
