@@ -593,10 +593,11 @@ struct Fused {
       const int64_t target = there ? a.targets[token] : -1;
       const bool counts = there && target != a.ignore && target >= 0 && target < a.vocab;
       const float lse = counts ? a.lse[token] : INFINITY, base = -1.44269504088896340736f * lse, g = counts ? a.dloss[token] * scale : 0.f;
+      // (zero by choice, not by g = 0: the logits of a token that does not count may be infinite or NaN)
 #pragma unroll
       for (int bi = 0; bi < C::MBLK; ++bi)
 #pragma unroll
-        for (int v = 0; v < NACC; ++v) acc[bi][bj][v] = g * probability<C>(acc[bi][bj][v], lse, base);
+        for (int v = 0; v < NACC; ++v) acc[bi][bj][v] = counts ? g * probability<C>(acc[bi][bj][v], lse, base) : 0.f;
       const int at = counts && target >= first && target < (int64_t)first + C::WM ? (int)(target - first) - 4 * fgrp : -1;
       if (__any(at >= 0)) {
 #pragma unroll
