@@ -95,13 +95,13 @@ gensor_status gensor_xent_forward(gensor_dtype dtype, int64_t T, int64_t V, int6
 
 /*
  * Its gradient: with G[t][v] = dloss[t] * (exp(z[t][v] - lse[t]) - (v == targets[t])), zero for tokens whose target is ignore_index
- * or outside [0, V), whatever their logits and their lse are,
+ * or outside [0, V), whatever their logits, their lse and their dloss are,
  *     dX = G * W,   dW = G^T * X
  * in `dtype`; dX or dW may be NULL.  (A row of X that is not finite reaches dW as zero times it.)  lse is the forward's, dloss (fp32, device) the
  * gradient of each token's loss.  The logits are computed again, a piece of the vocabulary at a time: G of a piece lies in the workspace in
- * `dtype` (f16: scaled by a power of two so that the largest |dloss| fills its range, undone in fp32), and dX is summed over the pieces in
- * fp32.  With less workspace than gensor_xent_workspace_bytes(..., 1) the pieces are smaller, down to 256 entries; WORKSPACE if not even
- * those fit.
+ * `dtype` (f16: scaled by a power of two so that the largest |dloss| of the tokens that count fills its range, undone in fp32), and dX is
+ * summed over the pieces in fp32.  With less workspace than gensor_xent_workspace_bytes(..., 1) the pieces are smaller, down to 256 entries;
+ * WORKSPACE if not even those fit.
  */
 gensor_status gensor_xent_backward(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, const void* X, int64_t ldx,
                                    const void* W, int64_t ldw, const int64_t* targets, int64_t ignore_index,

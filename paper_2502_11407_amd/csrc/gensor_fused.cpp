@@ -503,13 +503,15 @@ __global__ __launch_bounds__(1024) void xent_join_kernel(const float* part_max, 
   }
 }
 
-// f16 gradients of a mean are below its normal range: the largest dloss scaled to [2^14, 2^15).  scale[0] = a power of two, scale[1] its inverse.
-__global__ __launch_bounds__(1024) void xent_scale_kernel(const float* dloss, int tokens, float* scale) {
+// f16 gradients of a mean are below its normal range: the largest dloss of the tokens that count scaled to [2^14, 2^15).  (The others' G is zero,
+// whatever stands there: 1e8 at padding would leave the rest f16's last bits.)  scale[0] = a power of two, scale[1] its inverse.
+__global__ __launch_bounds__(1024) void xent_scale_kernel(const float* dloss, const int64_t* targets, int64_t ignore, int vocab, int tokens, float* scale) {
   __shared__ float tops[16];
   float top = 0.f;
   for (int t = threadIdx.x; t < tokens; t += 1024) {
     const float x = fabsf(dloss[t]);
-    if (x < INFINITY) top = fmaxf(top, x);
+    const int64_t target = targets[t];
+    if (x < INFINITY && target != ignore && target >= 0 && target < vocab) top = fmaxf(top, x);
   }
 #pragma unroll
   for (int d = 32; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
@@ -780,7 +782,7 @@ extern "C" gensor_status gensor_xent_backward(gensor_dtype dtype, int64_t T, int
     }
   }
   if (scaled) {
-    hipLaunchKernelGGL(xent_scale_kernel, dim3(1), dim3(1024), 0, s, dloss, (int)T, scales);
+    hipLaunchKernelGGL(xent_scale_kernel, dim3(1), dim3(1024), 0, s, dloss, targets, ignore_index, (int)V, (int)T, scales);
     if (hipGetLastError() != hipSuccess) return GENSOR_ERR_DEVICE;
   }
   if (pl.pad && dW) {

@@ -1,5 +1,5 @@
 """Tokens that do not count (their target is ignored or outside the vocabulary) have no say in the gradient of a projection's cross entropy,
-whatever their row of X and their lse hold: every other result is the same to the bit as with zeros in those places."""
+whatever their row of X, their lse and their dloss hold: every other result is the same to the bit as with zeros in those places."""
 import gc
 import math
 
@@ -78,3 +78,14 @@ def test_lse_that_does_not_count(gs, dtype, T, V, D):
         gX, gW = gradient(gs, dtype, X, W, t, lse, dloss)
         assert torch.equal(gX, dX) and torch.equal(gW, dW), value
 
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("T,V,D", SIZES)
+def test_dloss_that_does_not_count(gs, dtype, T, V, D):
+    """A mean over no token at all leaves 1 / 0 or 1e8 there; f16's scale is that of the tokens that count."""
+    X, W, t, out, lse, dloss, (dX, dW) = clean(gs, dtype, T, V, D)
+    assert bool((dW != 0).any())
+    for value in (1e8, -1e30, math.inf, math.nan):
+        dloss[out] = value
+        gX, gW = gradient(gs, dtype, X, W, t, lse, dloss)
+        assert torch.equal(gX, dX) and torch.equal(gW, dW), value
