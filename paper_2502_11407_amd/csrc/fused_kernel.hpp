@@ -512,16 +512,21 @@ struct Fused {
 #pragma unroll
         for (int v = 0; v < NACC; ++v) top = fmaxf(top, acc[bi][bj][v]);
       // exp(z - ref) in three operations: the product log2e * ref is rounded, which multiplies every term by the same factor 2^off; it is taken
-      // out of the sum, so that the maximum's own term is 1.  (Where that product would not be finite: four operations.)
+      // out of the sum, so that the maximum's own term is 1.  (Where that product would not be finite: four operations.  The column's own
+      // choice: a token's bits do not depend on what its neighbours hold.)
       const float ref = lse_reference(top);
+      const bool far = fabsf(ref) > 1e37f;
+      const float base = far ? 0.f : -(log2e * ref), off = far ? 0.f : fmaf(log2e, ref, base);
       float sum = 0.f;
-      if (__any(fabsf(ref) > 1e37f)) {
+      if (__any(far)) {
 #pragma unroll
-        for (int bi = 0; bi < C::MBLK; ++bi)
+        for (int bi = 0; bi < C::MBLK; ++bi) {
+          float part = 0.f;
 #pragma unroll
-          for (int v = 0; v < NACC; ++v) sum += __builtin_amdgcn_exp2f(log2e * (acc[bi][bj][v] - ref));
+          for (int v = 0; v < NACC; ++v) part += __builtin_amdgcn_exp2f(far ? log2e * (acc[bi][bj][v] - ref) : fmaf(log2e, acc[bi][bj][v], base));
+          sum += part;
+        }
       } else {
-        const float base = -(log2e * ref), off = fmaf(log2e, ref, base);
 #pragma unroll
         for (int bi = 0; bi < C::MBLK; ++bi) {
           float part = 0.f;
@@ -529,8 +534,8 @@ struct Fused {
           for (int v = 0; v < NACC; ++v) part += __builtin_amdgcn_exp2f(fmaf(log2e, acc[bi][bj][v], base));
           sum += part;
         }
-        sum *= __builtin_amdgcn_exp2f(-off);
       }
+      sum *= __builtin_amdgcn_exp2f(-off);
 #pragma unroll
       for (int d = MB; d < 64; d *= 2) {
         const float t2 = __shfl_xor(top, d, 64), s2 = __shfl_xor(sum, d, 64);

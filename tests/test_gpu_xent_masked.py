@@ -1,4 +1,4 @@
-"""Tokens that do not count (their target is ignored or outside the vocabulary) have no say in the gradient of a projection's cross entropy,
+"""Tokens that do not count (their target is ignored or outside the vocabulary) have no say in a projection's cross entropy and its gradient,
 whatever their row of X, their lse and their dloss hold: every other result is the same to the bit as with zeros in those places."""
 import gc
 import math
@@ -89,3 +89,18 @@ def test_dloss_that_does_not_count(gs, dtype, T, V, D):
         dloss[out] = value
         gX, gW = gradient(gs, dtype, X, W, t, lse, dloss)
         assert torch.equal(gX, dX) and torch.equal(gW, dW), value
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("T,V,D", SIZES)
+def test_losses_beside_rows_that_do_not_count(gs, dtype, T, V, D):
+    X, W, t, out = inputs(dtype, T, V, D)
+    ws, big = workspace(gs.xent_workspace_bytes(dtype, T, V, D)), float(torch.finfo(TORCH[dtype]).max)
+    want, lse, loss, full = (torch.empty(T, device="cuda") for _ in range(4))
+    X[out] = 0
+    gs.xent_forward(X, W, t, want, lse, ignore_index=IGNORE, workspace=ws)
+    for value in (big, -big, big / 16, math.inf, math.nan):
+        X[out] = value
+        gs.xent_forward(X, W, t, loss, full, ignore_index=IGNORE, workspace=ws)
+        assert torch.equal(full[~out], lse[~out]) and torch.equal(loss[~out], want[~out]), value
+        assert bool((loss[t == IGNORE] == 0).all())
