@@ -86,8 +86,9 @@ size_t gensor_bias_grad_workspace_bytes(gensor_dtype in_dtype, int64_t groups, i
  * `dtype`, targets int64 on the device.
  *     lse[t] = log sum_v exp(z[t][v]),   loss[t] = lse[t] - z[t][targets[t]]
  * in fp32; loss[t] = 0 where targets[t] == ignore_index, NaN where a target is neither that nor in [0, V).  loss or lse may be NULL (targets
- * too, without loss).  The workspace holds a maximum and a sum per token and slab of the vocabulary
- * (gensor_xent_workspace_bytes(..., 0), 256-byte aligned; WORKSPACE otherwise).
+ * too, without loss).  The workspace (256-byte aligned) holds a maximum and a sum per token and slab of the vocabulary.  What
+ * gensor_xent_workspace_bytes(..., 0) asks for serves any leading dimensions; with less, or where rows are too far apart for the tile it is
+ * meant for, the vocabulary is taken in pieces, a pair of launches each.  WORKSPACE if not even one row of tiles' slabs fit beside the sums so far.
  */
 gensor_status gensor_xent_forward(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, const void* X, int64_t ldx,
                                   const void* W, int64_t ldw, const int64_t* targets, int64_t ignore_index,

@@ -547,7 +547,8 @@ struct Fused {
       at_target[bj] = 0.f;
       if (a.targets) {
         const int64_t target = there ? a.targets[token] : -1;
-        const int at = target != a.ignore && target >= first && target < (int64_t)first + rows ? (int)(target - first) - 4 * fgrp : -1;
+        const int64_t entry = (int64_t)first + a.row_first;
+        const int at = target != a.ignore && target >= entry && target < entry + rows ? (int)(target - entry) - 4 * fgrp : -1;
         if (__any(at >= 0)) {
 #pragma unroll
           for (int bi = 0; bi < C::MBLK; ++bi)

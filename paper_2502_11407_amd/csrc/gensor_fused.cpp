@@ -463,9 +463,10 @@ extern "C" gensor_status gensor_bias_grad(gensor_dtype in_dtype, gensor_dtype ou
 namespace gensor {
 
 // The slabs' maxima and sums of a token joined.  A workgroup takes `per` tokens (a power of two); the threads of a token take turns at
-// the slabs, several requested together, and are joined in LDS.
-__global__ __launch_bounds__(1024) void xent_join_kernel(const float* part_max, const float* part_sum, int slabs, int tokens, int per, const int64_t* targets,
-                                                         int64_t ignore, int vocab, const float* at_target, float* loss, float* lse) {
+// the slabs, several requested together, and are joined in LDS.  keep_max: the slabs of further pieces follow, so what there is so far is left
+// there (it may be the first of the slabs) in place of results.
+__global__ __launch_bounds__(1024) void xent_join_kernel(const float* part_max, const float* part_sum, int slabs, int tokens, int per, float* keep_max, float* keep_sum,
+                                                         const int64_t* targets, int64_t ignore, int vocab, const float* at_target, float* loss, float* lse) {
   constexpr int UNROLL = 4;
   __shared__ float tops[1024], sums[1024];
   const int i = threadIdx.x, lanes = 1024 / per, lane = i / per;
@@ -494,6 +495,11 @@ __global__ __launch_bounds__(1024) void xent_join_kernel(const float* part_max, 
     }
   }
   if (lane != 0 || t >= tokens) return;
+  if (keep_max) {
+    keep_max[t] = top;
+    keep_sum[t] = sum;
+    return;
+  }
   const float ref = lse_reference(top), rest = logf(sum);
   if (lse) lse[t] = ref + rest;
   if (loss) {
@@ -685,13 +691,17 @@ extern "C" size_t gensor_xent_workspace_bytes(gensor_dtype dtype, int64_t T, int
     plan_xent(dtype, T, V, D, SIZE_MAX, &pl);
     return pl.total;
   }
-  // whichever tile the operands' alignment leads to
+  // whichever tile the operands' alignment leads to, and, for rows so far apart that a smaller tile serves them, a piece of any tile's
   const GemmView v = product_view(dtype, dtype, V, T, D, A_KC, B_KC);
   size_t most = 0;
   for (int vec = 0; vec < 2; ++vec) {
     FusedChoice c;
     const LeadingDims ld = {D, D, 0};
     if (choose(v, FUSED_LSE, vec != 0, ld, 0, &c) == GENSOR_OK) most = std::max(most, lse_bytes(T, V, c.f->d.wm));
+  }
+  for (int i = 0; i < g_num_fused; ++i) {
+    const InstanceDesc& d = g_fused[i].d;
+    if (g_fused[i].launch[FUSED_LSE] && instance_serves(d, v)) most = std::max(most, lse_bytes(T, std::min<int64_t>(V, d.bm + d.wm), d.wm));
   }
   return round_up((size_t)T * 4, 256) + 2 * most;
     }();
@@ -711,27 +721,49 @@ extern "C" gensor_status gensor_xent_forward(gensor_dtype dtype, int64_t T, int6
   FusedChoice c;
   st = choose_logits(dtype, FUSED_LSE, V, T, D, W, ldw, X, ldx, 0, &v, &c);
   if (st != GENSOR_OK) return st;
-  const int wm = c.f->d.wm;
-  const size_t head = round_up((size_t)T * 4, 256), each = lse_bytes(T, V, wm);
-  if (usable_room(workspace, workspace_bytes) < head + 2 * each) return GENSOR_ERR_WORKSPACE;
-  FusedArgs a = product_args(v, W, ldw, X, ldx, nullptr, 0, 1.f);
-  a.targets = loss ? targets : nullptr;
-  a.ignore = ignore_index;
-  a.tokens = (int32_t)T;
-  a.vocab = (int32_t)V;
-  a.at_target = (float*)workspace;
-  a.part_max = (float*)((char*)workspace + head);
-  a.part_sum = (float*)((char*)workspace + head + each);
+  const InstanceDesc& d = c.f->d;
+  const size_t room = usable_room(workspace, workspace_bytes), head = round_up((size_t)T * 4, 256);
+  // Room for fewer slabs than the vocabulary has (rows that are far apart lead to smaller tiles, of more slabs, than the room was asked for): pieces of
+  // as many whole tiles' rows as fit, evened out.  Slab 0 is what the pieces in front have been joined to.
+  int64_t piece = V, pieces = 1;
+  size_t each = lse_bytes(T, V, d.wm);
+  if (room < head + 2 * each) {
+    each = room > head ? (room - head) / 2 / 256 * 256 : 0;
+    const int64_t most = ((int64_t)(each / ((size_t)T * 4)) - 1) * d.wm / d.bm * d.bm;
+    if (most <= 0) return GENSOR_ERR_WORKSPACE;
+    pieces = (V + most - 1) / most;
+    piece = ((V + pieces - 1) / pieces + d.bm - 1) / d.bm * d.bm;
+    pieces = (V + piece - 1) / piece;
+  }
   hipStream_t s = (hipStream_t)hip_stream;
-  tiles_of(&a, v, c, V, T);
-  if ((int64_t)a.tiles_m * a.tiles_n > INT32_MAX) return GENSOR_ERR_UNSUPPORTED;
-  hipError_t e = c.f->launch[FUSED_LSE](a, s);
-  if (e != hipSuccess) return GENSOR_ERR_DEVICE;
+  float* at_target = (float*)workspace;
+  float* tops = (float*)((char*)workspace + head);
+  float* sums = (float*)((char*)workspace + head + each);
   int per = 1;
   while (per < 32 && per < T) per *= 2;          // whole lines (of 8192 tokens: 3 us of 612 less than with 16, 15 less than with 8)
-  hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)((T + per - 1) / per)), dim3(1024), 0, s, a.part_max, a.part_sum, (int)((V + wm - 1) / wm), (int)T, per,
-                     targets, ignore_index, (int)V, a.at_target, loss, lse);
-  return launched(hipGetLastError());
+  for (int64_t i = 0; i < pieces; ++i) {
+    const bool first = i == 0, last = i + 1 == pieces;
+    const int64_t entry = i * piece, rows = last ? V - entry : piece, kept = pieces > 1 ? T : 0;
+    const GemmView q = prob_view(dtype, rows, T, D);
+    FusedArgs a = product_args(q, (const char*)W + entry * ldw * size_of(dtype), ldw, X, ldx, nullptr, 0, 1.f);
+    a.targets = loss ? targets : nullptr;
+    a.ignore = ignore_index;
+    a.tokens = (int32_t)T;
+    a.row_first = (int32_t)entry;
+    a.vocab = (int32_t)V;
+    a.at_target = at_target;
+    a.part_max = tops + kept;
+    a.part_sum = sums + kept;
+    tiles_of(&a, q, c, rows, T);
+    if ((int64_t)a.tiles_m * a.tiles_n > INT32_MAX) return GENSOR_ERR_UNSUPPORTED;
+    if (c.f->launch[FUSED_LSE](a, s) != hipSuccess) return GENSOR_ERR_DEVICE;
+    const int64_t from = first ? kept : 0;
+    const int slabs = (int)((rows + d.wm - 1) / d.wm) + (first ? 0 : 1);
+    hipLaunchKernelGGL(xent_join_kernel, dim3((unsigned)((T + per - 1) / per)), dim3(1024), 0, s, tops + from, sums + from, slabs, (int)T, per,
+                       last ? nullptr : tops, last ? nullptr : sums, targets, ignore_index, (int)V, at_target, loss, lse);
+    if (hipGetLastError() != hipSuccess) return GENSOR_ERR_DEVICE;
+  }
+  return GENSOR_OK;
   });
 }
 
