@@ -535,18 +535,16 @@ __global__ __launch_bounds__(1024) void xent_scale_kernel(const float* dloss, co
 // rows of D elements copied to rows of D elements, `padded` of them, those behind `rows` zero
 template <int ES>
 __global__ __launch_bounds__(256) void xent_pad_kernel(const char* X, int64_t ld, int rows, int padded, int D, char* out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (i >= (int64_t)padded * D) return;
-  const int r = (int)(i / D), c = (int)(i - (int64_t)r * D);
-  if constexpr (ES == 4) ((uint32_t*)out)[i] = r < rows ? ((const uint32_t*)X)[(int64_t)r * ld + c] : 0u;
-  else ((uint16_t*)out)[i] = r < rows ? ((const uint16_t*)X)[(int64_t)r * ld + c] : (uint16_t)0;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)padded * D; i += (int64_t)gridDim.x * 256) {
+    const int r = (int)(i / D), c = (int)(i - (int64_t)r * D);
+    if constexpr (ES == 4) ((uint32_t*)out)[i] = r < rows ? ((const uint32_t*)X)[(int64_t)r * ld + c] : 0u;
+    else ((uint16_t*)out)[i] = r < rows ? ((const uint16_t*)X)[(int64_t)r * ld + c] : (uint16_t)0;
+  }
 }
 
 }  // namespace gensor
 
 namespace {
-
-struct XentShape { int dtype; int64_t T, V, D, ignore; };
 
 gensor_status check_xent(gensor_dtype dtype, int64_t T, int64_t V, int64_t D) {
   if (!valid_dtype(dtype) || T <= 0 || V <= 0 || D <= 0) return GENSOR_ERR_INVALID_ARG;
@@ -818,7 +816,8 @@ extern "C" gensor_status gensor_xent_backward(gensor_dtype dtype, int64_t T, int
     if (hipGetLastError() != hipSuccess) return GENSOR_ERR_DEVICE;
   }
   if (pl.pad && dW) {
-    const unsigned blocks = (unsigned)((pl.pitch * D + 255) / 256);
+    // (a launch has fewer than 2^32 threads along an axis, and the rest is cut off without an error)
+    const unsigned blocks = (unsigned)std::min<int64_t>((pl.pitch * D + 255) / 256, 1 << 20);
     if (es == 4) hipLaunchKernelGGL(xent_pad_kernel<4>, dim3(blocks), dim3(256), 0, s, (const char*)X, ldx, (int)T, (int)pl.pitch, (int)D, padded);
     else hipLaunchKernelGGL(xent_pad_kernel<2>, dim3(blocks), dim3(256), 0, s, (const char*)X, ldx, (int)T, (int)pl.pitch, (int)D, padded);
     if (hipGetLastError() != hipSuccess) return GENSOR_ERR_DEVICE;
