@@ -59,6 +59,15 @@ double tile_price(const FusedDesc& f, const GemmView& v, int kind, int split) {
   return std::max(us, fused_price(f.d, one, 1));
 }
 
+// Can one launch have all of the product's tiles?  (Ragged rows: as many as any offsets could need.  Split tiles add less than sixteen rounds.)
+bool tiles_fit(const InstanceDesc& d, const GemmView& v, int kind) {
+  const int64_t bn = d.alternate() && kind == FUSED_LINEAR ? 192 : d.bn;
+  const double rows = kind == FUSED_ROWS ? (double)(v.M * v.batch / d.bm + v.batch) : (double)((v.M + d.bm - 1) / d.bm) * (double)v.batch;
+  const double tiles = rows * (double)((v.N + bn - 1) / bn);
+  if (kind == FUSED_LSE && d.alternate()) return tiles <= INT32_MAX;         // its workgroups stay: a fixed number of them
+  return launch_fits(tiles + 16 * gensor_hw_mi355x()->compute_units, d.threads);
+}
+
 gensor_status choose(const GemmView& v, int kind, bool vec_ok, const LeadingDims& ld, size_t room, FusedChoice* out) {
   const std::array<int64_t, 14> key = {kind, v.in_dtype, v.out_dtype, v.asrc, v.bsrc, vec_ok, v.M, v.N, v.K, v.batch, ld.a, ld.b, ld.c, 0};
   std::lock_guard<std::mutex> lock(g_choice_mutex);
@@ -67,7 +76,7 @@ gensor_status choose(const GemmView& v, int kind, bool vec_ok, const LeadingDims
     std::vector<FusedChoice> all;
     for (int i = 0; i < g_num_fused; ++i) {
       const FusedDesc& f = g_fused[i];
-      if (!f.launch[kind] || !instance_serves(f.d, v) || (f.d.vec && !vec_ok) || !offsets_fit(f.d, v, ld)) continue;
+      if (!f.launch[kind] || !instance_serves(f.d, v) || (f.d.vec && !vec_ok) || !offsets_fit(f.d, v, ld) || !tiles_fit(f.d, v, kind)) continue;
       if (f.d.direct && !f.d.any_k() && (kind == FUSED_DEPTH || v.K % f.d.bk != 0)) continue;
       for (int split : kSplits) {
         if (split > 1 && (kind != FUSED_LINEAR || (v.K + f.d.bk - 1) / f.d.bk < split)) break;
@@ -147,13 +156,11 @@ gensor_status run_linear(FusedArgs& a, const GemmView& v, const FusedChoice& c, 
   const SplitPlan sp = split_plan(d, v, c.split, 0);
   a.narrow = d.alternate() && sp.split == 1 && narrow_tiles(v, gensor_hw_mi355x()->compute_units);
   tiles_of(&a, v, c, v.M, v.N, panel);
-  if ((int64_t)a.tiles_m * a.tiles_n > INT32_MAX) return GENSOR_ERR_UNSUPPORTED;
   a.split = sp.split;
   a.whole = sp.split == 1 ? a.tiles_m * a.tiles_n : (int32_t)sp.whole;
   if (sp.split == 1) return launched(c.f->launch[FUSED_LINEAR](a, st));
   a.partials = (float*)workspace;
   const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n - a.whole, blocks = tiles * (d.bm * d.bn / 4) / 256;
-  if (blocks > INT32_MAX) return GENSOR_ERR_UNSUPPORTED;
   hipError_t e = c.f->launch[FUSED_LINEAR_SPLIT](a, st);
   if (e != hipSuccess) return GENSOR_ERR_DEVICE;
   const unsigned n = (unsigned)blocks;
@@ -277,7 +284,6 @@ extern "C" gensor_status gensor_grouped_gemm(const gensor_problem* p, const int3
   tiles_of(&a, v, c, rows, v.N);
   // whole tiles of the rows, and one more of each group that can have rows
   const int64_t tile_rows = rows / c.f->d.bm + std::min(groups, rows);
-  if (tile_rows * a.tiles_n > INT32_MAX) return GENSOR_ERR_UNSUPPORTED;
   a.tiles_m = (int32_t)tile_rows;
   a.panel = 4;
   a.batch = 1;
@@ -313,7 +319,6 @@ extern "C" gensor_status gensor_grouped_wgrad(const gensor_problem* p, const int
   st = choose(v, FUSED_DEPTH, vector_ok(v, L, ldl, 0, R, ldr, 0), ld, 0, &c);
   if (st != GENSOR_OK) return st;
   tiles_of(&a, v, c, m, n);
-  if ((int64_t)a.tiles_m * a.tiles_n * a.batch > INT32_MAX) return GENSOR_ERR_UNSUPPORTED;
   return launched(c.f->launch[FUSED_DEPTH](a, (hipStream_t)hip_stream));
   });
 }
@@ -577,7 +582,7 @@ double best_price(const GemmView& v, int kind, bool vec, size_t room) {
   double best = 1e30;
   for (int i = 0; i < g_num_fused; ++i) {
     const FusedDesc& f = g_fused[i];
-    if (!f.launch[kind] || f.d.vec != (vec ? 1 : 0) || !instance_serves(f.d, v) || !offsets_fit(f.d, v, ld)) continue;
+    if (!f.launch[kind] || f.d.vec != (vec ? 1 : 0) || !instance_serves(f.d, v) || !offsets_fit(f.d, v, ld) || !tiles_fit(f.d, v, kind)) continue;
     for (int split : kSplits) {
       if (split > 1 && (kind != FUSED_LINEAR || (v.K + f.d.bk - 1) / f.d.bk < split)) break;
       const double us = tile_price(f, v, kind, split);
@@ -739,6 +744,7 @@ extern "C" gensor_status gensor_xent_forward(gensor_dtype dtype, int64_t T, int6
   float* sums = (float*)((char*)workspace + head + each);
   int per = 1;
   while (per < 32 && per < T) per *= 2;          // whole lines (of 8192 tokens: 3 us of 612 less than with 16, 15 less than with 8)
+  while (!launch_fits((double)((T + per - 1) / per), 1024)) per *= 2;
   for (int64_t i = 0; i < pieces; ++i) {
     const bool first = i == 0, last = i + 1 == pieces;
     const int64_t entry = i * piece, rows = last ? V - entry : piece, kept = pieces > 1 ? T : 0;
@@ -753,7 +759,6 @@ extern "C" gensor_status gensor_xent_forward(gensor_dtype dtype, int64_t T, int6
     a.part_max = tops + kept;
     a.part_sum = sums + kept;
     tiles_of(&a, q, c, rows, T);
-    if ((int64_t)a.tiles_m * a.tiles_n > INT32_MAX) return GENSOR_ERR_UNSUPPORTED;
     if (c.f->launch[FUSED_LSE](a, s) != hipSuccess) return GENSOR_ERR_DEVICE;
     const int64_t from = first ? kept : 0;
     const int slabs = (int)((rows + d.wm - 1) / d.wm) + (first ? 0 : 1);
@@ -839,7 +844,6 @@ extern "C" gensor_status gensor_xent_backward(gensor_dtype dtype, int64_t T, int
       a.row_first = (int32_t)q.first;
       a.vocab = (int32_t)V;
       tiles_of(&a, q.vp, q.cp, q.rows, pl.pitch);
-      if ((int64_t)a.tiles_m * a.tiles_n > INT32_MAX) return GENSOR_ERR_UNSUPPORTED;
       if (q.cp.f->launch[FUSED_PROB](a, s) != hipSuccess) return GENSOR_ERR_DEVICE;
     }
     if (dW) {

@@ -90,6 +90,9 @@ inline bool narrow_tiles(const GemmView& v, int64_t compute_units) {
 struct LeadingDims { int64_t a, b, c; };
 bool offsets_fit(const InstanceDesc& d, const GemmView& v, const LeadingDims& ld);
 
+// A launch has fewer than 2^32 threads along an axis; what is beyond is cut off without an error.
+inline bool launch_fits(double workgroups, int threads) { return workgroups * threads <= (double)UINT32_MAX; }
+
 // Can the operands be read in whole 16-byte vectors?
 bool vector_ok(const GemmView& v, const void* A, int64_t lda, int64_t strideA, const void* B, int64_t ldb, int64_t strideB);
 
