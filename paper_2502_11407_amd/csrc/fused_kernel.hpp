@@ -35,6 +35,7 @@ struct FusedArgs : KernelArgs {
   // groups
   const int32_t* offsets;          // groups + 1 of them; any values: what they name is cut to the `rows` there are
   int32_t groups, rows;
+  int32_t tile_first;              // MOVE_ROWS: the tile of workgroup 0 (of a call's further launches)
   // END_LSE and END_PROB; a column is a token
   const int64_t* targets;
   int64_t ignore;
@@ -176,6 +177,7 @@ struct Fused {
         total += __builtin_amdgcn_readlane(mine, 63);
       }
       total *= a.tiles_n;
+      id += a.tile_first;
       if (id >= total) return false;
       const int t = xcd_contiguous(id, total);
       int before = 0;                                // tile rows of the groups before this chunk of them

@@ -59,12 +59,12 @@ double tile_price(const FusedDesc& f, const GemmView& v, int kind, int split) {
   return std::max(us, fused_price(f.d, one, 1));
 }
 
-// Can one launch have all of the product's tiles?  (Ragged rows: as many as any offsets could need.  Split tiles add less than sixteen rounds.)
+// Can one launch have all of the product's tiles?  (Split tiles add less than sixteen rounds.)
 bool tiles_fit(const InstanceDesc& d, const GemmView& v, int kind) {
   const int64_t bn = d.alternate() && kind == FUSED_LINEAR ? 192 : d.bn;
-  const double rows = kind == FUSED_ROWS ? (double)(v.M * v.batch / d.bm + v.batch) : (double)((v.M + d.bm - 1) / d.bm) * (double)v.batch;
-  const double tiles = rows * (double)((v.N + bn - 1) / bn);
+  const double tiles = (double)((v.M + d.bm - 1) / d.bm) * (double)v.batch * (double)((v.N + bn - 1) / bn);
   if (kind == FUSED_LSE && d.alternate()) return tiles <= INT32_MAX;         // its workgroups stay: a fixed number of them
+  if (kind == FUSED_ROWS) return true;                                       // any number of launches
   return launch_fits(tiles + 16 * gensor_hw_mi355x()->compute_units, d.threads);
 }
 
@@ -236,6 +236,20 @@ extern "C" gensor_status gensor_gemm_fused(const gensor_problem* p, const gensor
   set_epilogue(&a, e, v, &ld);
   FusedChoice c;
   st = choose(v, FUSED_LINEAR, vector_ok(v, A, lda, 0, B, ldb, 0), ld, usable_room(workspace, workspace_bytes), &c);
+  if (st == GENSOR_ERR_UNSUPPORTED && v.M >= 1 << 20) {
+    // More tiles than a launch can have, whichever is taken: the rows in two halves (or rows too far apart, which the first half says, too)
+    gensor_problem half = *p;
+    half.M = (v.M / 2 + 255) / 256 * 256;
+    st = gensor_gemm_fused(&half, e, alpha, A, lda, B, ldb, C, ldc, workspace, workspace_bytes, hip_stream);
+    if (st != GENSOR_OK) return st;
+    gensor_epilogue rest = e ? *e : gensor_epilogue{};
+    if (rest.preact) rest.preact = (char*)rest.preact + half.M * rest.ld_preact * v.osize;
+    if (rest.residual) rest.residual = (const char*)rest.residual + half.M * rest.ld_residual * v.osize;
+    const char* A2 = (const char*)A + half.M * (v.asrc == A_KC ? lda : 1) * v.esize;
+    char* C2 = (char*)C + half.M * ldc * v.osize;
+    half.M = v.M - half.M;
+    return gensor_gemm_fused(&half, e ? &rest : nullptr, alpha, A2, lda, B, ldb, C2, ldc, workspace, workspace_bytes, hip_stream);
+  }
   if (st != GENSOR_OK) return st;
   // Panels of two tile rows: what is read and kept beside C lies closer together.  Two and four, us: 8192 x 3072 x 768 with Z kept 57.4 and 59.0,
   // the gradient through gelu with the bias's 78.6 and 83.0; 16384 x 3072 x 768 102.9 and 102.6, 4096 x 4096 x 1024 38.1 and 37.3, 8192 x 768 x
@@ -282,12 +296,18 @@ extern "C" gensor_status gensor_grouped_gemm(const gensor_problem* p, const int3
   st = choose(each, FUSED_ROWS, vector_ok(v, A, lda, 0, B, ldb, strideB), ld, 0, &c);
   if (st != GENSOR_OK) return st;
   tiles_of(&a, v, c, rows, v.N);
-  // whole tiles of the rows, and one more of each group that can have rows
+  // whole tiles of the rows, and one more of each group that can have rows; in several launches where one cannot have them
   const int64_t tile_rows = rows / c.f->d.bm + std::min(groups, rows);
-  a.tiles_m = (int32_t)tile_rows;
+  if (tile_rows * a.tiles_n > INT32_MAX) return GENSOR_ERR_UNSUPPORTED;
   a.panel = 4;
   a.batch = 1;
-  return launched(c.f->launch[FUSED_ROWS](a, (hipStream_t)hip_stream));
+  const int64_t most = std::max<int64_t>(1, UINT32_MAX / c.f->d.threads / a.tiles_n);
+  for (int64_t at = 0; at < tile_rows; at += most) {
+    a.tile_first = (int32_t)(at * a.tiles_n);
+    a.tiles_m = (int32_t)std::min(most, tile_rows - at);
+    if (c.f->launch[FUSED_ROWS](a, (hipStream_t)hip_stream) != hipSuccess) return GENSOR_ERR_DEVICE;
+  }
+  return GENSOR_OK;
   });
 }
 
@@ -317,6 +337,17 @@ extern "C" gensor_status gensor_grouped_wgrad(const gensor_problem* p, const int
   const LeadingDims ld = {ldl, ldr, lddw};
   FusedChoice c;
   st = choose(v, FUSED_DEPTH, vector_ok(v, L, ldl, 0, R, ldr, 0), ld, 0, &c);
+  if (st == GENSOR_ERR_UNSUPPORTED && groups >= 1 << 10) {
+    // more tiles than a launch can have: the groups in two halves (their rows stay where they are)
+    gensor_problem half = *p;
+    half.batch = groups / 2;
+    st = gensor_grouped_wgrad(&half, offsets, A, lda, dY, lddy, dW, lddw, stride_dw, hip_stream);
+    if (st != GENSOR_OK) return st;
+    char* dW2 = (char*)dW + half.batch * stride_dw * v.osize;
+    const int32_t* offsets2 = offsets + half.batch;
+    half.batch = groups - half.batch;
+    return gensor_grouped_wgrad(&half, offsets2, A, lda, dY, lddy, dW2, lddw, stride_dw, hip_stream);
+  }
   if (st != GENSOR_OK) return st;
   tiles_of(&a, v, c, m, n);
   return launched(c.f->launch[FUSED_DEPTH](a, (hipStream_t)hip_stream));
@@ -723,6 +754,14 @@ extern "C" gensor_status gensor_xent_forward(gensor_dtype dtype, int64_t T, int6
   GemmView v;
   FusedChoice c;
   st = choose_logits(dtype, FUSED_LSE, V, T, D, W, ldw, X, ldx, 0, &v, &c);
+  if (st == GENSOR_ERR_UNSUPPORTED && T >= 1 << 20) {
+    // more tiles than a launch can have: the tokens in two halves
+    const int64_t half = (T / 2 + 255) / 256 * 256;
+    st = gensor_xent_forward(dtype, half, V, D, X, ldx, W, ldw, targets, ignore_index, loss, lse, workspace, workspace_bytes, hip_stream);
+    if (st != GENSOR_OK) return st;
+    return gensor_xent_forward(dtype, T - half, V, D, (const char*)X + half * ldx * size_of(dtype), ldx, W, ldw, targets ? targets + half : nullptr, ignore_index,
+                               loss ? loss + half : nullptr, lse ? lse + half : nullptr, workspace, workspace_bytes, hip_stream);
+  }
   if (st != GENSOR_OK) return st;
   const InstanceDesc& d = c.f->d;
   const size_t room = usable_room(workspace, workspace_bytes), head = round_up((size_t)T * 4, 256);

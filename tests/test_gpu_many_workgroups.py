@@ -41,6 +41,18 @@ def test_grouped(gs):
     assert int((C != A).sum()) == 0
 
 
+def test_grouped_gradient(gs):
+    """A matrix of one element to each of twenty million groups, the first and the last ten of them empty."""
+    G = 20000000
+    off = torch.arange(G + 1, dtype=torch.int32, device="cuda").clamp_(10, G - 10)
+    A, dY = rows(G), torch.full((G, 1), 2.0, dtype=torch.float16, device="cuda")
+    dW = torch.full((G, 1, 1), 7.5, dtype=torch.float16, device="cuda")
+    gs.grouped_wgrad(gs.grouped_problem("f16", G, G, 1, 1, 0, "f16"), off, A, dY, dW)
+    want = 2 * A
+    want[:10], want[-10:] = 0, 0
+    assert int((dW.view(G, 1) != want).sum()) == 0
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_loss(gs, dtype):
     """lse moves by no more than a logit's error, 2 u |x w|, and 2e-6 + 2 u |lse| of the exponentials and sums."""
