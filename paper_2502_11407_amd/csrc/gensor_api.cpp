@@ -397,6 +397,32 @@ gensor_status run(const gensor_schedule* s, const gensor_problem* p, const GemmV
     sp = split_plan(*d, v, s->split_k, s->round_units);
   }
 
+  // More tiles than a launch can have: two halves, of the batch or of the rows (which reach 2^31 / 33 bytes at most: a row has 2^20 tiles).
+  const int64_t narrowest = d->alternate() ? 192 : d->bn;
+  const double tiles = (double)((v.M + d->bm - 1) / d->bm) * (double)((v.N + narrowest - 1) / narrowest) * (double)v.batch;
+  if (!launch_fits(tiles + 16.0 * gensor_hw_mi355x()->compute_units, d->threads)) {
+    GemmView head = v, rest = v;
+    int64_t a_at = 0, b_at = 0, c_at = 0;
+    if (v.bsrc == B_CONV) return GENSOR_ERR_UNSUPPORTED;
+    if (s != &local) local = *s;
+    local.split_k = 1;                                           // (a half has another remainder than the room was brought for)
+    s = &local;
+    if (v.batch > 1) {
+      head.batch = v.batch / 2;
+      rest.batch = v.batch - head.batch;
+      a_at = head.batch * strideA; b_at = head.batch * strideB; c_at = head.batch * strideC;
+    } else {
+      head.M = (v.M / 2 + 255) / 256 * 256;
+      rest.M = v.M - head.M;
+      a_at = head.M * (v.asrc == A_KC ? lda : 1); c_at = head.M * ldc;
+      if (rest.M <= 0) return GENSOR_ERR_UNSUPPORTED;
+    }
+    const gensor_status st = run(s, p, head, alpha, A, lda, strideA, B, ldb, strideB, beta, C, ldc, strideC, workspace, workspace_bytes, stream);
+    if (st != GENSOR_OK) return st;
+    return run(s, p, rest, alpha, (const char*)A + a_at * v.esize, lda, strideA, (const char*)B + b_at * v.esize, ldb, strideB, beta,
+               (char*)C + c_at * v.osize, ldc, strideC, workspace, workspace_bytes, stream);
+  }
+
   KernelArgs a;
   std::memset(&a, 0, sizeof(a));
   a.A = A; a.B = B; a.C = C;

@@ -74,3 +74,19 @@ def test_loss(gs, dtype):
         bad += int(((loss[at:at + step].double() - (want - z.gather(1, t[at:at + step, None])[:, 0])).abs() > 2 * limit).sum())
     assert bad == 0
 
+
+def test_plain_product(gs):
+    A, B = rows(ROWS), torch.full((1, 1), 2.0, dtype=torch.float16, device="cuda")
+    C = torch.full((ROWS, 1), 7.5, dtype=torch.float16, device="cuda")
+    gs.gemm(gs.gemm_problem("f16", ROWS, 1, 1, out_dtype="f16"), A, B, C)
+    assert int((C != 2 * A).sum()) == 0
+
+
+def test_plain_batches(gs):
+    """Thirty million products of two rows, a column and two terms."""
+    n = 30000000
+    A, B = (rows(4 * n) % 29).view(n, 2, 2), torch.full((n, 2, 1), 2.0, dtype=torch.float16, device="cuda")
+    B[:, 1] = 3.0
+    C = torch.full((n, 2, 1), 7.5, dtype=torch.float16, device="cuda")
+    gs.bmm(gs.gemm_problem("f16", 2, 1, 2, batch=n, out_dtype="f16"), A, B, C)
+    assert int((C[:, :, 0] != 2 * A[:, :, 0] + 3 * A[:, :, 1]).sum()) == 0
