@@ -4,6 +4,8 @@
 // arithmetic on the vector ALUs and one store per output.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "../../include/gensor.h"
 #include "gemm_kernel.hpp"
 
@@ -217,9 +219,9 @@ __global__ __launch_bounds__(256) void avgpool_lds_kernel(const char* in, void* 
 }
 
 template <typename T, typename OutT>
-__global__ __launch_bounds__(256) void avgpool_direct_kernel(const void* in, void* out, int64_t total, int H, int W, int P, int Q, int F,
-                                                             int S) {
-  const int64_t idx = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(256) void avgpool_direct_kernel(const void* in, void* out, int64_t first, int64_t total, int H, int W, int P, int Q,
+                                                             int F, int S) {
+  const int64_t idx = first + (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (idx >= total) return;
   const int64_t t = idx / Q;
   const int q = (int)(idx - t * Q);
@@ -283,8 +285,10 @@ hipError_t launch_pool(const void* in, void* out, int64_t planes, int64_t h, int
                        (int)h, (int)w, (int)P, (int)Q, (int)f, (int)s, (int)G, (int)R, (int)cpp);
   } else {
     const int64_t total = planes * P * Q;
-    hipLaunchKernelGGL((avgpool_direct_kernel<T, OutT>), dim3((unsigned)((total + 255) / 256)), dim3(256), 0, st, in, out, total, (int)h,
-                       (int)w, (int)P, (int)Q, (int)f, (int)s);
+    const int64_t most = (int64_t)1 << 31;                       // outputs of a launch, which has fewer than 2^32 threads
+    for (int64_t first = 0; first < total; first += most)
+      hipLaunchKernelGGL((avgpool_direct_kernel<T, OutT>), dim3((unsigned)((std::min(most, total - first) + 255) / 256)), dim3(256), 0, st, in, out, first,
+                         total, (int)h, (int)w, (int)P, (int)Q, (int)f, (int)s);
   }
   return hipGetLastError();
 }
