@@ -235,9 +235,12 @@ def _sref(s):
 
 
 def _ws(workspace):
+    """Address and bytes of a workspace, or of none.  The kernels write to it: memory of the host's, or a view with gaps, is refused."""
     if workspace is None:
         return None, 0
-    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if not (workspace.is_cuda and workspace.is_contiguous()):
+        raise ValueError(f"workspace: a contiguous device tensor is wanted, got strides {workspace.stride()} on {workspace.device}")
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def gemm(p: Problem, A, B, Cout, alpha: float = 1.0, beta: float = 0.0, schedule: Optional[Schedule] = None,
@@ -279,8 +282,7 @@ def workspace_bytes(p: Problem, schedule: Optional[Schedule] = None) -> int:
 def conv2d(p: Problem, I, W, O, schedule: Optional[Schedule] = None, workspace=None, stream=None):
     """O = conv(I, W): contiguous NCHW input, KCRS filters, NKPQ output, all on the device.
     `workspace` is a device tensor of at least workspace_bytes(p, schedule) bytes (or None)."""
-    ws_ptr = workspace.data_ptr() if workspace is not None else None
-    ws_len = workspace.numel() * workspace.element_size() if workspace is not None else 0
+    ws_ptr, ws_len = _ws(workspace)
     st = lib.gensor_conv2d(_sref(schedule), C.byref(p), I.data_ptr(), W.data_ptr(), O.data_ptr(), ws_ptr, ws_len,
                            _stream_ptr(stream))
     _check(st, "gensor_conv2d")
@@ -418,7 +420,7 @@ def _gemm_fused(p, A, B, Cout, bias, act, preact, residual, grad, alpha, workspa
     lda = _matrix(A, K, M, dtype, "A") if p.transA else _matrix(A, M, K, dtype, "A")
     ldb = _matrix(B, N, K, dtype, "B") if p.transB else _matrix(B, K, N, dtype, "B")
     ldc = _matrix(Cout, M, N, out, "C")
-    ws_ptr, ws_len = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    ws_ptr, ws_len = _ws(workspace)
     st = lib.gensor_gemm_fused(C.byref(p), e, alpha, A.data_ptr(), lda, B.data_ptr(), ldb, Cout.data_ptr(), ldc, ws_ptr, ws_len, _stream_ptr(stream))
     if st:
         _check(st, "gensor_gemm_fused")
@@ -493,7 +495,7 @@ def bias_grad(dY, db, offsets=None, stream=None, workspace=None):
     if db.shape != ((N,) if offsets is None else (groups, N)) or not db.is_contiguous() or not db.is_cuda:
         raise ValueError(f"db: a contiguous device tensor of {(N,) if offsets is None else (groups, N)} is wanted, got {tuple(db.shape)} on {db.device}")
     ld = _matrix(dY, rows, N, dY.dtype, "dY")
-    ws_ptr, ws_len = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    ws_ptr, ws_len = _ws(workspace)
     st = lib.gensor_bias_grad(dt, out, groups, rows, N, dY.data_ptr(), ld, off, db.data_ptr(), ws_ptr, ws_len, _stream_ptr(stream))
     if st:
         _check(st, "gensor_bias_grad")
@@ -509,7 +511,7 @@ def xent_forward(X, W, targets, loss, lse, ignore_index: int = -100, stream=None
     (T, D), (V, _) = X.shape, W.shape
     dt, dtype = _code(X, "X"), X.dtype
     ldx, ldw = _matrix(X, T, D, dtype, "X"), _matrix(W, V, D, dtype, "W")
-    ws_ptr, ws_len = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    ws_ptr, ws_len = _ws(workspace)
     _check(lib.gensor_xent_forward(dt, T, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw,
                                    None if targets is None else _vector(targets, T, "torch.int64", "targets"), ignore_index,
                                    None if loss is None else _vector(loss, T, "torch.float32", "loss"),
@@ -522,7 +524,7 @@ def xent_backward(X, W, targets, lse, dloss, dX, dW, ignore_index: int = -100, s
     (T, D), (V, _) = X.shape, W.shape
     dt, dtype = _code(X, "X"), X.dtype
     ldx, ldw = _matrix(X, T, D, dtype, "X"), _matrix(W, V, D, dtype, "W")
-    ws_ptr, ws_len = (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
+    ws_ptr, ws_len = _ws(workspace)
     _check(lib.gensor_xent_backward(dt, T, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, _vector(targets, T, "torch.int64", "targets"), ignore_index,
                                     _vector(lse, T, "torch.float32", "lse"), _vector(dloss, T, "torch.float32", "dloss"),
                                     None if dX is None else dX.data_ptr(), 0 if dX is None else _matrix(dX, T, D, dtype, "dX"),
