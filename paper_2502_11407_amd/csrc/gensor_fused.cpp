@@ -50,6 +50,9 @@ const int kSplits[] = {1, 2, 3, 4, 5, 6, 7, 8, 10, 12, 14, 16};
 // The cost model's time.  A group's tiles of a product over ragged rows take as long as its rows are many, and groups are rarely even: a launch
 // is no shorter than one group of three times the mean's rows alone.  (8 groups of 2048 rows on average, the largest 5000, 768 x 3072 each:
 // 256x256 tiles 121 us, 256x128 103; 32 groups of 512: 125 and 149.)
+// (An unsplit 256x256 tile is priced as 192-column ones where narrow_tiles() says so, for the grouped, logit and probability ends too, which have no such
+// form.  At the price of the wide form 1.2 % of the choices over drawn shapes change, to smaller tiles: 53 of them took 0.80 to 1.35 of the
+// time, in the geometric mean 1.004.)
 double tile_price(const FusedDesc& f, const GemmView& v, int kind, int split) {
   const double us = fused_price(f.d, v, split);
   if (kind != FUSED_DEPTH || us <= 0 || v.batch == 1) return us;
@@ -283,10 +286,11 @@ extern "C" gensor_status gensor_grouped_gemm(const gensor_problem* p, const int3
   st = check_epilogue(e, v, C);
   if (st != GENSOR_OK) return st;
   if (rows == 0) return GENSOR_OK;
-  FusedArgs a = product_args(v, A, lda, B, ldb, C, ldc, alpha);
-  LeadingDims ld = {lda, ldb, ldc};
-  GemmView each = v;                       // what a group is on average, for the choice of the tile
+  GemmView all = v, each = v;              // one output of all rows; what a group is on average, for the choice of the tile
+  all.batch = 1;
   each.M = (rows + groups - 1) / groups;
+  FusedArgs a = product_args(all, A, lda, B, ldb, C, ldc, alpha);
+  LeadingDims ld = {lda, ldb, ldc};
   set_epilogue(&a, e, v, &ld);
   a.strideB = strideB;
   a.offsets = offsets;
@@ -295,6 +299,11 @@ extern "C" gensor_status gensor_grouped_gemm(const gensor_problem* p, const int3
   FusedChoice c;
   st = choose(each, FUSED_ROWS, vector_ok(v, A, lda, 0, B, ldb, strideB), ld, 0, &c);
   if (st != GENSOR_OK) return st;
+  // Rows of C that do not start on cache lines: the tiles at any alignment, whose own rows are not whole vectors either, leave write-through
+  // earlier.  Through and back, us: 8 groups, 8355 x 502 x 120 f16 (8 MB) 9.4 and 8.7, 13345 x 1100 x 264 (28 MB) 26.6 and 24.1, with fp32
+  // output 7149 rows (30 MB) 21.3 and 20.5; but 4 MB 7.2 both, fp32 output of 8 MB 10.4 and 10.9.  Aligned: 16 groups, 8192 x 1000 x 256 (16 MB) 19.5 and
+  // 20.8, 8192 x 1400 x 352 (22 MB) 18.0 and 19.8.
+  if (!c.f->d.vec && (ldc * v.osize) % 128 != 0) a.through = rows * v.N * v.osize <= (v.osize == 2 ? 4ll : 16ll) * 1024 * 1024;
   tiles_of(&a, v, c, rows, v.N);
   // whole tiles of the rows, and one more of each group that can have rows; in several launches where one cannot have them
   const int64_t tile_rows = rows / c.f->d.bm + std::min(groups, rows);
