@@ -100,7 +100,7 @@ gensor_status gensor_xent_forward(gensor_dtype dtype, int64_t T, int64_t V, int6
  *     dX = G * W,   dW = G^T * X
  * in `dtype`; dX or dW may be NULL.  (A row of X that is not finite reaches dW as zero times it.)  lse is the forward's, dloss (fp32, device) the
  * gradient of each token's loss.  The logits are computed again, a piece of the vocabulary at a time: G of a piece lies in the workspace in
- * `dtype` (f16: scaled by a power of two so that the largest |dloss| of the tokens that count fills its range, undone in fp32), and dX is
+ * `dtype` (16-bit types: scaled so that the largest |dloss| of the tokens that count is 2^15, undone in fp32), and dX is
  * summed over the pieces in fp32.  With less workspace than gensor_xent_workspace_bytes(..., 1) the pieces are smaller, down to 256 entries;
  * WORKSPACE if not even those fit.
  */

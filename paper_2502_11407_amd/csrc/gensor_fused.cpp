@@ -554,8 +554,10 @@ __global__ __launch_bounds__(1024) void xent_join_kernel(const float* part_max, 
   }
 }
 
-// f16 gradients of a mean are below its normal range: the largest dloss of the tokens that count scaled to [2^14, 2^15).  (The others' G is zero,
-// whatever stands there: 1e8 at padding would leave the rest f16's last bits.)  scale[0] = a power of two, scale[1] its inverse.
+// G is rounded to the type, and most of it is -dloss at the targets: where all tokens have the same dloss (1 / 401 is 0.26 % off in bf16, 0.035 in f16) that
+// would be one common factor of both gradients.  So G is scaled to make the largest dloss of the tokens that count 2^15, which both types
+// have and which fills f16's range (gradients of a mean are below its normal one); the products undo it in fp32.  (The other tokens' G is zero,
+// whatever stands there: 1e8 at padding would leave the rest f16's last bits.)  scale[0] = the factor, scale[1] its inverse.
 __global__ __launch_bounds__(1024) void xent_scale_kernel(const float* dloss, const int64_t* targets, int64_t ignore, int vocab, int tokens, float* scale) {
   __shared__ float tops[16];
   float top = 0.f;
@@ -570,11 +572,9 @@ __global__ __launch_bounds__(1024) void xent_scale_kernel(const float* dloss, co
   __syncthreads();
   if (threadIdx.x != 0) return;
   for (int w = 1; w < 16; ++w) top = fmaxf(top, tops[w]);
-  int e = 0;
-  if (top > 0.f) (void)frexpf(top, &e);            // top = m 2^e, m in [0.5, 1)
-  e = min(max(15 - e, -100), 100);
-  scale[0] = ldexpf(1.f, e);
-  scale[1] = ldexpf(1.f, -e);
+  const float f = top > 0.f ? fminf(fmaxf(32768.f / top, 0x1p-100f), 0x1p100f) : 1.f;
+  scale[0] = f;
+  scale[1] = 1.f / f;
 }
 
 // rows of D elements copied to rows of D elements, `padded` of them, those behind `rows` zero
@@ -836,7 +836,7 @@ extern "C" gensor_status gensor_xent_backward(gensor_dtype dtype, int64_t T, int
   char* parts = (char*)sums + pl.sum_bytes;
   char* G = parts + pl.part_bytes;
   hipStream_t s = (hipStream_t)hip_stream;
-  const bool scaled = dtype == GENSOR_F16;
+  const bool scaled = dtype != GENSOR_F32;
 
   // every product's tile is chosen before anything is launched
   struct Piece { int64_t first, rows; GemmView vp, vw, vx; FusedChoice cp, cw, cx; };
