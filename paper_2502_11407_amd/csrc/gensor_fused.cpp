@@ -66,7 +66,8 @@ double tile_price(const FusedDesc& f, const GemmView& v, int kind, int split) {
 bool tiles_fit(const InstanceDesc& d, const GemmView& v, int kind) {
   const int64_t bn = d.alternate() && kind == FUSED_LINEAR ? 192 : d.bn;
   const double tiles = (double)((v.M + d.bm - 1) / d.bm) * (double)v.batch * (double)((v.N + bn - 1) / bn);
-  if (kind == FUSED_LSE && d.alternate()) return tiles <= INT32_MAX;         // its workgroups stay: a fixed number of them
+  // (the logits' workgroups stay: a fixed number of them, each of which counts one round beyond its last tile)
+  if (kind == FUSED_LSE && d.alternate()) return tiles <= INT32_MAX - gensor_hw_mi355x()->compute_units;
   if (kind == FUSED_ROWS) return true;                                       // any number of launches
   return launch_fits(tiles + 16 * gensor_hw_mi355x()->compute_units, d.threads);
 }
