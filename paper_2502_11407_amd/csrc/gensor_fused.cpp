@@ -560,12 +560,21 @@ __global__ __launch_bounds__(1024) void xent_join_kernel(const float* part_max, 
 // have and which fills f16's range (gradients of a mean are below its normal one); the products undo it in fp32.  (The other tokens' G is zero,
 // whatever stands there: 1e8 at padding would leave the rest f16's last bits.)  scale[0] = the factor, scale[1] its inverse.
 __global__ __launch_bounds__(1024) void xent_scale_kernel(const float* dloss, const int64_t* targets, int64_t ignore, int vocab, int tokens, float* scale) {
+  constexpr int UNROLL = 8;
   __shared__ float tops[16];
   float top = 0.f;
-  for (int t = threadIdx.x; t < tokens; t += 1024) {
-    const float x = fabsf(dloss[t]);
-    const int64_t target = targets[t];
-    if (x < INFINITY && target != ignore && target >= 0 && target < vocab) top = fmaxf(top, x);
+  for (int first = threadIdx.x; first < tokens; first += UNROLL * 1024) {
+    float x[UNROLL];
+    int64_t target[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const bool there = first + u * 1024 < tokens;
+      x[u] = there ? fabsf(dloss[first + u * 1024]) : 0.f;
+      target[u] = there ? targets[first + u * 1024] : ignore;
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u)
+      if (x[u] < INFINITY && target[u] != ignore && target[u] >= 0 && target[u] < vocab) top = fmaxf(top, x[u]);
   }
 #pragma unroll
   for (int d = 32; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
