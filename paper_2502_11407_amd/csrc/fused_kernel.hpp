@@ -485,8 +485,8 @@ struct Fused {
   // ---- the logits of a wave's rows (vocabulary entries) reduced for each column (token).  A lane's registers are rows of one
   // column, so the reduction stays inside the lane but for the two or four lane groups of a block at the end: with the tokens
   // as rows it would cross 32 lanes for every row.  Bound by the products; then by the vector unit, three operations and an exponential a
-  // logit, 3 us of a tile's 22.  8192 tokens, 50257 entries, 768 wide, f16: 536 us, 1.18 PFLOP/s, where the product that stores its logits takes
-  // 645.
+  // logit, 3 us of a tile's 22.  8192 tokens, 50257 entries, 768 wide, f16: 560 to 600 us with the join's 8, 1.05 to 1.13 PFLOP/s (matrix units busy 54 % of the
+  // cycles, 0.97 GB read), where the product that stores its logits takes 645.
   template <typename C, typename Acc, typename Hook>
   static __device__ __attribute__((always_inline)) void finish_lse(const FusedArgs& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p, Hook&& before_stores) {
     constexpr int MB = C::MB, NACC = MB * MB / 64;
@@ -587,7 +587,8 @@ struct Fused {
   }
 
   // ---- scale * dloss * (softmax - one at the target), in the input type, a product's operand next.  Columns beyond the tokens,
-  // up to whole vectors (store_n), are written as zeros.  4096 tokens, 50257 entries, 768 wide, bf16: 345 us in two pieces, 0.92 PFLOP/s.
+  // up to whole vectors (store_n), are written as zeros.  4096 tokens, 50257 entries, 768 wide, bf16: 340 to 360 us in two pieces,
+  // 0.88 to 0.93 PFLOP/s.
   template <typename C, typename Acc>
   static __device__ __attribute__((always_inline)) void finish_prob(const FusedArgs& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p) {
     constexpr int MB = C::MB, NACC = MB * MB / 64;

@@ -619,13 +619,13 @@ struct XentPlan {
   size_t pad_bytes, sum_bytes, part_bytes, piece_bytes, total;
 };
 
-// A piece's G at most: larger pieces fill the chip in more whole rounds and split dX's sum less often (50257 entries, 4096 tokens, 768 wide, bf16: pieces
-// of 64 MiB 1215 us, 128 1051, 256 956), but the logits of a batch are not to be kept.
+// A piece's G at most: larger pieces fill the chip in more whole rounds and split dX's sum less often (50257 entries, 4096 tokens, 768 wide, bf16: in a
+// workspace of 64 MiB 1721 us, 128 1259, 192 1082, 306, as asked for with pieces of 256 at most, 866), but the logits of a batch are not to be kept.
 const size_t kPieceBytes = (size_t)256 << 20;
 const size_t kPartBytes = (size_t)64 << 20;
 
-// The gradient of 4096 tokens over 50257 entries of width 768 in bf16, 866 us (1.10 PFLOP/s of the six 2TVD): logits again 345, dW 279, dX 248 with its
-// partial tiles' 38.
+// The gradient of 4096 tokens over 50257 entries of width 768 in bf16, 866 us (1.10 PFLOP/s of the six 2TVD): logits again 337 to 361, dW 271 to 286, dX 241 to
+// 260 and its partial tiles' sums 39, the scale 5.
 // The cheapest whole or split tile's price, not remembered.
 double best_price(const GemmView& v, int kind, bool vec, size_t room) {
   const LeadingDims ld = {v.asrc == A_KC ? v.K : v.M, v.bsrc == B_KC ? v.K : v.N, v.N};
