@@ -1,4 +1,4 @@
-"""ctypes face of libgensor.so (include/gensor.h and include/gensor_fused.h).  Argument marshalling only: every step
+"""ctypes face of libgensor.so (include/gensor.h, include/gensor_fused.h and include/gensor_lm.h).  Argument marshalling only: every step
 of the operators runs in the library's HIP kernels, the constructor in its C++ host code.
 PyTorch is used for device memory and the current stream, nothing else.
 
@@ -28,6 +28,9 @@ EXPORTS = ["gensor_hw_mi355x", "gensor_construct", "gensor_construct_trace", "ge
 FUSED_EXPORTS = ["gensor_gemm_fused", "gensor_gemm_fused_workspace_bytes", "gensor_grouped_gemm", "gensor_grouped_wgrad",
                  "gensor_bias_grad", "gensor_bias_grad_workspace_bytes", "gensor_xent_forward", "gensor_xent_backward",
                  "gensor_xent_workspace_bytes"]          # include/gensor_fused.h
+LM_EXPORTS = ["gensor_gated_gemm", "gensor_gated_act_grad", "gensor_logprobs", "gensor_logprobs_workspace_bytes", "gensor_distill_forward",
+              "gensor_distill_backward", "gensor_distill_workspace_bytes"]               # include/gensor_lm.h
+TOP_MAX, TEACHER_MAX = 64, 256
 
 
 class Problem(C.Structure):
@@ -136,6 +139,20 @@ def _load():
     L.gensor_xent_backward.argtypes = [i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, vp, vp, i64, vp, i64, vp, sz, vp]
     L.gensor_xent_workspace_bytes.restype = sz
     L.gensor_xent_workspace_bytes.argtypes = [i32, i64, i64, i64, i32]
+    L.gensor_gated_gemm.restype = i32
+    L.gensor_gated_gemm.argtypes = [P, i32, f32, vp, i64, vp, i64, i64, vp, vp, i64, vp, i64, i64, vp]
+    L.gensor_gated_act_grad.restype = i32
+    L.gensor_gated_act_grad.argtypes = [P, i32, f32, vp, i64, vp, i64, vp, i64, i64, vp, i64, i64, vp, i64, vp]
+    L.gensor_logprobs.restype = i32
+    L.gensor_logprobs.argtypes = [i32, i64, i64, i64, vp, i64, vp, i64, f32, vp, i64, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+    L.gensor_logprobs_workspace_bytes.restype = sz
+    L.gensor_logprobs_workspace_bytes.argtypes = [i32, i64, i64, i64, i32]
+    L.gensor_distill_forward.restype = i32
+    L.gensor_distill_forward.argtypes = [i32, i64, i64, i64, vp, i64, vp, i64, f32, i32, vp, vp, i32, vp, vp, vp, sz, vp]
+    L.gensor_distill_backward.restype = i32
+    L.gensor_distill_backward.argtypes = [i32, i64, i64, i64, vp, i64, vp, i64, f32, i32, vp, vp, i32, vp, vp, vp, i64, vp, i64, vp, sz, vp]
+    L.gensor_distill_workspace_bytes.restype = sz
+    L.gensor_distill_workspace_bytes.argtypes = [i32, i64, i64, i64, i32, i32]
     return L
 
 
@@ -530,3 +547,141 @@ def xent_backward(X, W, targets, lse, dloss, dX, dW, ignore_index: int = -100, s
                                     None if dX is None else dX.data_ptr(), 0 if dX is None else _matrix(dX, T, D, dtype, "dX"),
                                     None if dW is None else dW.data_ptr(), 0 if dW is None else _matrix(dW, V, D, dtype, "dW"),
                                     ws_ptr, ws_len, _stream_ptr(stream)), "gensor_xent_backward")
+
+
+# ---- a language model's gated layers, the scores of its vocabulary, and learning from a teacher.  The launches go to the current device: tensors
+# of another one are refused.
+def _on_current_device(stream, **tensors):
+    import torch
+    here = torch.cuda.current_device()
+    if stream is not None and stream.device_index != here:
+        raise ValueError(f"stream: one of the current device, {here}, is wanted, got device {stream.device_index}")
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != here:
+            raise ValueError(f"{name}: a tensor on the current device, {here}, is wanted, got {t.device}")
+
+
+def _act(act: str) -> int:
+    code = ACT.get(act)
+    if code is None:
+        raise ValueError(f"act: one of {sorted(ACT)} is wanted, got {act!r}")
+    return code
+
+
+def _two(t, rows: int, cols: int, dtype, what: str):
+    """Two matrices as one tensor [2][rows][cols], wherever the second lies behind the first: (leading dimension, distance)."""
+    if t.shape == (2, rows, cols) and t.dtype is dtype and t.is_cuda:
+        far, ld, inner = t.stride()
+        if (cols == 1 or inner == 1) and (rows == 1 or ld >= cols):
+            return ld if rows > 1 else cols, far
+        raise ValueError(f"{what}: contiguous rows that do not overlap are wanted, got strides {t.stride()}")
+    raise ValueError(f"{what}: two device matrices of {rows} x {cols} {dtype} are wanted, got {tuple(t.shape)} {t.dtype} on {t.device}")
+
+
+def gated_gemm(p: Problem, A, B, Cout, act: str = "silu", bias=None, preact=None, alpha: float = 1.0, stream=None):
+    """C = act(G) * U of the products G = alpha A op(B[0]) + bias[0] and U = alpha A op(B[1]) + bias[1]: p is either product's, B [2][K][N] ([2][N][K] if
+    p.transB) a tensor of both matrices, which may lie side by side in one: W.view(K, 2, N).transpose(0, 1).  bias [2][N]; preact [2][M][N] receives G
+    and U in C's type (as the gradient needs them)."""
+    if _TORCH is None:
+        _torch_types()
+    M, N, K, dtype, out = p.M, p.N, p.K, _TORCH[p.in_dtype], _TORCH[p.out_dtype]
+    code = _act(act)
+    lda, ldc = _matrix(A, M, K, dtype, "A"), _matrix(Cout, M, N, out, "C")
+    ldb, far = _two(B, N, K, dtype, "B") if p.transB else _two(B, K, N, dtype, "B")
+    ldz, far_z = (0, 0) if preact is None else _two(preact, M, N, out, "preact")
+    if bias is not None and (bias.shape != (2, N) or not bias.is_contiguous() or bias.dtype is not dtype or not bias.is_cuda):
+        raise ValueError(f"bias: a contiguous device tensor of {(2, N)} {dtype} is wanted, got {tuple(bias.shape)} {bias.dtype} on {bias.device}")
+    _on_current_device(stream, A=A, B=B, C=Cout, bias=bias, preact=preact)
+    st = lib.gensor_gated_gemm(C.byref(p), code, alpha, A.data_ptr(), lda, B.data_ptr(), ldb, far, None if bias is None else bias.data_ptr(), Cout.data_ptr(), ldc,
+                               None if preact is None else preact.data_ptr(), ldz, far_z, _stream_ptr(stream))
+    if st:
+        _check(st, "gensor_gated_gemm")
+
+
+def gated_act_grad(p: Problem, A, B, preact, dpreact, act: str = "silu", H=None, alpha: float = 1.0, stream=None):
+    """At the end of the product D = alpha A op(B), the gradient of a gated layer's result: dpreact[0] = D * U * act'(G) and dpreact[1] = D * act(G) of
+    preact = (G, U), all [2][M][N]; dpreact may be preact.  H [M][N] receives act(G) * U again."""
+    if _TORCH is None:
+        _torch_types()
+    M, N, K, dtype, out = p.M, p.N, p.K, _TORCH[p.in_dtype], _TORCH[p.out_dtype]
+    code = _act(act)
+    lda = _matrix(A, M, K, dtype, "A")
+    ldb = _matrix(B, N, K, dtype, "B") if p.transB else _matrix(B, K, N, dtype, "B")
+    ldz, far_z = _two(preact, M, N, out, "preact")
+    ldd, far_d = _two(dpreact, M, N, out, "dpreact")
+    ldh = 0 if H is None else _matrix(H, M, N, out, "H")
+    _on_current_device(stream, A=A, B=B, preact=preact, dpreact=dpreact, H=H)
+    st = lib.gensor_gated_act_grad(C.byref(p), code, alpha, A.data_ptr(), lda, B.data_ptr(), ldb, preact.data_ptr(), ldz, far_z, dpreact.data_ptr(), ldd, far_d,
+                                   None if H is None else H.data_ptr(), ldh, _stream_ptr(stream))
+    if st:
+        _check(st, "gensor_gated_act_grad")
+
+
+def _table(t, shape, dtype: str, what: str) -> int:
+    """The address of a contiguous device tensor."""
+    if t.shape != shape or not t.is_contiguous() or not t.is_cuda or str(t.dtype) != dtype:
+        raise ValueError(f"{what}: a contiguous device tensor of {shape} {dtype} is wanted, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def logprobs_workspace_bytes(dtype: str, T: int, V: int, D: int, top: int = 0) -> int:
+    return int(lib.gensor_logprobs_workspace_bytes(DTYPE[dtype], T, V, D, top))
+
+
+def logprobs(X, W, targets=None, logprob=None, lse=None, entropy=None, top_index=None, top_logprob=None, scale: float = 1.0, ignore_index: int = -100,
+             stream=None, workspace=None):
+    """Scores of the logits z = scale X W^T, which are not kept: X [T][D], W [V][D] of one type.  Into logprob [T] the log probabilities of `targets` [T]
+    int64, into lse [T] log sum exp z, into entropy [T] the distributions' entropies, into top_index [T][k] int64 and top_logprob [T][k] the k most likely entries
+    and their log probabilities, falling, of equal ones the lowest first; all fp32, each may be None.  `workspace`: logprobs_workspace_bytes(...) bytes, or
+    less for smaller pieces of the vocabulary."""
+    (T, D), (V, _) = X.shape, W.shape
+    dt, dtype = _code(X, "X"), X.dtype
+    ldx, ldw = _matrix(X, T, D, dtype, "X"), _matrix(W, V, D, dtype, "W")
+    if (top_index is None) != (top_logprob is None):
+        raise ValueError("top_index and top_logprob: both or neither are wanted")
+    top = 0 if top_index is None else top_index.shape[-1]
+    if top_index is not None and top == 0:
+        raise ValueError("top_index: room for one alternative at least is wanted")
+    ws_ptr, ws_len = _ws(workspace)
+    _on_current_device(stream, X=X, W=W, targets=targets, logprob=logprob, lse=lse, entropy=entropy, top_index=top_index, top_logprob=top_logprob, workspace=workspace)
+    _check(lib.gensor_logprobs(dt, T, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, scale, None if targets is None else _vector(targets, T, "torch.int64", "targets"),
+                               ignore_index, None if logprob is None else _vector(logprob, T, "torch.float32", "logprob"),
+                               None if lse is None else _vector(lse, T, "torch.float32", "lse"), None if entropy is None else _vector(entropy, T, "torch.float32", "entropy"),
+                               top, None if top == 0 else _table(top_index, (T, top), "torch.int64", "top_index"),
+                               None if top == 0 else _table(top_logprob, (T, top), "torch.float32", "top_logprob"), ws_ptr, ws_len, _stream_ptr(stream)), "gensor_logprobs")
+
+
+def distill_workspace_bytes(dtype: str, T: int, V: int, D: int, k: int, backward: bool = False) -> int:
+    return int(lib.gensor_distill_workspace_bytes(DTYPE[dtype], T, V, D, k, 1 if backward else 0))
+
+
+def _distill(X, W, index, teacher, stream, **tensors):
+    (T, D), (V, _), k = X.shape, W.shape, index.shape[-1]
+    dt, dtype = _code(X, "X"), X.dtype
+    ldx, ldw = _matrix(X, T, D, dtype, "X"), _matrix(W, V, D, dtype, "W")
+    at, q = _table(index, (T, k), "torch.int64", "index"), _table(teacher, (T, k), "torch.float32", "teacher")
+    _on_current_device(stream, X=X, W=W, index=index, teacher=teacher, **tensors)
+    return dt, T, V, D, ldx, ldw, k, at, q
+
+
+def distill_forward(X, W, index, teacher, loss, lse, scale: float = 1.0, normalize: bool = True, stream=None, workspace=None):
+    """loss[t] = sum_j p_j (log p_j - z[index_j] + lse) of the logits z = scale X W^T, which are not kept, against a teacher's entries: index [T][k] int64 (-1: none)
+    and their log probabilities teacher [T][k] fp32; p = softmax of scale * teacher over the token's entries, or exp(teacher) as it is.  loss and lse [T]
+    fp32, either may be None.  `workspace`: distill_workspace_bytes(...) bytes."""
+    dt, T, V, D, ldx, ldw, k, at, q = _distill(X, W, index, teacher, stream, loss=loss, lse=lse, workspace=workspace)
+    ws_ptr, ws_len = _ws(workspace)
+    _check(lib.gensor_distill_forward(dt, T, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, scale, k, at, q, 1 if normalize else 0,
+                                      None if loss is None else _vector(loss, T, "torch.float32", "loss"),
+                                      None if lse is None else _vector(lse, T, "torch.float32", "lse"), ws_ptr, ws_len, _stream_ptr(stream)), "gensor_distill_forward")
+
+
+def distill_backward(X, W, index, teacher, lse, dloss, dX, dW, scale: float = 1.0, normalize: bool = True, stream=None, workspace=None):
+    """dX = G W and dW = G^T X with G[t][v] = dloss[t] scale (P exp(z[t][v] - lse[t]) - sum of p_j over index_j == v), P = sum_j p_j; dX or dW may be None.
+    `workspace`: distill_workspace_bytes(..., backward=True) bytes, or less for smaller pieces of the vocabulary."""
+    dt, T, V, D, ldx, ldw, k, at, q = _distill(X, W, index, teacher, stream, lse=lse, dloss=dloss, dX=dX, dW=dW, workspace=workspace)
+    ws_ptr, ws_len = _ws(workspace)
+    _check(lib.gensor_distill_backward(dt, T, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, scale, k, at, q, 1 if normalize else 0,
+                                       _vector(lse, T, "torch.float32", "lse"), _vector(dloss, T, "torch.float32", "dloss"),
+                                       None if dX is None else dX.data_ptr(), 0 if dX is None else _matrix(dX, T, D, X.dtype, "dX"),
+                                       None if dW is None else dW.data_ptr(), 0 if dW is None else _matrix(dW, V, D, X.dtype, "dW"),
+                                       ws_ptr, ws_len, _stream_ptr(stream)), "gensor_distill_backward")

@@ -56,8 +56,9 @@ def generate():
         _write_if_changed(path, "\n".join(src))
         tus.append(path)
     tus += generate_fused()
+    tus += generate_lm()
     for f in os.listdir(GEN):                      # units of an earlier lattice
-        if f.endswith(".hip") and os.path.join(GEN, f) not in tus and f not in ("registry.hip", "fused_registry.hip"):
+        if f.endswith(".hip") and os.path.join(GEN, f) not in tus and f not in ("registry.hip", "fused_registry.hip", "lm_registry.hip"):
             os.remove(os.path.join(GEN, f))
             if os.path.exists(os.path.join(GEN, f[:-4] + ".o")):
                 os.remove(os.path.join(GEN, f[:-4] + ".o"))
@@ -117,18 +118,50 @@ def generate_fused():
     return tus + [path]
 
 
+LM_ENDS = {"score": ("ScoreArgs", "Score"), "teach": ("FusedArgs", "Teach"), "gated_grad": ("GatedArgs", "GatedGrad"), "gated": ("GatedArgs", "Gated")}
+
+
+def generate_lm():
+    """Units and tables of the ends of lm_kernel.hpp: those of the tiles above, and the tiles of two products at once."""
+    units, reg = [], ['#include "lm_registry.hpp"', "#if !defined(__HIP_DEVICE_COMPILE__)", "namespace gensor {"]
+    fused, gated = lattice.fused(), lattice.gated()
+    for name, group in (("lm", fused), ("gated", gated)):
+        for d in group:
+            ends = ["gated"] if name == "gated" else lattice.lm_ends(d)
+            if not ends:
+                continue
+            src = ['#include "lm_registry.hpp"', "namespace gensor {", "typedef %s C_%d;" % (lattice.cfg_type(d), d["id"])]
+            for k in ends:
+                src.append("hipError_t %s_%d_%s(const %s& a, hipStream_t st) { return launch_end<C_%d, %s>(a, st); }" % (name, d["id"], k, LM_ENDS[k][0], d["id"], LM_ENDS[k][1]))
+                reg.append("hipError_t %s_%d_%s(const %s&, hipStream_t);" % (name, d["id"], k, LM_ENDS[k][0]))
+            path = os.path.join(GEN, "%s%s_%03d.hip" % (name, "chains" if lattice.chains(d) > 1 else "", d["id"]))
+            _write_if_changed(path, "\n".join(src + ["}  // namespace gensor\n"]))
+            units.append(path)
+    reg.append("const LmEnds g_lm_ends[] = {")
+    reg += ["  {%s}," % ", ".join("lm_%d_%s" % (d["id"], k) if k in lattice.lm_ends(d) else "nullptr" for k in ("score", "teach", "gated_grad")) for d in fused]
+    reg += ["};", "const GatedDesc g_gated[] = {"]
+    reg += ["  {{%s, nullptr, nullptr}, gated_%d_gated}," % (instance_fields(d), d["id"]) for d in gated]
+    reg += ["};", "const int g_num_gated = %d;" % len(gated), "}  // namespace gensor", "#endif\n"]
+    path = os.path.join(GEN, "lm_registry.hip")
+    _write_if_changed(path, "\n".join(reg))
+    return units + [path]
+
+
 def _compile(src):
     obj = os.path.join(GEN, os.path.basename(src).rsplit(".", 1)[0] + ".o")
     deps = [src, os.path.join(HERE, "gemm_kernel.hpp"), os.path.join(HERE, "conv_kernel.hpp"), os.path.join(HERE, "conv_rows_kernel.hpp"), os.path.join(HERE, "registry.hpp"),
             os.path.join(HERE, "host_common.hpp"), os.path.join(PKG, "..", "include", "gensor.h")]
     if "fused" in os.path.basename(src):
         deps += [os.path.join(HERE, "fused_kernel.hpp"), os.path.join(HERE, "fused_registry.hpp"), os.path.join(PKG, "..", "include", "gensor_fused.h")]
+    if os.path.basename(src).startswith(("lm", "gated", "gensor_lm")):
+        deps += [os.path.join(HERE, f) for f in ("fused_kernel.hpp", "fused_registry.hpp", "lm_kernel.hpp", "lm_registry.hpp", "fused_host.hpp")]
+        deps += [os.path.join(PKG, "..", "include", f) for f in ("gensor_fused.h", "gensor_lm.h")]
     if os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps if os.path.exists(d)):
         return obj
     # host sources: no fused multiply-add contraction, so the constructor's double arithmetic
     # is the plain IEEE sequence its tests compare against
     extra = ["-ffp-contract=off"] if src.endswith(".cpp") else []
-    if os.path.basename(src).startswith(("conv_", "chains_", "fusedchains_")):
+    if os.path.basename(src).startswith(("conv_", "chains_", "fusedchains_", "lmchains_", "gatedchains_")):
         extra += CONV_FLAGS
     cmd = [HIPCC] + FLAGS + extra + ["-x", "hip", "-c", src, "-o", obj]
     r = subprocess.run(cmd, capture_output=True, text=True)
@@ -143,7 +176,7 @@ def _compile(src):
 def build(force=False, jobs=None):
     tus = generate()
     tus += [os.path.join(HERE, "gensor_api.cpp"), os.path.join(HERE, "constructor.cpp"), os.path.join(HERE, "scan_kernels.cpp"),
-            os.path.join(HERE, "gensor_fused.cpp")]
+            os.path.join(HERE, "gensor_fused.cpp"), os.path.join(HERE, "gensor_lm.cpp")]
     probe = os.path.join(HERE, "probe.cpp")
     if force:
         for f in os.listdir(GEN):

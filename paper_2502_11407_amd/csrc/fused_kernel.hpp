@@ -107,7 +107,7 @@ struct Fused {
   typedef FusedArgs Args;
   static constexpr int MOVES = MOVE;
   static constexpr bool OWN_END = true;
-  static constexpr bool STAYS = END == END_LSE;
+  static constexpr bool STAYS = END == END_LSE, DUAL = false;
   // The rows of the first 64 groups, one a lane.
   static __device__ __attribute__((always_inline)) GroupRows own_group(const FusedArgs& a) {
     GroupRows r{0, -1};

@@ -324,12 +324,13 @@ __device__ inline void tile_of(const KernelArgs& args, int t, int& tile_m, int& 
 
 // What a launch does with the tile of a workgroup: `Args` are the kernel's arguments, MOVES whether the products are grouped and `place`
 // finds the tile and the group's rows (PLACE_ROWS: of A and C, PLACE_DEPTH: k rows of both operands), OWN_END whether `finish`
-// takes the place of the plain epilogue.  This is the plain product.
+// takes the place of the plain epilogue.  DUAL: the products of A with two matrices of B, KernelArgs::strideB apart, a tile computing BN / 2
+// columns of each.  This is the plain product.
 enum { PLACE_ALL = 0, PLACE_ROWS = 1, PLACE_DEPTH = 2 };
 struct PlainOutput {
   typedef KernelArgs Args;
   static constexpr int MOVES = PLACE_ALL;
-  static constexpr bool OWN_END = false, STAYS = false;
+  static constexpr bool OWN_END = false, STAYS = false, DUAL = false;
 };
 
 // A tile of a grouped product: the group, its rows, the tile inside them.
@@ -405,7 +406,8 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
     tile_of(args, wg - bidx * tiles_per_batch, tile_m, tile_n);
   }
   int m0 = tile_m * BM;
-  int n0 = tile_n * BN;
+  constexpr int BNC = F::DUAL ? BN / 2 : BN;          // columns of C that the tile computes
+  int n0 = tile_n * BNC;
 
   // k range of this workgroup: the whole of K, or k tiles [kpart * nk / kparts, (kpart + 1) * nk / kparts) of a split
   // tile.  The operand bases move to the first k of the range and Kx is its length, so everything below
@@ -459,7 +461,13 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
   };
   if constexpr (F::MOVES == PLACE_ROWS) Ab += (int64_t)where.first * args.lda * ES;
   int rows_valid = min(BM, (F::MOVES == PLACE_ROWS ? where.count : args.M) - m0);
-  int cols_valid = min(BN, args.N - n0);
+  int cols_valid = min(BNC, args.N - n0);
+  // DUAL: a wave's columns of the B tile are WN / 2 of the first matrix and the same WN / 2 of the second, so that a lane holds both products
+  // of one place of C.  Both matrices are reached from the first one's base: the descriptor ends with the second, what lies between them is memory
+  // that the caller says is there, and rows or columns beyond N are never stored.
+  const uint32_t b_far = F::DUAL ? (uint32_t)(args.strideB * ES) : 0u;
+  auto b_column = [](int c) -> int { return F::DUAL ? c / C::WN * (C::WN / 2) + c % (C::WN / 2) : c; };       // of its matrix
+  auto b_matrix = [&](int c) -> uint32_t { return F::DUAL && c % C::WN >= C::WN / 2 ? b_far : 0u; };
   const char* a_tile = (C::ASRC == A_KC) ? Ab + (int64_t)m0 * args.lda * ES : Ab + (int64_t)m0 * ES;
   const char* b_tile = (C::BSRC == B_KC) ? Bb + (int64_t)n0 * args.ldb * ES : (C::BSRC == B_NCS2 ? Bb : Bb + (int64_t)n0 * ES);
   // Operands without VEC start anywhere: the descriptor begins at the 16-byte granule that holds the tile's first
@@ -480,13 +488,13 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
   auto rsrc_b = [&](int k0) {
     if constexpr (C::BSRC == B_KC)
       return __builtin_amdgcn_make_buffer_rsrc((void*)(b_tile + (int64_t)k0 * ES), 0,
-          clamp_records(((int64_t)(cols_valid - 1) * args.ldb + (Kx - k0)) * ES), RSRC_FLAGS);
+          clamp_records(((int64_t)(cols_valid - 1) * args.ldb + (Kx - k0)) * ES + b_far), RSRC_FLAGS);
     else if constexpr (C::BSRC == B_NCS2)
       return __builtin_amdgcn_make_buffer_rsrc((void*)(b_tile + (int64_t)k0 * args.ldb * ES), 0,
           clamp_records((int64_t)(Kx - k0) * args.ldb * ES), RSRC_FLAGS);
     else
       return __builtin_amdgcn_make_buffer_rsrc((void*)(b_tile + (int64_t)k0 * args.ldb * ES), 0,
-          clamp_records(((int64_t)(Kx - k0 - 1) * args.ldb + (args.N - n0)) * ES), RSRC_FLAGS);
+          clamp_records(((int64_t)(Kx - k0 - 1) * args.ldb + (args.N - n0)) * ES + b_far), RSRC_FLAGS);
   };
 
   // ---- who loads what.  A thread owns LDS chunk slots q = tid + i*THREADS of a
@@ -519,7 +527,7 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
     const int q = tid + i * C::THREADS;
     if constexpr (C::BSRC == B_KC) {
       const int row = q / C::CPR, ch = swizzled_chunk(row, q % C::CPR, C::RPP, C::VN);
-      b_voff[i] = (uint32_t)((row * (int)args.ldb + ch * EPC) * ES);
+      b_voff[i] = (uint32_t)((b_column(row) * (int)args.ldb + ch * EPC) * ES) + b_matrix(row);
       b_kch[i] = ch * EPC;
     } else if constexpr (C::BSRC == B_NCS2) {
       // chunk = EPC consecutive columns = two halves of EPC/2 columns, each inside one output
@@ -537,7 +545,7 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
       const int krow = q / CPRN;
       int ch = q % CPRN;
       if constexpr (C::NC_DIRECT) ch ^= nc_swizzle(krow, C::VN) >> 4;      // slot q receives the chunk the swizzle maps there
-      b_voff[i] = (uint32_t)((krow * (int)args.ldb + ch * EPC) * ES);
+      b_voff[i] = (uint32_t)((krow * (int)args.ldb + b_column(ch * EPC)) * ES) + b_matrix(ch * EPC);
       b_kch[i] = krow;
     }
   }
@@ -662,10 +670,10 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
       }
     } else if constexpr (LOOSE_B) {
       if constexpr (C::BSRC == B_KC)
-        fetch_loose(b_tile + (int64_t)k0 * ES, ((int64_t)(cols_valid - 1) * args.ldb + (Kx - k0)) * ES, full, Kx - k0,
+        fetch_loose(b_tile + (int64_t)k0 * ES, ((int64_t)(cols_valid - 1) * args.ldb + (Kx - k0)) * ES + b_far, full, Kx - k0,
                     b_voff, b_kch, rb[set], std::true_type{}, std::integral_constant<int, C::B_CHUNKS>{});
       else
-        fetch_loose(b_tile + (int64_t)k0 * args.ldb * ES, ((int64_t)(Kx - k0 - 1) * args.ldb + (args.N - n0)) * ES, Kx - k0 >= BK + EPC - 1, Kx - k0,
+        fetch_loose(b_tile + (int64_t)k0 * args.ldb * ES, ((int64_t)(Kx - k0 - 1) * args.ldb + (args.N - n0)) * ES + b_far, Kx - k0 >= BK + EPC - 1, Kx - k0,
                     b_voff, b_kch, rb[set], std::false_type{}, std::integral_constant<int, C::B_CHUNKS>{});
     } else {
       const __amdgpu_buffer_rsrc_t r = rsrc_b(k0);
@@ -674,7 +682,8 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
         if (C::B_CHUNKS % C::THREADS != 0 && tid + i * C::THREADS >= C::B_CHUNKS) break;
         if (i * parts < part * C::B_LOADS || i * parts >= (part + 1) * C::B_LOADS) continue;
         uint32_t off = b_voff[i];
-        if constexpr (C::BSRC == B_KC && (!C::DIRECT || C::RING_16)) off = (full || (int)b_kch[i] < Kx - k0) ? off : OOB;
+        // (k rows of the first of two matrices beyond K are no end of the descriptor's: what lies there may be infinite)
+        if constexpr ((C::BSRC == B_KC && (!C::DIRECT || C::RING_16)) || (F::DUAL && C::BSRC == B_NC)) off = (full || (int)b_kch[i] < Kx - k0) ? off : OOB;
         if constexpr (C::DIRECT) {
           __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (GENSOR_LDS void*)(lds + st * C::STAGE_BYTES + C::A_BYTES + (i * C::THREADS + wave * 64) * 16),
                                                    16, off, 0, 0, 0);
@@ -695,8 +704,8 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
       const __amdgpu_buffer_rsrc_t r = C::ASRC == A_KC ? loose_rsrc(a_tile + (int64_t)k0 * ES, ((int64_t)(rows_valid - 1) * args.lda + (Kx - k0)) * ES, skew)
           : loose_rsrc(a_tile + (int64_t)k0 * args.lda * ES, ((int64_t)(Kx - k0 - 1) * args.lda + (args.M - m0)) * ES, skew);
       load_chunks(r, skew, a_voff, ra[set], std::integral_constant<int, C::A_CHUNKS>{});
-      const __amdgpu_buffer_rsrc_t q = C::BSRC == B_KC ? loose_rsrc(b_tile + (int64_t)k0 * ES, ((int64_t)(cols_valid - 1) * args.ldb + (Kx - k0)) * ES, skew)
-          : loose_rsrc(b_tile + (int64_t)k0 * args.ldb * ES, ((int64_t)(Kx - k0 - 1) * args.ldb + (args.N - n0)) * ES, skew);
+      const __amdgpu_buffer_rsrc_t q = C::BSRC == B_KC ? loose_rsrc(b_tile + (int64_t)k0 * ES, ((int64_t)(cols_valid - 1) * args.ldb + (Kx - k0)) * ES + b_far, skew)
+          : loose_rsrc(b_tile + (int64_t)k0 * args.ldb * ES, ((int64_t)(Kx - k0 - 1) * args.ldb + (args.N - n0)) * ES + b_far, skew);
       load_chunks(q, skew, b_voff, rb[set], std::integral_constant<int, C::B_CHUNKS>{});
     }
   };
@@ -1047,12 +1056,13 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
       const int q2 = half_b * (NBR * 256) + q;
       if constexpr (C::BSRC == B_KC) {
         const int row = q2 / C::CPR;
-        vb[i] = (uint32_t)((row * (int)args.ldb + swizzled_chunk(row, q2 % C::CPR, C::RPP, C::VN) * EPC) * ES);
-        step_b = (uint32_t)((512 / C::CPR) * (int)args.ldb * ES);
+        static_assert(!F::DUAL || 512 / C::CPR == C::WN, "the step is from one wave's columns to the next one's");
+        vb[i] = (uint32_t)((b_column(row) * (int)args.ldb + swizzled_chunk(row, q2 % C::CPR, C::RPP, C::VN) * EPC) * ES) + b_matrix(row);
+        step_b = (uint32_t)((512 / C::CPR / (F::DUAL ? 2 : 1)) * (int)args.ldb * ES);
       } else {
         constexpr int CPRN = BN * ES / 16;
         const int krow = q2 / CPRN, ch = (q2 % CPRN) ^ (swizzle_b(krow) >> 4);
-        vb[i] = (uint32_t)((krow * (int)args.ldb + ch * EPC) * ES);
+        vb[i] = (uint32_t)((krow * (int)args.ldb + b_column(ch * EPC)) * ES) + b_matrix(ch * EPC);
         if constexpr (!ROWS_24) step_b = (uint32_t)((512 / CPRN) * (int)args.ldb * ES);
       }
     }
@@ -1060,13 +1070,21 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
     // would alias the next row and is sent out of range (an offset at OOB stays there when a step is added).
     const int k_a = (int)((lane & 7) ^ (((w4 * 8 + (lane >> 3)) / C::RPP) % C::VM)) * EPC;
     const int k_b = (int)((lane & 7) ^ (((w4 * 8 + (lane >> 3)) / C::RPP) % C::VN)) * EPC;
-    struct Offsets { uint32_t at[3]; };
+    constexpr bool DUAL_ROWS = F::DUAL && C::BSRC == B_NC;     // k rows beyond K lie inside the descriptor, which ends with the second matrix
+    struct Offsets { uint32_t at[DUAL_ROWS ? 4 : 3]; };
     auto offsets_a = [&](int t) {
       if constexpr (C::ASRC != A_KC) return Offsets{{va[0], va[1], 0}};
       const bool in = k_a < Kx - t * BK;
       return Offsets{{in ? va[0] : OOB, in ? va[1] : OOB, 0}};
     };
     auto offsets_b = [&](int t) {
+      if constexpr (DUAL_ROWS) {
+        const int left = Kx - t * BK - ((half_b * (NBR * 256) + w4 * 64 + lane) / (BN * ES / 16));
+        Offsets o;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.at[i] = left > 8 * i ? vb[i & 1] + (uint32_t)(i >> 1) * step_b : OOB;
+        return o;
+      }
       if constexpr (C::BSRC != B_KC) return Offsets{{vb[0], vb[1], vb[VB - 1]}};
       const bool in = k_b < Kx - t * BK;
       return Offsets{{in ? vb[0] : OOB, in ? vb[1] : OOB, 0}};
@@ -1075,7 +1093,7 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
       load_to_lds(r, stage + (half_a * 16 + i * 4 + w4) * 1024, o.at[i & 1] + (uint32_t)(i >> 1) * step_a);
     };
     auto load_b = [&](const __amdgpu_buffer_rsrc_t& r, const Offsets& o, GENSOR_LDS char* stage, int i) {
-      load_to_lds(r, stage + (half_b * (NBR * 4) + i * 4 + w4) * 1024, ROWS_24 ? o.at[i] : o.at[i & 1] + (uint32_t)(i >> 1) * step_b);
+      load_to_lds(r, stage + (half_b * (NBR * 4) + i * 4 + w4) * 1024, ROWS_24 || DUAL_ROWS ? o.at[i] : o.at[i & 1] + (uint32_t)(i >> 1) * step_b);
     };
     auto request_a = [&](int t) {
       const __amdgpu_buffer_rsrc_t r = rsrc_a(t * BK);
@@ -1283,9 +1301,9 @@ __global__ __launch_bounds__(C::THREADS) void contraction_kernel(const typename 
       if (again) {
         tile_of(args, xcd_contiguous(turn, total), tile_m, tile_n);
         m0 = tile_m * BM;
-        n0 = tile_n * BN;
+        n0 = tile_n * BNC;
         rows_valid = min(BM, args.M - m0);
-        cols_valid = min(BN, args.N - n0);
+        cols_valid = min(BNC, args.N - n0);
         a_tile = Ab + (C::ASRC == A_KC ? (int64_t)m0 * args.lda : (int64_t)m0) * ES;
         b_tile = Bb + (C::BSRC == B_KC ? (int64_t)n0 * args.ldb : (int64_t)n0) * ES;
         first_requests();

@@ -10,37 +10,16 @@
 #include <mutex>
 #include <vector>
 
-#include "../../include/gensor_fused.h"
-#include "fused_registry.hpp"
-#include "host_common.hpp"
+#include "fused_host.hpp"
 
 using namespace gensor;
 
 namespace {
 
-bool valid_dtype(int d) { return d == GENSOR_F32 || d == GENSOR_F16 || d == GENSOR_BF16; }
-int size_of(int d) { return d == GENSOR_F32 ? 4 : 2; }
-bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-GemmView product_view(int in_dtype, int out_dtype, int64_t M, int64_t N, int64_t K, int asrc, int bsrc, int64_t batch = 1) {
-  GemmView v;
-  std::memset(&v, 0, sizeof(v));
-  v.M = M; v.N = N; v.K = K; v.batch = batch;
-  v.in_dtype = in_dtype; v.out_dtype = out_dtype; v.esize = size_of(in_dtype); v.osize = size_of(out_dtype);
-  v.asrc = asrc; v.bsrc = bsrc;
-  return v;
-}
-
 // ------------------------------------------------------------------------------------
 // The tile: the cheapest by the cost model of those that exist with this end, reach the operands' rows and fit the room for partial
 // tiles.  Remembered per shape.
 // ------------------------------------------------------------------------------------
-struct FusedChoice {
-  const FusedDesc* f;
-  int split;
-  size_t bytes;
-  double us;
-};
 std::mutex g_choice_mutex;
 std::map<std::array<int64_t, 14>, std::vector<FusedChoice>> g_choices;
 const size_t kChoiceLimit = 4096;
@@ -72,7 +51,9 @@ bool tiles_fit(const InstanceDesc& d, const GemmView& v, int kind) {
   return launch_fits(tiles + 16 * gensor_hw_mi355x()->compute_units, d.threads);
 }
 
-gensor_status choose(const GemmView& v, int kind, bool vec_ok, const LeadingDims& ld, size_t room, FusedChoice* out) {
+}  // namespace
+
+gensor_status gensor::choose(const GemmView& v, int kind, bool vec_ok, const LeadingDims& ld, size_t room, FusedChoice* out) {
   const std::array<int64_t, 14> key = {kind, v.in_dtype, v.out_dtype, v.asrc, v.bsrc, vec_ok, v.M, v.N, v.K, v.batch, ld.a, ld.b, ld.c, 0};
   std::lock_guard<std::mutex> lock(g_choice_mutex);
   auto it = g_choices.find(key);
@@ -103,50 +84,7 @@ gensor_status choose(const GemmView& v, int kind, bool vec_ok, const LeadingDims
   return GENSOR_ERR_UNSUPPORTED;
 }
 
-// `panel`: tile rows that are walked together, column by column (L2 reuse).
-void tiles_of(FusedArgs* a, const GemmView& v, const FusedChoice& c, int64_t M, int64_t N, int panel = 4) {
-  const InstanceDesc& d = c.f->d;
-  a->tiles_m = (int32_t)((M + d.bm - 1) / d.bm);
-  const int bn = a->narrow ? 192 : d.bn;
-  a->tiles_n = (int32_t)((N + bn - 1) / bn);
-  a->batch = (int32_t)v.batch;
-  a->panel = std::min(panel, std::max(1, a->tiles_m));
-  a->lds_stages = d.stages;
-}
-
-// The part of the arguments that every product shares.  C's rows are stored past the caches unless a large output's rows do
-// not start on cache lines (as gensor_gemm does).
-FusedArgs product_args(const GemmView& v, const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, float alpha) {
-  FusedArgs a;
-  std::memset(&a, 0, sizeof(a));
-  a.A = A; a.B = B; a.C = C;
-  a.M = (int32_t)v.M; a.N = (int32_t)v.N; a.K = (int32_t)v.K;
-  a.lda = lda; a.ldb = ldb; a.ldc = ldc;
-  a.alpha = alpha;
-  a.store_m = a.M; a.store_n = a.N;
-  a.split = 1;
-  const int64_t c_bytes = v.batch * v.M * v.N * v.osize;
-  a.through = !((ldc * v.osize) % 128 != 0 && c_bytes > (v.osize == 2 ? 32ll : 64ll) * 1024 * 1024);
-  return a;
-}
-
-// Are the columns 2j and 2j + 1 of a 16-bit matrix one aligned dword?
-bool pairs(const void* p, int64_t ld, int64_t N, int osize) { return osize == 2 && N % 2 == 0 && ld % 2 == 0 && aligned(p, 4); }
-
-// Nothing leaves a C entry as an exception (the host's containers may run out of memory).
-template <typename F>
-gensor_status guarded(F&& body) {
-  try {
-    return body();
-  } catch (...) {
-    return GENSOR_ERR_DEVICE;
-  }
-}
-
-// The kernels number rows and columns to the end of the last tile in 32 bits.
-bool extents_fit(const GemmView& v) { return v.M <= INT32_MAX - 256 && v.N <= INT32_MAX - 256 && v.K <= INT32_MAX - 256; }
-
-gensor_status launched(hipError_t e) { return e == hipSuccess ? GENSOR_OK : GENSOR_ERR_DEVICE; }
+namespace {
 
 template <typename T, typename OutT>
 hipError_t launch_reduce(const FusedArgs& a, const InstanceDesc& d, unsigned blocks, hipStream_t st) {
@@ -173,8 +111,6 @@ gensor_status run_linear(FusedArgs& a, const GemmView& v, const FusedChoice& c, 
   else e = v.osize == 4 ? launch_reduce<bf16_t, f32_t>(a, d, n, st) : launch_reduce<bf16_t, bf16_t>(a, d, n, st);
   return launched(e);
 }
-
-size_t usable_room(const void* workspace, size_t bytes) { return workspace && aligned(workspace, 256) ? bytes : 0; }
 
 // The epilogue's arguments against the product's extents.
 gensor_status check_epilogue(const gensor_epilogue* e, const GemmView& v, const void* C) {
@@ -601,13 +537,17 @@ __global__ __launch_bounds__(256) void xent_pad_kernel(const char* X, int64_t ld
 
 namespace {
 
-gensor_status check_xent(gensor_dtype dtype, int64_t T, int64_t V, int64_t D) {
+}  // namespace
+
+gensor_status gensor::check_xent(gensor_dtype dtype, int64_t T, int64_t V, int64_t D) {
   if (!valid_dtype(dtype) || T <= 0 || V <= 0 || D <= 0) return GENSOR_ERR_INVALID_ARG;
   if (T > INT32_MAX / 8 || V > INT32_MAX / 8 || D > INT32_MAX / 8) return GENSOR_ERR_UNSUPPORTED;
   return GENSOR_OK;
 }
 
-size_t round_up(size_t n, size_t to) { return (n + to - 1) / to * to; }
+GemmView gensor::prob_view(int dtype, int64_t rows, int64_t T, int64_t D) { return product_view(dtype, dtype, rows, T, D, A_KC, B_KC); }
+
+namespace {
 
 size_t lse_bytes(int64_t T, int64_t V, int wm) { return round_up((size_t)((V + wm - 1) / wm * T * 4), 256); }
 
@@ -642,7 +582,6 @@ double best_price(const GemmView& v, int kind, bool vec, size_t room) {
   return best;
 }
 
-GemmView prob_view(int dtype, int64_t rows, int64_t T, int64_t D) { return product_view(dtype, dtype, rows, T, D, A_KC, B_KC); }
 GemmView dw_view(int dtype, int64_t rows, int64_t pitch, int64_t D) { return product_view(dtype, dtype, rows, D, pitch, A_KC, B_NC); }
 GemmView dx_view(int dtype, int64_t rows, int64_t pitch, int64_t D, bool last) {
   return product_view(dtype, last ? dtype : (int)GENSOR_F32, pitch, D, rows, A_MC, B_NC);
@@ -828,14 +767,9 @@ extern "C" gensor_status gensor_xent_forward(gensor_dtype dtype, int64_t T, int6
   });
 }
 
-extern "C" gensor_status gensor_xent_backward(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, const void* X, int64_t ldx, const void* W, int64_t ldw,
-                                              const int64_t* targets, int64_t ignore_index, const float* lse, const float* dloss, void* dX,
-                                              int64_t lddx, void* dW, int64_t lddw, void* workspace, size_t workspace_bytes, void* hip_stream) {
-  return guarded([&]() -> gensor_status {
-  gensor_status st = check_xent(dtype, T, V, D);
-  if (st != GENSOR_OK) return st;
-  if (!X || !W || !targets || !lse || !dloss || (!dX && !dW) || ldx < D || ldw < D || (dX && lddx < D) || (dW && lddw < D) || !aligned(targets, 8))
-    return GENSOR_ERR_INVALID_ARG;
+gensor_status gensor::vocabulary_gradient(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                                          const VocabularyLoss& loss, void* dX, int64_t lddx, void* dW, int64_t lddw, void* workspace, size_t workspace_bytes, hipStream_t s) {
+  gensor_status st = GENSOR_OK;
   XentPlan pl;
   if (!plan_xent(dtype, T, V, D, usable_room(workspace, workspace_bytes), &pl)) return GENSOR_ERR_WORKSPACE;
   const int es = size_of(dtype);
@@ -845,7 +779,6 @@ extern "C" gensor_status gensor_xent_backward(gensor_dtype dtype, int64_t T, int
   float* sums = (float*)(padded + pl.pad_bytes);
   char* parts = (char*)sums + pl.sum_bytes;
   char* G = parts + pl.part_bytes;
-  hipStream_t s = (hipStream_t)hip_stream;
   const bool scaled = dtype != GENSOR_F32;
 
   // every product's tile is chosen before anything is launched
@@ -874,10 +807,7 @@ extern "C" gensor_status gensor_xent_backward(gensor_dtype dtype, int64_t T, int
       if (st != GENSOR_OK) return st;
     }
   }
-  if (scaled) {
-    hipLaunchKernelGGL(xent_scale_kernel, dim3(1), dim3(1024), 0, s, dloss, targets, ignore_index, (int)V, (int)T, scales);
-    if (hipGetLastError() != hipSuccess) return GENSOR_ERR_DEVICE;
-  }
+  if (loss.prepare(scaled ? scales : nullptr, s) != hipSuccess) return GENSOR_ERR_DEVICE;
   if (pl.pad && dW) {
     // (a launch has fewer than 2^32 threads along an axis, and the rest is cut off without an error)
     const unsigned blocks = (unsigned)std::min<int64_t>((pl.pitch * D + 255) / 256, 1 << 20);
@@ -894,15 +824,11 @@ extern "C" gensor_status gensor_xent_backward(gensor_dtype dtype, int64_t T, int
       a.store_n = (int32_t)pl.pitch;
       a.paired = es == 2;
       a.scale = scaled ? scales : nullptr;
-      a.targets = targets;
-      a.ignore = ignore_index;
-      a.lse = lse;
-      a.dloss = dloss;
       a.tokens = (int32_t)T;
       a.row_first = (int32_t)q.first;
       a.vocab = (int32_t)V;
       tiles_of(&a, q.vp, q.cp, q.rows, pl.pitch);
-      if (q.cp.f->launch[FUSED_PROB](a, s) != hipSuccess) return GENSOR_ERR_DEVICE;
+      if (loss.piece(a, *q.cp.f, s) != hipSuccess) return GENSOR_ERR_DEVICE;
     }
     if (dW) {
       char* dWp = (char*)dW + q.first * lddw * es;
@@ -931,5 +857,29 @@ extern "C" gensor_status gensor_xent_backward(gensor_dtype dtype, int64_t T, int
     }
   }
   return GENSOR_OK;
+}
+
+extern "C" gensor_status gensor_xent_backward(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, const void* X, int64_t ldx, const void* W, int64_t ldw,
+                                              const int64_t* targets, int64_t ignore_index, const float* lse, const float* dloss, void* dX,
+                                              int64_t lddx, void* dW, int64_t lddw, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return guarded([&]() -> gensor_status {
+  gensor_status st = check_xent(dtype, T, V, D);
+  if (st != GENSOR_OK) return st;
+  if (!X || !W || !targets || !lse || !dloss || (!dX && !dW) || ldx < D || ldw < D || (dX && lddx < D) || (dW && lddw < D) || !aligned(targets, 8))
+    return GENSOR_ERR_INVALID_ARG;
+  VocabularyLoss loss;
+  loss.prepare = [&](float* scales, hipStream_t s) {
+    if (!scales) return hipSuccess;
+    hipLaunchKernelGGL(xent_scale_kernel, dim3(1), dim3(1024), 0, s, dloss, targets, ignore_index, (int)V, (int)T, scales);
+    return hipGetLastError();
+  };
+  loss.piece = [&](FusedArgs& a, const FusedDesc& tile, hipStream_t s) {
+    a.targets = targets;
+    a.ignore = ignore_index;
+    a.lse = lse;
+    a.dloss = dloss;
+    return tile.launch[FUSED_PROB](a, s);
+  };
+  return vocabulary_gradient(dtype, T, V, D, X, ldx, W, ldw, loss, dX, lddx, dW, lddw, workspace, workspace_bytes, (hipStream_t)hip_stream);
   });
 }

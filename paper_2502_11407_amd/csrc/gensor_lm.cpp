@@ -1,0 +1,792 @@
+// C ABI of the gated layers, the scores of a vocabulary and learning from a teacher (gensor_lm.h).  Argument validation, the choice of the
+// tiles, the launches and the small kernels between the products.  No device memory is allocated here.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <array>
+#include <cmath>
+#include <cstring>
+#include <map>
+#include <mutex>
+#include <vector>
+
+#include "../../include/gensor_lm.h"
+#include "fused_host.hpp"
+#include "lm_registry.hpp"
+
+using namespace gensor;
+
+// ------------------------------------------------------------------------------------ gated layers
+namespace {
+
+std::mutex g_gated_mutex;
+std::map<std::array<int64_t, 13>, const GatedDesc*> g_gated_choices;
+const size_t kGatedLimit = 4096;
+
+// The cheapest tile of two products at once: priced as one product of twice the columns.
+gensor_status choose_gated(const GemmView& v, bool vec_ok, const LeadingDims& ld, int64_t strideB, const GatedDesc** out) {
+  const std::array<int64_t, 13> key = {v.in_dtype, v.out_dtype, v.bsrc, vec_ok, v.M, v.N, v.K, ld.a, ld.b, ld.c, strideB, 0, 0};
+  std::lock_guard<std::mutex> lock(g_gated_mutex);
+  auto it = g_gated_choices.find(key);
+  if (it == g_gated_choices.end()) {
+    GemmView both = v;
+    both.N = 2 * v.N;
+    const GatedDesc* best = nullptr;
+    double best_us = 1e30;
+    for (int i = 0; i < g_num_gated; ++i) {
+      const InstanceDesc& d = g_gated[i].d;
+      if (!instance_serves(d, v) || (d.vec && !vec_ok) || !offsets_fit(d, v, ld)) continue;
+      if (d.direct && !d.any_k() && v.K % d.bk != 0) continue;
+      // the second matrix is reached from the first one's base
+      const double reach = v.bsrc == B_KC ? (double)(d.bn + 1) * (double)ld.b : (double)(d.bk + 1) * (double)ld.b + d.bn;
+      if (((double)strideB + reach) * v.esize >= 2147483647.0) continue;
+      const double tiles = (double)((v.M + d.bm - 1) / d.bm) * (double)((2 * v.N + d.bn - 1) / d.bn);
+      if (!launch_fits(tiles, d.threads)) continue;
+      const double us = fused_price(d, both, 1);
+      if (us > 0 && us < best_us) { best_us = us; best = &g_gated[i]; }
+    }
+    if (g_gated_choices.size() >= kGatedLimit) g_gated_choices.clear();
+    it = g_gated_choices.emplace(key, best).first;
+  }
+  *out = it->second;
+  return *out ? GENSOR_OK : GENSOR_ERR_UNSUPPORTED;
+}
+
+template <typename Args>
+Args end_args(const GemmView& v, const void* A, int64_t lda, const void* B, int64_t ldb, void* C, int64_t ldc, float alpha, const InstanceDesc& d, int columns, int panel) {
+  Args a;
+  std::memset(&a, 0, sizeof(a));
+  a.A = A; a.B = B; a.C = C;
+  a.M = (int32_t)v.M; a.N = (int32_t)v.N; a.K = (int32_t)v.K;
+  a.lda = lda; a.ldb = ldb; a.ldc = ldc;
+  a.alpha = alpha;
+  a.split = 1;
+  a.tiles_m = (int32_t)((v.M + d.bm - 1) / d.bm);
+  a.tiles_n = (int32_t)((v.N + columns - 1) / columns);
+  a.batch = 1;
+  a.panel = std::min(panel, std::max(1, a.tiles_m));
+  a.lds_stages = d.stages;
+  return a;
+}
+
+// Do two matrices of M x N, `apart` elements from one another, not overlap: one behind the other, or side by side in the same rows?
+bool disjoint(int64_t M, int64_t N, int64_t ld, int64_t apart) {
+  if (apart >= N && ld - apart >= N) return true;
+  return (double)apart >= (double)(M - 1) * (double)ld + (double)N;
+}
+
+bool two_pairs(const void* p, int64_t ld, int64_t apart, int64_t N, int osize) { return pairs(p, ld, N, osize) && apart % 2 == 0; }
+
+// Outputs whose rows do not start on cache lines go back through the caches where they are large, as gensor_gemm's do.
+bool stored_through(int64_t M, int64_t N, int64_t ld, int osize) {
+  return !((ld * osize) % 128 != 0 && M * N * osize > (osize == 2 ? 32ll : 64ll) * 1024 * 1024);
+}
+
+gensor_status gated_view(const gensor_problem* p, int32_t act, GemmView* v) {
+  if (!p || p->op != GENSOR_OP_GEMM || p->transA != 0 || act < GENSOR_ACT_NONE || act > GENSOR_ACT_SILU) return GENSOR_ERR_INVALID_ARG;
+  const gensor_status st = gemm_view(p, v);
+  if (st != GENSOR_OK) return st;
+  return v->N > (INT32_MAX - 256) / 2 || !extents_fit(*v) ? GENSOR_ERR_UNSUPPORTED : GENSOR_OK;
+}
+
+}  // namespace
+
+extern "C" gensor_status gensor_gated_gemm(const gensor_problem* p, int32_t act, float alpha, const void* A, int64_t lda, const void* B, int64_t ldb, int64_t strideB,
+                                           const void* bias, void* C, int64_t ldc, void* preact, int64_t ld_preact, int64_t stride_preact, void* hip_stream) {
+  return guarded([&]() -> gensor_status {
+  GemmView v;
+  gensor_status st = gated_view(p, act, &v);
+  if (st != GENSOR_OK) return st;
+  if (!A || !B || !C || lda < v.K || ldb < (v.bsrc == B_KC ? v.K : v.N) || ldc < v.N || strideB < 0) return GENSOR_ERR_INVALID_ARG;
+  if (preact && (ld_preact < v.N || !disjoint(v.M, v.N, ld_preact, stride_preact) || preact == C || (char*)preact + stride_preact * v.osize == C)) return GENSOR_ERR_INVALID_ARG;
+  const LeadingDims ld = {lda, ldb, preact ? std::max(ldc, ld_preact) : ldc};
+  const GatedDesc* g;
+  st = choose_gated(v, vector_ok(v, A, lda, 0, B, ldb, strideB), ld, strideB, &g);
+  if (st == GENSOR_ERR_UNSUPPORTED && v.M >= 1 << 20) {
+    // more tiles than a launch can have: the rows in two halves
+    gensor_problem half = *p;
+    half.M = (v.M / 2 + 255) / 256 * 256;
+    // (G and U of a half are as far apart as those of the whole: whether they overlap has been checked)
+    st = gensor_gated_gemm(&half, act, alpha, A, lda, B, ldb, strideB, bias, C, ldc, preact, ld_preact, stride_preact, hip_stream);
+    if (st != GENSOR_OK) return st;
+    const char* A2 = (const char*)A + half.M * lda * v.esize;
+    char* C2 = (char*)C + half.M * ldc * v.osize;
+    char* Z2 = preact ? (char*)preact + half.M * ld_preact * v.osize : nullptr;
+    half.M = v.M - half.M;
+    return gensor_gated_gemm(&half, act, alpha, A2, lda, B, ldb, strideB, bias, C2, ldc, Z2, ld_preact, stride_preact, hip_stream);
+  }
+  if (st != GENSOR_OK) return st;
+  GatedArgs a = end_args<GatedArgs>(v, A, lda, B, ldb, C, ldc, alpha, g->d, g->d.bn / 2, 4);
+  a.strideB = strideB;
+  a.act = act;
+  a.bias = bias;
+  a.preact = preact;
+  a.ld_preact = ld_preact;
+  a.far_preact = stride_preact;
+  a.paired = pairs(C, ldc, v.N, v.osize) && (!preact || two_pairs(preact, ld_preact, stride_preact, v.N, v.osize));
+  a.through = stored_through(v.M, v.N, ldc, v.osize) && (!preact || stored_through(v.M, v.N, ld_preact, v.osize));
+  return launched(g->launch(a, (hipStream_t)hip_stream));
+  });
+}
+
+extern "C" gensor_status gensor_gated_act_grad(const gensor_problem* p, int32_t act, float alpha, const void* A, int64_t lda, const void* B, int64_t ldb,
+                                               const void* preact, int64_t ld_preact, int64_t stride_preact, void* dpreact, int64_t ld_dpreact,
+                                               int64_t stride_dpreact, void* H, int64_t ldh, void* hip_stream) {
+  return guarded([&]() -> gensor_status {
+  GemmView v;
+  gensor_status st = gated_view(p, act, &v);
+  if (st != GENSOR_OK) return st;
+  if (!A || !B || !preact || !dpreact || lda < v.K || ldb < (v.bsrc == B_KC ? v.K : v.N) || (H && ldh < v.N)) return GENSOR_ERR_INVALID_ARG;
+  if (ld_preact < v.N || ld_dpreact < v.N || !disjoint(v.M, v.N, ld_preact, stride_preact) || !disjoint(v.M, v.N, ld_dpreact, stride_dpreact)) return GENSOR_ERR_INVALID_ARG;
+  const char *g0 = (const char*)preact, *u0 = g0 + stride_preact * v.osize, *dg0 = (const char*)dpreact, *du0 = dg0 + stride_dpreact * v.osize;
+  if (g0 == dg0 && (ld_preact != ld_dpreact || stride_preact != stride_dpreact)) return GENSOR_ERR_INVALID_ARG;
+  if (g0 == du0 || u0 == dg0 || (H && (H == g0 || H == u0 || H == dg0 || H == du0))) return GENSOR_ERR_INVALID_ARG;
+  const LeadingDims ld = {lda, ldb, std::max({ld_preact, ld_dpreact, H ? ldh : (int64_t)0})};
+  FusedChoice c;
+  st = choose(v, FUSED_LINEAR, vector_ok(v, A, lda, 0, B, ldb, 0), ld, 0, &c);
+  if (st == GENSOR_ERR_UNSUPPORTED && v.M >= 1 << 20) {
+    gensor_problem half = *p;
+    half.M = (v.M / 2 + 255) / 256 * 256;
+    st = gensor_gated_act_grad(&half, act, alpha, A, lda, B, ldb, preact, ld_preact, stride_preact, dpreact, ld_dpreact, stride_dpreact, H, ldh, hip_stream);
+    if (st != GENSOR_OK) return st;
+    const int64_t h = half.M;
+    half.M = v.M - h;
+    return gensor_gated_act_grad(&half, act, alpha, (const char*)A + h * lda * v.esize, lda, B, ldb, g0 + h * ld_preact * v.osize, ld_preact, stride_preact,
+                                 (char*)dpreact + h * ld_dpreact * v.osize, ld_dpreact, stride_dpreact, H ? (char*)H + h * ldh * v.osize : nullptr, ldh, hip_stream);
+  }
+  if (st != GENSOR_OK) return st;
+  GatedArgs a = end_args<GatedArgs>(v, A, lda, B, ldb, H, ldh, alpha, c.f->d, c.f->d.bn, 2);
+  a.act = act;
+  a.preact = (void*)preact;
+  a.ld_preact = ld_preact;
+  a.far_preact = stride_preact;
+  a.dpreact = dpreact;
+  a.ld_dpreact = ld_dpreact;
+  a.far_dpreact = stride_dpreact;
+  a.paired = two_pairs(preact, ld_preact, stride_preact, v.N, v.osize) && two_pairs(dpreact, ld_dpreact, stride_dpreact, v.N, v.osize) && (!H || pairs(H, ldh, v.N, v.osize));
+  a.through = stored_through(v.M, v.N, ld_dpreact, v.osize) && (!H || stored_through(v.M, v.N, ldh, v.osize));
+  return launched(g_lm_ends[c.f - g_fused].gated_grad(a, (hipStream_t)hip_stream));
+  });
+}
+
+// ------------------------------------------------------------------------------------ scores of a vocabulary
+namespace gensor {
+
+// Sums of exponentials relative to a maximum, and weighted with the exponents: joined with another part's (join_sums).  A part without terms has the
+// maximum -inf and the sums 0.
+__device__ inline void join_scores(float& top, float& sum, float& rest, float top2, float sum2, float rest2) {
+  constexpr float log2e = 1.44269504088896340736f;
+  const float both = fmaxf(top, top2), r = lse_reference(both);
+  const float d1 = fabsf(top) == INFINITY ? 0.f : top - r, d2 = fabsf(top2) == INFINITY ? 0.f : top2 - r;
+  const float f1 = __builtin_amdgcn_exp2f(log2e * d1), f2 = __builtin_amdgcn_exp2f(log2e * d2);
+  // (terms that vanish beside the larger maximum: the distance itself may be infinite)
+  rest = (f1 > 0.f ? f1 * fmaf(sum, d1, rest) : 0.f) + (f2 > 0.f ? f2 * fmaf(sum2, d2, rest2) : 0.f);
+  sum = sum * f1 + sum2 * f2;
+  top = both;
+}
+
+struct AdvanceArgs {
+  const f32x4* parts;              // of this piece
+  const float* set_max;
+  const float* logits;
+  int32_t slabs, slab_pitch, sets, set_pitch, set_size;
+  int32_t tokens, row_first, vocab, top, first, last;
+  f32x4* state;                    // [tokens]: joined so far
+  float* bar;                      // [tokens]: a later logit is among the largest only above it
+  float* values;                   // [tokens][top]: the largest logits so far; log probabilities in the end
+  int64_t* index;
+  const int64_t* targets;
+  int64_t ignore;
+  const float* at_target;
+  float *logprob, *lse, *entropy;
+};
+
+// The list of the largest, a lane each, in order; lane 0 the largest.  Entry NONE stands where there is none yet.
+struct TopList {
+  static constexpr int NONE = 0x7fffffff;
+  float value;
+  int entry;
+  __device__ static bool above(float v, int e, float v2, int e2) { return v > v2 || (v == v2 && e < e2); }
+  // puts (v, e), the same in all lanes, where it belongs
+  __device__ void insert(float v, int e) {
+    const int lane = threadIdx.x & 63;
+    const int at = __popcll(__ballot(above(value, entry, v, e)));
+    const float value_before = __shfl_up(value, 1, 64);
+    const int entry_before = __shfl_up(entry, 1, 64);
+    if (lane == at) { value = v; entry = e; }
+    else if (lane > at) { value = value_before; entry = entry_before; }
+  }
+  // every lane offers one; `n` of the list count.  (Which of them are above the n'th is known to all lanes; those are put in one by one.)
+  __device__ void offer(float v, int e, bool there, int n) {
+    // (all lanes ask for the n'th: a lane that is switched off has no value to give)
+    const bool is_above = above(v, e, __shfl(value, n - 1, 64), __shfl(entry, n - 1, 64));
+    uint64_t wanted = __ballot(there && is_above);
+    while (wanted) {
+      const int l = __builtin_ctzll(wanted);
+      insert(__shfl(v, l, 64), __shfl(e, l, 64));
+      const bool still = above(v, e, __shfl(value, n - 1, 64), __shfl(entry, n - 1, 64));
+      wanted &= (wanted - 1) & __ballot(still);
+    }
+  }
+};
+
+// A wave per token: joins a piece's parts to what was joined before, and finds the largest logits among the piece's and those so far.  The `top` largest
+// lie in the `top` sets with the largest maxima (equal maxima: those of lower entries): a set that is not one of them has that many larger ones, or
+// equal ones in front of it.
+__global__ __launch_bounds__(256) void advance_kernel(const AdvanceArgs a) {
+  const int lane = threadIdx.x & 63;
+  for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < a.tokens; t += gridDim.x * 4) {
+    float top = -INFINITY, sum = 0.f, rest = 0.f;
+    for (int s = lane; s < a.slabs; s += 4 * 64) {
+      f32x4 p[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) p[u] = s + 64 * u < a.slabs ? a.parts[(int64_t)t * a.slab_pitch + s + 64 * u] : f32x4{-INFINITY, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) join_scores(top, sum, rest, p[u][0], p[u][1], p[u][2]);
+    }
+#pragma unroll
+    for (int d = 32; d >= 1; d /= 2) {
+      const float t2 = __shfl_xor(top, d, 64), s2 = __shfl_xor(sum, d, 64), r2 = __shfl_xor(rest, d, 64);
+      // (the same order in both lanes: the same bits)
+      if (lane & d) {
+        float x = t2, y = s2, z = r2;
+        join_scores(x, y, z, top, sum, rest);
+        top = x; sum = y; rest = z;
+      } else {
+        join_scores(top, sum, rest, t2, s2, r2);
+      }
+    }
+    if (!a.first) {
+      const f32x4 so_far = a.state[t];
+      float x = so_far[0], y = so_far[1], z = so_far[2];
+      join_scores(x, y, z, top, sum, rest);
+      top = x; sum = y; rest = z;
+    }
+    if (!a.last && lane == 0) a.state[t] = f32x4{top, sum, rest, 0.f};
+    const float ref = lse_reference(top), log_sum = logf(sum);
+    if (a.last && lane == 0) {
+      if (a.lse) a.lse[t] = ref + log_sum;
+      if (a.entropy) a.entropy[t] = log_sum - rest / sum;
+      if (a.logprob) {
+        const int64_t target = a.targets[t];
+        // (the maximum's part first: a target that is the maximum loses log(1 + the others), not a difference of large numbers)
+        a.logprob[t] = target == a.ignore ? 0.f : target >= 0 && target < a.vocab ? (a.at_target[t] - ref) - log_sum : NAN;
+      }
+    }
+    if (a.top == 0) continue;
+
+    const float bar = a.first ? NAN : a.bar[t];
+    TopList best_sets{-INFINITY, TopList::NONE};
+    for (int s = lane; s < (a.sets + 63) / 64 * 64; s += 4 * 64) {
+      float m[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) m[u] = s + 64 * u < a.sets ? a.set_max[(int64_t)t * a.set_pitch + s + 64 * u] : -INFINITY;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) best_sets.offer(m[u], s + 64 * u, s + 64 * u < a.sets && !(m[u] <= bar), a.top);
+    }
+    TopList best{-INFINITY, TopList::NONE};
+    if (!a.first && lane < a.top) {
+      const int64_t e = a.index[(int64_t)t * a.top + lane];
+      best.value = a.values[(int64_t)t * a.top + lane];
+      best.entry = e < 0 ? TopList::NONE : (int)e;
+    }
+    const int chosen = min(a.top, __popcll(__ballot(best_sets.entry != TopList::NONE)));
+    const int per = 64 / a.set_size;                                   // sets that the wave looks at together
+    for (int j = 0; j < chosen; j += 4 * per) {
+      float v[4];
+      int e[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int which = j + u * per + lane / a.set_size, set = __shfl(best_sets.entry, which & 63, 64);
+        const bool there = which < chosen;
+        const int entry = set * a.set_size + lane % a.set_size;
+        v[u] = there ? a.logits[((int64_t)set * a.tokens + t) * a.set_size + lane % a.set_size] : -INFINITY;
+        e[u] = there && entry < a.vocab - a.row_first ? a.row_first + entry : TopList::NONE;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) best.offer(v[u], e[u], e[u] != TopList::NONE, a.top);
+    }
+    const bool full = __shfl(best.entry, a.top - 1, 64) != TopList::NONE;
+    const float least = __shfl(best.value, a.top - 1, 64);
+    if (!a.last && lane == 0) a.bar[t] = full ? least : NAN;
+    if (lane < a.top) {
+      const bool none = best.entry == TopList::NONE;
+      a.index[(int64_t)t * a.top + lane] = none ? -1 : (int64_t)best.entry;
+      a.values[(int64_t)t * a.top + lane] = !a.last ? best.value : none ? NAN : (best.value - ref) - log_sum;
+    }
+  }
+}
+
+}  // namespace gensor
+
+namespace {
+
+// Logits of a piece at most, where the largest are asked for
+const size_t kScoreBytes = (size_t)256 << 20;
+
+struct ScorePlan {
+  int64_t slabs, sets;             // of a piece
+  size_t parts, maxima, logits;    // bytes
+  size_t total() const { return parts + maxima + logits; }
+};
+
+ScorePlan score_plan(const InstanceDesc& d, int64_t T, int64_t rows, int top) {
+  ScorePlan s;
+  const int set = score_set(d.wm);
+  s.slabs = (rows + d.wm - 1) / d.wm;
+  s.sets = top ? s.slabs * (d.wm / set) : 0;
+  s.parts = round_up((size_t)(s.slabs * T) * 16, 256);
+  s.maxima = round_up((size_t)(s.sets * T) * 4, 256);
+  s.logits = round_up((size_t)(s.sets * T) * set * 4, 256);
+  return s;
+}
+
+// [state][bar][logit of the target] in front of a piece's
+size_t score_head(int64_t T) { return round_up((size_t)T * 16, 256) + 2 * round_up((size_t)T * 4, 256); }
+
+// Vocabulary entries of a piece where the room does not limit it
+int64_t score_piece(const InstanceDesc& d, int64_t T, int64_t V, int top) {
+  if (top == 0) return V;
+  const int64_t most = std::max<int64_t>(1, (int64_t)(kScoreBytes / ((size_t)T * 4)) / d.bm) * d.bm;
+  return std::min(V, most);
+}
+
+gensor_status choose_score(int dtype, int64_t T, int64_t V, int64_t D, const void* W, int64_t ldw, const void* X, int64_t ldx, FusedChoice* c) {
+  const GemmView v = prob_view(dtype, V, T, D);
+  const LeadingDims ld = {ldw, ldx, 0};
+  return choose(v, FUSED_LSE, vector_ok(v, W, ldw, 0, X, ldx, 0), ld, 0, c);
+}
+
+size_t score_bytes(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, int top) {
+  const GemmView v = prob_view(dtype, V, T, D);
+  size_t most = 0;
+  for (int vec = 0; vec < 2; ++vec) {
+    FusedChoice c;
+    const LeadingDims ld = {D, D, 0};
+    if (choose(v, FUSED_LSE, vec != 0, ld, 0, &c) == GENSOR_OK) most = std::max(most, score_plan(c.f->d, T, score_piece(c.f->d, T, V, top), top).total());
+  }
+  // (rows so far apart that another tile serves them: a piece of any)
+  for (int i = 0; i < g_num_fused; ++i) {
+    const InstanceDesc& d = g_fused[i].d;
+    if (g_lm_ends[i].score && instance_serves(d, v)) most = std::max(most, score_plan(d, T, std::min<int64_t>(V, d.bm), top).total());
+  }
+  return score_head(T) + most;
+}
+
+struct ScoreOutputs {
+  float *logprob, *lse, *entropy;
+  int32_t top;
+  int64_t* top_index;
+  float* top_logprob;
+};
+
+gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, const void* X, int64_t ldx, const void* W, int64_t ldw, float scale,
+                         const int64_t* targets, int64_t ignore, const ScoreOutputs& out, void* workspace, size_t workspace_bytes, hipStream_t s) {
+  FusedChoice c;
+  gensor_status st = choose_score(dtype, T, V, D, W, ldw, X, ldx, &c);
+  if (st == GENSOR_ERR_UNSUPPORTED && T >= 1 << 20) {
+    // more tiles than a launch can have: the tokens in two halves
+    const int64_t half = (T / 2 + 255) / 256 * 256;
+    st = run_scores(dtype, half, V, D, X, ldx, W, ldw, scale, targets, ignore, out, workspace, workspace_bytes, s);
+    if (st != GENSOR_OK) return st;
+    auto behind = [&](float* p) { return p ? p + half : nullptr; };
+    const ScoreOutputs rest = {behind(out.logprob), behind(out.lse), behind(out.entropy), out.top, out.top ? out.top_index + half * out.top : nullptr,
+                               out.top ? out.top_logprob + half * out.top : nullptr};
+    return run_scores(dtype, T - half, V, D, (const char*)X + half * ldx * size_of(dtype), ldx, W, ldw, scale, targets ? targets + half : nullptr, ignore, rest,
+                      workspace, workspace_bytes, s);
+  }
+  if (st != GENSOR_OK) return st;
+  const InstanceDesc& d = c.f->d;
+  const size_t room = usable_room(workspace, workspace_bytes), head = score_head(T);
+  int64_t piece = score_piece(d, T, V, out.top);
+  while (head + score_plan(d, T, piece, out.top).total() > room) {
+    if (piece <= d.bm) return GENSOR_ERR_WORKSPACE;
+    piece = std::max<int64_t>(1, piece / 2 / d.bm) * d.bm;
+  }
+  const ScorePlan pl = score_plan(d, T, piece, out.top);
+  char* at = (char*)workspace;
+  f32x4* state = (f32x4*)at;
+  float* bar = (float*)(at + round_up((size_t)T * 16, 256));
+  float* at_target = (float*)((char*)bar + round_up((size_t)T * 4, 256));
+  f32x4* parts = (f32x4*)(at + head);
+  float* maxima = (float*)(at + head + pl.parts);
+  float* logits = (float*)(at + head + pl.parts + pl.maxima);
+  const unsigned blocks = (unsigned)std::min<int64_t>((T + 3) / 4, 1 << 20);
+  for (int64_t entry = 0; entry < V; entry += piece) {
+    const int64_t rows = std::min(piece, V - entry);
+    const bool first = entry == 0, last = entry + rows == V;
+    const GemmView q = prob_view(dtype, rows, T, D);
+    ScoreArgs a = end_args<ScoreArgs>(q, (const char*)W + entry * ldw * size_of(dtype), ldw, X, ldx, nullptr, 0, scale, d, d.bn, 4);
+    a.targets = out.logprob ? targets : nullptr;
+    a.ignore = ignore;
+    a.tokens = (int32_t)T;
+    a.row_first = (int32_t)entry;
+    a.vocab = (int32_t)V;
+    a.slabs = (int32_t)pl.slabs;
+    a.sets = (int32_t)pl.sets;
+    a.parts = parts;
+    a.set_max = maxima;
+    a.logits = logits;
+    a.bar = first ? nullptr : bar;
+    a.at_target = at_target;
+    if (g_lm_ends[c.f - g_fused].score(a, s) != hipSuccess) return GENSOR_ERR_DEVICE;
+    AdvanceArgs v;
+    std::memset(&v, 0, sizeof(v));
+    v.parts = parts;
+    v.set_max = maxima;
+    v.logits = logits;
+    v.slabs = (int32_t)((rows + d.wm - 1) / d.wm);
+    v.slab_pitch = a.slabs;
+    v.set_size = score_set(d.wm);
+    v.sets = out.top ? (int32_t)((rows + v.set_size - 1) / v.set_size) : 0;
+    v.set_pitch = a.sets;
+    v.tokens = (int32_t)T;
+    v.row_first = (int32_t)entry;
+    v.vocab = (int32_t)V;
+    v.top = out.top;
+    v.first = first;
+    v.last = last;
+    v.state = state;
+    v.bar = bar;
+    v.values = out.top_logprob;
+    v.index = out.top_index;
+    v.targets = targets;
+    v.ignore = ignore;
+    v.at_target = at_target;
+    v.logprob = out.logprob;
+    v.lse = out.lse;
+    v.entropy = out.entropy;
+    hipLaunchKernelGGL(advance_kernel, dim3(blocks), dim3(256), 0, s, v);
+    if (hipGetLastError() != hipSuccess) return GENSOR_ERR_DEVICE;
+  }
+  return GENSOR_OK;
+}
+
+bool valid_scale(float scale) { return scale > 0.f && std::isfinite(scale); }
+
+}  // namespace
+
+extern "C" size_t gensor_logprobs_workspace_bytes(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, int32_t top) {
+  size_t bytes = 0;
+  guarded([&]() -> gensor_status {
+    if (check_xent(dtype, T, V, D) == GENSOR_OK && top >= 0 && top <= GENSOR_TOP_MAX && top <= V) bytes = score_bytes(dtype, T, V, D, top);
+    return GENSOR_OK;
+  });
+  return bytes;
+}
+
+extern "C" gensor_status gensor_logprobs(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, const void* X, int64_t ldx, const void* W, int64_t ldw, float scale,
+                                         const int64_t* targets, int64_t ignore_index, float* logprob, float* lse, float* entropy, int32_t top, int64_t* top_index,
+                                         float* top_logprob, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return guarded([&]() -> gensor_status {
+  const gensor_status st = check_xent(dtype, T, V, D);
+  if (st != GENSOR_OK) return st;
+  if (!X || !W || ldx < D || ldw < D || !valid_scale(scale) || top < 0 || top > GENSOR_TOP_MAX || top > V) return GENSOR_ERR_INVALID_ARG;
+  if ((!logprob && !lse && !entropy && !top) || (logprob && !targets) || (targets && !aligned(targets, 8))) return GENSOR_ERR_INVALID_ARG;
+  if (top ? (!top_index || !top_logprob || !aligned(top_index, 8)) : (top_index || top_logprob)) return GENSOR_ERR_INVALID_ARG;
+  const ScoreOutputs out = {logprob, lse, entropy, top, top_index, top_logprob};
+  return run_scores(dtype, T, V, D, X, ldx, W, ldw, scale, targets, ignore_index, out, workspace, workspace_bytes, (hipStream_t)hip_stream);
+  });
+}
+
+// ------------------------------------------------------------------------------------ learning from a teacher
+namespace gensor {
+
+struct TeacherArgs {
+  const char* X;
+  const char* W;
+  int64_t ldx, ldw;
+  const int64_t* index;
+  const float* teacher;
+  const float* lse;
+  int32_t T, V, D, k, normalize;
+  float scale;
+  float* loss;                     // forward
+  const float* dloss;              // gradient
+  float* weights;                  // dloss * scale * P, zero for tokens that teach nothing
+  int32_t* entries;                // [T][k]: where G gets another value, or -1
+  float* values;                   // ... and that value
+};
+
+// A token's entries, probabilities and logits in LDS.
+struct TeacherEntries {
+  int entry[256];
+  float log_p[256], p[256], z[256];
+  float mass;
+  int bad;
+};
+
+// Fills them, all 256 threads of a workgroup: a wave takes four entries at a time, whose rows of W it reads side by side with the token's row of X.
+template <typename T, bool VEC>
+__device__ inline void teacher_entries(const TeacherArgs& a, int t, TeacherEntries& e) {
+  constexpr int ES = ElemSize<T>::value, EPC = 16 / ES;
+  const int i = threadIdx.x, lane = i & 63, wave = i >> 6;
+  __syncthreads();                                                   // (the token before)
+  if (i == 0) e.bad = 0;
+  __syncthreads();
+  if (i < a.k) {
+    const int64_t at = a.index[(int64_t)t * a.k + i];
+    const bool there = at >= 0 && at < a.V;
+    e.entry[i] = there ? (int)at : -1;
+    if (at < -1 || at >= a.V) e.bad = 1;                             // (any of the threads that find one)
+    e.log_p[i] = there ? a.teacher[(int64_t)t * a.k + i] : -INFINITY;
+  }
+  __syncthreads();
+  if (wave == 0) {
+    float shift = 0.f;
+    if (a.normalize) {
+      float top = -INFINITY, sum = 0.f;
+      for (int j = lane; j < a.k; j += 64) {
+        if (e.entry[j] >= 0) e.log_p[j] *= a.scale;
+        top = e.log_p[j] > top || e.log_p[j] != e.log_p[j] ? e.log_p[j] : top;
+      }
+      for (int d = 32; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+      if (top > -INFINITY)
+        for (int j = lane; j < a.k; j += 64) sum += expf(e.log_p[j] - top);
+      for (int d = 32; d >= 1; d /= 2) sum += __shfl_xor(sum, d, 64);
+      shift = top > -INFINITY ? top + logf(sum) : 0.f;
+    }
+    float mass = 0.f;
+    for (int j = lane; j < a.k; j += 64) {
+      const float q = e.log_p[j] - shift;
+      e.log_p[j] = q;
+      e.p[j] = expf(q);
+      mass += e.p[j];
+    }
+    for (int d = 32; d >= 1; d /= 2) mass += __shfl_xor(mass, d, 64);
+    if (lane == 0) e.mass = mass;
+  }
+  const char* x = a.X + (int64_t)t * a.ldx * ES;
+  for (int j = 4 * wave; j < a.k; j += 16) {
+    const char* w[4];
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) w[u] = a.W + (int64_t)(j + u < a.k ? max(e.entry[j + u], 0) : 0) * a.ldw * ES;
+    if constexpr (VEC) {
+      for (int c = lane * EPC; c < a.D; c += 64 * EPC) {
+        const u32x4 xv = *(const u32x4*)(x + (int64_t)c * ES);
+        u32x4 wv[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) wv[u] = *(const u32x4*)(w[u] + (int64_t)c * ES);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int n = 0; n < EPC; ++n) {
+            if constexpr (ES == 4) acc[u] = fmaf(as_f32(xv[n]), as_f32(wv[u][n]), acc[u]);
+            else acc[u] = fmaf(from_pair<T>(xv[n / 2], n & 1), from_pair<T>(wv[u][n / 2], n & 1), acc[u]);
+          }
+      }
+    } else {
+      for (int c = lane; c < a.D; c += 64) {
+        const float xv = to_float<T>(x, c);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) acc[u] = fmaf(xv, to_float<T>(w[u], c), acc[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      for (int d = 32; d >= 1; d /= 2) acc[u] += __shfl_xor(acc[u], d, 64);
+      if (lane == 0 && j + u < a.k) e.z[j + u] = a.scale * acc[u];
+    }
+  }
+  __syncthreads();
+}
+
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void teacher_loss_kernel(const TeacherArgs a) {
+  __shared__ TeacherEntries e;
+  for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
+    teacher_entries<T, VEC>(a, t, e);
+    if (threadIdx.x >= 64) continue;
+    const float lse = a.lse[t];
+    float loss = 0.f;
+    // (entries that are none and probabilities of zero by choice: their logarithms and logits may be infinite)
+    for (int j = threadIdx.x; j < a.k; j += 64) loss += e.p[j] == 0.f ? 0.f : e.p[j] * ((e.log_p[j] - e.z[j]) + lse);
+    for (int d = 32; d >= 1; d /= 2) loss += __shfl_xor(loss, d, 64);
+    if (threadIdx.x == 0) a.loss[t] = e.bad ? NAN : loss;
+  }
+}
+
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void teacher_weights_kernel(const TeacherArgs a) {
+  __shared__ TeacherEntries e;
+  for (int t = blockIdx.x; t < a.T; t += gridDim.x) {
+    teacher_entries<T, VEC>(a, t, e);
+    const float dloss = a.dloss[t] * a.scale;
+    const bool teaches = !e.bad && e.mass != 0.f && dloss != 0.f;
+    if (threadIdx.x == 0) a.weights[t] = teaches ? dloss * e.mass : 0.f;
+    const int j = threadIdx.x;
+    if (j < a.k) {
+      // an entry that is named again is the first one's business
+      const int at = e.entry[j];
+      bool mine = teaches && at >= 0;
+      float p = 0.f;
+      if (mine)
+        for (int i = 0; i < a.k; ++i)
+          if (e.entry[i] == at) {
+            if (i < j) mine = false;
+            p += e.p[i];
+          }
+      a.entries[(int64_t)t * a.k + j] = mine ? at : -1;
+      a.values[(int64_t)t * a.k + j] = mine ? dloss * (e.mass * expf(e.z[j] - a.lse[t]) - p) : 0.f;
+    }
+  }
+}
+
+// scale[0]: a power of two's worth of G, so that the largest weight becomes 2^15 (xent_scale_kernel says why); scale[1]: its inverse
+__global__ __launch_bounds__(1024) void teacher_scale_kernel(const float* weights, int tokens, float* scale) {
+  constexpr int UNROLL = 8;
+  __shared__ float tops[16];
+  float top = 0.f;
+  for (int first = threadIdx.x; first < tokens; first += UNROLL * 1024) {
+    float x[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) x[u] = first + u * 1024 < tokens ? fabsf(weights[first + u * 1024]) : 0.f;
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u)
+      if (x[u] < INFINITY) top = fmaxf(top, x[u]);
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int w = 1; w < 16; ++w) top = fmaxf(top, tops[w]);
+  const float f = top > 0.f ? fminf(fmaxf(32768.f / top, 0x1p-100f), 0x1p100f) : 1.f;
+  scale[0] = f;
+  scale[1] = 1.f / f;
+}
+
+// G of a piece at the teacher's entries
+template <typename T>
+__global__ __launch_bounds__(256) void teacher_place_kernel(const int32_t* entries, const float* values, const float* scale, int64_t n, int k, int row_first, int rows,
+                                                            char* G, int64_t pitch) {
+  const float f = scale ? *scale : 1.f;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int at = entries[i];
+    if (at >= row_first && at - row_first < rows) store_out<T>(G, (int64_t)(at - row_first) * pitch + i / k, values[i] * f);
+  }
+}
+
+}  // namespace gensor
+
+namespace {
+
+gensor_status check_teacher(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, int32_t k) {
+  const gensor_status st = check_xent(dtype, T, V, D);
+  if (st != GENSOR_OK) return st;
+  return k < 1 || k > GENSOR_TEACHER_MAX ? GENSOR_ERR_INVALID_ARG : GENSOR_OK;
+}
+
+template <typename F>
+hipError_t by_type(gensor_dtype dtype, F&& f) {
+  if (dtype == GENSOR_F32) return f(f32_t{});
+  return dtype == GENSOR_F16 ? f(f16_t{}) : f(bf16_t{});
+}
+
+TeacherArgs teacher_args(int64_t T, int64_t V, int64_t D, const void* X, int64_t ldx, const void* W, int64_t ldw, float scale, int32_t k, const int64_t* index,
+                         const float* teacher, int32_t normalize) {
+  TeacherArgs a;
+  std::memset(&a, 0, sizeof(a));
+  a.X = (const char*)X; a.W = (const char*)W;
+  a.ldx = ldx; a.ldw = ldw;
+  a.index = index; a.teacher = teacher;
+  a.T = (int32_t)T; a.V = (int32_t)V; a.D = (int32_t)D; a.k = k; a.normalize = normalize;
+  a.scale = scale;
+  return a;
+}
+
+bool whole_vectors(gensor_dtype dtype, int64_t D, const void* X, int64_t ldx, const void* W, int64_t ldw) {
+  const int epc = 16 / size_of(dtype);
+  return D % epc == 0 && ldx % epc == 0 && ldw % epc == 0 && aligned(X, 16) && aligned(W, 16);
+}
+
+unsigned token_blocks(int64_t T) { return (unsigned)std::min<int64_t>(T, 1 << 20); }
+
+size_t teacher_room(int64_t T, int32_t k) { return round_up((size_t)T * 4 + (size_t)T * k * 8, 256); }
+
+}  // namespace
+
+extern "C" size_t gensor_distill_workspace_bytes(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, int32_t k, int32_t backward) {
+  size_t bytes = 0;
+  guarded([&]() -> gensor_status {
+    if (check_teacher(dtype, T, V, D, k) != GENSOR_OK) return GENSOR_OK;
+    bytes = backward ? teacher_room(T, k) + gensor_xent_workspace_bytes(dtype, T, V, D, 1) : round_up((size_t)T * 4, 256) + score_bytes(dtype, T, V, D, 0);
+    return GENSOR_OK;
+  });
+  return bytes;
+}
+
+extern "C" gensor_status gensor_distill_forward(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, const void* X, int64_t ldx, const void* W, int64_t ldw, float scale,
+                                                int32_t k, const int64_t* index, const float* teacher, int32_t normalize, float* loss, float* lse, void* workspace,
+                                                size_t workspace_bytes, void* hip_stream) {
+  return guarded([&]() -> gensor_status {
+  gensor_status st = check_teacher(dtype, T, V, D, k);
+  if (st != GENSOR_OK) return st;
+  if (!X || !W || ldx < D || ldw < D || !valid_scale(scale) || !index || !aligned(index, 8) || !teacher || (normalize != 0 && normalize != 1) || (!loss && !lse))
+    return GENSOR_ERR_INVALID_ARG;
+  const size_t head = round_up((size_t)T * 4, 256), room = usable_room(workspace, workspace_bytes);
+  if (room < head) return GENSOR_ERR_WORKSPACE;
+  float* sums = lse ? lse : (float*)workspace;
+  hipStream_t s = (hipStream_t)hip_stream;
+  const ScoreOutputs out = {nullptr, sums, nullptr, 0, nullptr, nullptr};
+  st = run_scores(dtype, T, V, D, X, ldx, W, ldw, scale, nullptr, 0, out, (char*)workspace + head, room - head, s);
+  if (st != GENSOR_OK || !loss) return st;
+  TeacherArgs a = teacher_args(T, V, D, X, ldx, W, ldw, scale, k, index, teacher, normalize);
+  a.lse = sums;
+  a.loss = loss;
+  const bool vec = whole_vectors(dtype, D, X, ldx, W, ldw);
+  return launched(by_type(dtype, [&](auto type) {
+    typedef decltype(type) E;
+    if (vec) hipLaunchKernelGGL((teacher_loss_kernel<E, true>), dim3(token_blocks(T)), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((teacher_loss_kernel<E, false>), dim3(token_blocks(T)), dim3(256), 0, s, a);
+    return hipGetLastError();
+  }));
+  });
+}
+
+extern "C" gensor_status gensor_distill_backward(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, const void* X, int64_t ldx, const void* W, int64_t ldw, float scale,
+                                                 int32_t k, const int64_t* index, const float* teacher, int32_t normalize, const float* lse, const float* dloss,
+                                                 void* dX, int64_t lddx, void* dW, int64_t lddw, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  return guarded([&]() -> gensor_status {
+  const gensor_status st = check_teacher(dtype, T, V, D, k);
+  if (st != GENSOR_OK) return st;
+  if (!X || !W || ldx < D || ldw < D || !valid_scale(scale) || !index || !aligned(index, 8) || !teacher || (normalize != 0 && normalize != 1)) return GENSOR_ERR_INVALID_ARG;
+  if (!lse || !dloss || (!dX && !dW) || (dX && lddx < D) || (dW && lddw < D)) return GENSOR_ERR_INVALID_ARG;
+  const size_t head = teacher_room(T, k), room = usable_room(workspace, workspace_bytes);
+  if (room < head) return GENSOR_ERR_WORKSPACE;
+  TeacherArgs a = teacher_args(T, V, D, X, ldx, W, ldw, scale, k, index, teacher, normalize);
+  a.lse = lse;
+  a.dloss = dloss;
+  a.weights = (float*)workspace;
+  a.entries = (int32_t*)(a.weights + T);
+  a.values = (float*)(a.entries + T * k);
+  const bool vec = whole_vectors(dtype, D, X, ldx, W, ldw);
+  VocabularyLoss loss;
+  loss.prepare = [&](float* scales, hipStream_t s) {
+    const hipError_t e = by_type(dtype, [&](auto type) {
+      typedef decltype(type) E;
+      if (vec) hipLaunchKernelGGL((teacher_weights_kernel<E, true>), dim3(token_blocks(T)), dim3(256), 0, s, a);
+      else hipLaunchKernelGGL((teacher_weights_kernel<E, false>), dim3(token_blocks(T)), dim3(256), 0, s, a);
+      return hipGetLastError();
+    });
+    if (e != hipSuccess || !scales) return e;
+    hipLaunchKernelGGL(teacher_scale_kernel, dim3(1), dim3(1024), 0, s, a.weights, (int)T, scales);
+    return hipGetLastError();
+  };
+  loss.piece = [&](FusedArgs& f, const FusedDesc& tile, hipStream_t s) {
+    f.alpha = scale;
+    f.lse = lse;
+    f.dloss = a.weights;
+    const hipError_t e = g_lm_ends[&tile - g_fused].teach(f, s);
+    if (e != hipSuccess) return e;
+    const int64_t n = T * k;
+    return by_type(dtype, [&](auto type) {
+      hipLaunchKernelGGL((teacher_place_kernel<decltype(type)>), dim3((unsigned)std::min<int64_t>((n + 255) / 256, 1 << 20)), dim3(256), 0, s, a.entries, a.values, f.scale, n,
+                         (int)k, f.row_first, f.M, (char*)f.C, f.ldc);
+      return hipGetLastError();
+    });
+  };
+  return vocabulary_gradient(dtype, T, V, D, X, ldx, W, ldw, loss, dX, lddx, dW, lddw, (char*)workspace + head, room - head, (hipStream_t)hip_stream);
+  });
+}

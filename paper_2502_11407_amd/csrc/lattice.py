@@ -345,6 +345,30 @@ def fused():
     return out
 
 
+def lm_ends(d):
+    """What else a tile of fused() is compiled with (lm_kernel.hpp)."""
+    ends = ["score", "teach"] if "lse" in d["kinds"] else []
+    return ends + (["gated_grad"] if d["asrc"] == "KC" else [])
+
+
+def gated():
+    """The tiles of two products at once: a wave's columns are half of either, so two or more blocks side by side."""
+    tiles16 = [(256, 256, 64, 128, 64, 16, 1, 2, 1), (256, 128, 64, 64, 64, 16, 1, 3, 1), (128, 128, 64, 64, 32, 16, 1, 4, 1),
+               (64, 64, 64, 32, 32, 16, 1, 2, 0), (32, 64, 128, 16, 32, 16, 1, 2, 0),
+               (128, 128, 64, 64, 32, 16, 0, 2, 0), (64, 64, 64, 32, 32, 16, 0, 2, 0), (32, 64, 128, 16, 32, 16, 0, 2, 0)]
+    tiles32 = [(128, 128, 32, 64, 64, 32, 1, 2, 0), (64, 64, 32, 32, 32, 16, 1, 2, 0), (32, 64, 64, 16, 32, 16, 1, 2, 0),
+               (128, 128, 32, 64, 64, 32, 0, 2, 0), (64, 64, 32, 32, 32, 16, 0, 2, 0), (32, 64, 64, 16, 32, 16, 0, 2, 0)]
+    out = []
+    for dt in ("f16", "bf16", "f32"):
+        for (bm, bn, bk, wm, wn, mb, vec, stages, direct) in (tiles32 if dt == "f32" else tiles16):
+            for odt in ((dt,) if dt == "f32" else ("f32", dt)):
+                for bsrc in ("KC", "NC"):
+                    out.append(_inst(dt, odt, bm, bn, bk, wm, wn, mb, bsrc=bsrc, vec=vec, stages=stages, direct=direct))
+    for i, d in enumerate(out):
+        d["id"] = i
+    return out
+
+
 def cfg_type(d):
     if conv_rows(d):
         return "ConvRowsCfg<%s, %s, %d, %d, %d, %d>" % (CT[d["dt"]], CT[d["out"]], d["bm"], d["bn"], d["wm"], d["wn"])

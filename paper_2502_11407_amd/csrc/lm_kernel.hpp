@@ -1,0 +1,538 @@
+// Ends of the contraction kernel for a language model's gated layers, for the scores of a vocabulary and for learning from a teacher
+// (the F of contraction_kernel):
+//
+//   Gated      C = act(G) * U of the two products G = alpha A B0 + b0 and U = alpha A B1 + b1, which may be kept
+//   GatedGrad  of the gradient D = alpha A B of that C:  dG = D U act'(G),  dU = D act(G),  and C = act(G) U again
+//   Score      rows are vocabulary entries, columns tokens: each wave reduces its rows' logits to a maximum, a sum of exponentials and their
+//              sum weighted with the logits per token; where the largest entries are asked for, the maxima of sets of rows are left too, and the
+//              logits themselves of those sets that may hold one
+//   Teach      the same product again: C = scale * weight[token] * exp(logit - lse[token])
+#pragma once
+#include "fused_kernel.hpp"
+
+namespace gensor {
+
+struct GatedArgs : KernelArgs {
+  int32_t act;
+  const void* bias;                // [2][N] of the input type, or null
+  void* preact;                    // G, and U `far_preact` elements behind it: written, or null (GatedGrad: read)
+  int64_t ld_preact, far_preact;
+  void* dpreact;                   // GatedGrad: dG and dU
+  int64_t ld_dpreact, far_dpreact;
+};
+
+struct ScoreArgs : KernelArgs {
+  const int64_t* targets;
+  int64_t ignore;
+  int32_t tokens, row_first, vocab;        // row_first: vocabulary entry of row 0
+  int32_t slabs, sets;                     // of a token's row of `parts` and of `set_max` (0: the largest are not asked for)
+  f32x4* parts;                            // [token][slab of C::WM rows]: maximum, sum, weighted sum
+  float* set_max;                          // [token][set of rows]
+  float* logits;                           // [set][token][rows of a set]
+  const float* bar;                        // logits of sets whose maximum is not above a token's are not needed (NaN, or null: all are)
+  float* at_target;
+};
+
+// Rows of a set: as many as one set's logits, 128 bytes a token, fill of a line, of a wave's tile
+__host__ __device__ constexpr int score_set(int wm) { return wm < 32 ? wm : 32; }
+
+// ---------------------------------------------------------------- 16-bit values of MFMA blocks in whole dwords
+// A lane's registers are rows of one column, two bytes each in C.  Pairs of rows of a column are traded with the neighbour lane for pairs of
+// columns of a row, and of GB blocks side by side the lane groups' parts are gathered, so that a store writes runs of 32 GB bytes (blocks of
+// 16) or 64 GB (blocks of 32).  The exchange is its own inverse: what is read goes the same way backwards.  WIDTH: the columns of the wave's
+// part.  A pair of rows of GB blocks takes RS accesses, 4 rows apart.
+template <typename C, int WIDTH>
+struct Paired {
+  static constexpr int MB = C::MB, GB = WIDTH % 64 == 0 ? 64 / MB : WIDTH % 32 == 0 ? 32 / MB : 1, RS = GB;
+  static __device__ uint32_t trade(uint32_t own) {
+    const uint32_t other = (uint32_t)__builtin_amdgcn_mov_dpp((int)own, 0xB1, 0xF, 0xF, true);      // quad_perm [1,0,3,2]
+    return __builtin_amdgcn_perm(other, own, (threadIdx.x & 1) ? 0x03020706u : 0x05040100u);
+  }
+  static __device__ void swap16(uint32_t& x, uint32_t& y) {
+    const auto q = __builtin_amdgcn_permlane16_swap(x, y, false, false);
+    x = q[0]; y = q[1];
+  }
+  static __device__ void swap32(uint32_t& x, uint32_t& y) {
+    const auto q = __builtin_amdgcn_permlane32_swap(x, y, false, false);
+    x = q[0]; y = q[1];
+  }
+  // w[i]: block i's pair of rows -> access i's
+  static __device__ __attribute__((always_inline)) void gather(uint32_t (&w)[RS]) {
+    if constexpr (GB == 2 && MB == 32) swap32(w[0], w[1]);
+    else if constexpr (GB == 2) swap16(w[0], w[1]);
+    else if constexpr (GB == 4) {
+      swap16(w[0], w[1]);
+      swap16(w[2], w[3]);
+      swap32(w[0], w[2]);
+      swap32(w[1], w[3]);
+    }
+  }
+  static __device__ __attribute__((always_inline)) void scatter(uint32_t (&w)[RS]) {
+    if constexpr (GB == 2 && MB == 32) swap32(w[0], w[1]);
+    else if constexpr (GB == 2) swap16(w[0], w[1]);
+    else if constexpr (GB == 4) {
+      swap32(w[0], w[2]);
+      swap32(w[1], w[3]);
+      swap16(w[0], w[1]);
+      swap16(w[2], w[3]);
+    }
+  }
+  // first row (of the pair's row_of) and column of this lane's accesses
+  static __device__ int row(int lane) { return (lane & 1) + (GB == 1 ? 4 * (lane / MB) : GB * MB == 32 ? 8 * (lane >> 5) : 0); }
+  static __device__ int column(int lane) { return lane % (GB * MB) & ~1; }
+};
+
+template <typename C> static constexpr __device__ int block_row_of(int v) { return C::MB == 32 ? 8 * (v / 4) + v % 4 : v; }
+
+// A matrix beside C, seen from a tile.
+struct TileMatrix {
+  __amdgpu_buffer_rsrc_t r;
+  uint32_t pitch;
+  __device__ TileMatrix(const void* base, int64_t ld, int64_t row, int64_t col, int rows, int cols, int size)
+      : r(__builtin_amdgcn_make_buffer_rsrc((void*)(base ? (const char*)base + (row * ld + col) * size : nullptr), 0, base ? records(ld, rows, cols, size) : 0u, 0x00020000u)),
+        pitch((uint32_t)(ld * size)) {}
+  static __device__ uint32_t records(int64_t ld, int rows, int cols, int size) {
+    const int64_t bytes = ((int64_t)(rows - 1) * ld + cols) * size;
+    return bytes <= 0 ? 0u : bytes > 0x7fffffffll ? 0x7fffffffu : (uint32_t)bytes;
+  }
+};
+
+// One wave's blocks of a matrix beside C: MBLK x BLOCKS of them, the first column at `col` of the tile.
+template <typename C, int BLOCKS>
+struct WaveBlocks {
+  typedef typename C::OutT OutT;
+  static constexpr int OS = ElemSize<OutT>::value, MB = C::MB, NACC = MB * MB / 64, WIDTH = BLOCKS * MB;
+  typedef Paired<C, WIDTH> P;
+  static constexpr int GB = OS == 2 ? P::GB : 1, RS = OS == 2 ? P::RS : 1, HALVES = NACC / 2;
+  static constexpr uint32_t OOB = 0x80000000u;
+  int row0, col0, cols, lane;
+
+  // ---- pairs (16-bit types, rows of whole dwords): unit (bi, bj .. bj + GB - 1)
+  __device__ __attribute__((always_inline)) uint32_t at_pair(const TileMatrix& t, int bi, int bj) const {
+    const int c = col0 + bj * MB + P::column(lane);
+    return c < cols ? (uint32_t)(c * OS) + (uint32_t)(row0 + bi * MB + P::row(lane)) * t.pitch : OOB;
+  }
+  __device__ __attribute__((always_inline)) void request_pair(const TileMatrix& t, int bi, int bj, uint32_t (&in)[HALVES][RS]) const {
+    const uint32_t at = at_pair(t, bi, bj);
+#pragma unroll
+    for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+      for (int i = 0; i < RS; ++i) in[h][i] = __builtin_amdgcn_raw_buffer_load_b32(t.r, at + (uint32_t)(block_row_of<C>(2 * h) + 4 * i) * t.pitch, 0, 0);
+  }
+  __device__ __attribute__((always_inline)) void received_pair(const uint32_t (&in)[HALVES][RS], float (&x)[GB][NACC]) const {
+    if constexpr (OS == 2) {
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) {
+        uint32_t w[RS];
+#pragma unroll
+        for (int i = 0; i < RS; ++i) w[i] = in[h][i];
+        P::scatter(w);
+#pragma unroll
+        for (int g = 0; g < GB; ++g) {
+          const uint32_t t = P::trade(w[g]);
+          x[g][2 * h] = from_pair<OutT>(t, 0);
+          x[g][2 * h + 1] = from_pair<OutT>(t, 1);
+        }
+      }
+    }
+  }
+  __device__ __attribute__((always_inline)) void store_pair(const TileMatrix& t, int bi, int bj, const float (&val)[GB][NACC], bool through) const {
+    if constexpr (OS == 2) {
+      const uint32_t at = at_pair(t, bi, bj);
+#pragma unroll
+      for (int h = 0; h < HALVES; ++h) {
+        uint32_t w[RS];
+#pragma unroll
+        for (int g = 0; g < GB; ++g) w[g] = P::trade(pack_out<OutT>(val[g][2 * h], val[g][2 * h + 1]));
+        P::gather(w);
+#pragma unroll
+        for (int i = 0; i < RS; ++i) {
+          const uint32_t off = at + (uint32_t)(block_row_of<C>(2 * h) + 4 * i) * t.pitch;
+          if (through) __builtin_amdgcn_raw_buffer_store_b32(w[i], t.r, off, 0, 16);
+          else __builtin_amdgcn_raw_buffer_store_b32(w[i], t.r, off, 0, 0);
+        }
+      }
+    }
+  }
+  // ---- single elements: block (bi, bj)
+  __device__ __attribute__((always_inline)) uint32_t at_one(const TileMatrix& t, int bi, int bj) const {
+    const int c = col0 + bj * MB + lane % MB;
+    return c < cols ? (uint32_t)(c * OS) + (uint32_t)(row0 + bi * MB + 4 * (lane / MB)) * t.pitch : OOB;
+  }
+  __device__ __attribute__((always_inline)) void request_one(const TileMatrix& t, int bi, int bj, uint32_t (&in)[NACC]) const {
+    const uint32_t at = at_one(t, bi, bj);
+#pragma unroll
+    for (int v = 0; v < NACC; ++v) {
+      if constexpr (OS == 4) in[v] = __builtin_amdgcn_raw_buffer_load_b32(t.r, at + (uint32_t)block_row_of<C>(v) * t.pitch, 0, 0);
+      else in[v] = __builtin_amdgcn_raw_buffer_load_b16(t.r, at + (uint32_t)block_row_of<C>(v) * t.pitch, 0, 0);
+    }
+  }
+  __device__ __attribute__((always_inline)) void received_one(const uint32_t (&in)[NACC], float (&x)[NACC]) const {
+#pragma unroll
+    for (int v = 0; v < NACC; ++v) x[v] = from_bits<OutT>(in[v]);
+  }
+  __device__ __attribute__((always_inline)) void store_one(const TileMatrix& t, int bi, int bj, const float (&val)[NACC], bool through) const {
+    const uint32_t at = at_one(t, bi, bj);
+#pragma unroll
+    for (int v = 0; v < NACC; ++v) {
+      const uint32_t off = at + (uint32_t)block_row_of<C>(v) * t.pitch;
+      if constexpr (OS == 4) {
+        if (through) __builtin_amdgcn_raw_buffer_store_b32(as_u32(val[v]), t.r, off, 0, 16);
+        else __builtin_amdgcn_raw_buffer_store_b32(as_u32(val[v]), t.r, off, 0, 0);
+      } else {
+        uint16_t bits;
+        store_out<OutT>(&bits, 0, val[v]);
+        if (through) __builtin_amdgcn_raw_buffer_store_b16(bits, t.r, off, 0, 16);
+        else __builtin_amdgcn_raw_buffer_store_b16(bits, t.r, off, 0, 0);
+      }
+    }
+  }
+};
+
+// ---------------------------------------------------------------- the ends
+// act's value and slope at z, from one exponential
+__device__ inline void value_and_slope(const ActForm& form, int act, float z, float& value, float& slope) {
+  if (act == ACT_NONE) {
+    value = z;
+    slope = 1.f;
+  } else if (act == ACT_RELU) {
+    value = z < 0.f ? 0.f : z;
+    slope = z > 0.f ? 1.f : 0.f;
+  } else {
+    float q;
+    const float s = form.sigmoid(z, q);
+    value = z * s;
+    slope = fmaf(z * s * (1.f - s), fmaf(3.f * form.c2, q, form.c1), s);
+  }
+}
+
+struct Gated {
+  typedef GatedArgs Args;
+  static constexpr int MOVES = PLACE_ALL;
+  static constexpr bool OWN_END = true, STAYS = false, DUAL = true;
+  template <typename C>
+  static __device__ __attribute__((always_inline)) void touch(const Args&, const TilePlace&, uint32_t (&)[2]) {}
+
+  template <typename C, typename Acc, typename Hook>
+  static __device__ __attribute__((always_inline)) void finish(const Args& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p, Hook&&) {
+    constexpr int B2 = C::NBLK / 2, MB = C::MB, NACC = MB * MB / 64;
+    typedef WaveBlocks<C, B2> W;
+    const int rows = min(C::BM, a.M - p.m0), cols = min(C::BN / 2, a.N - p.n0);
+    const W w{p.row, p.col / 2, cols, p.lane};
+    const TileMatrix c(a.C, a.ldc, p.m0, p.n0, rows, cols, W::OS);
+    const TileMatrix g(a.preact, a.ld_preact, p.m0, p.n0, rows, cols, W::OS);
+    const TileMatrix u(a.preact ? (char*)a.preact + a.far_preact * W::OS : nullptr, a.ld_preact, p.m0, p.n0, rows, cols, W::OS);
+    const bool keeps = a.preact != nullptr, through = a.through;
+    const ActForm form(a.act);
+    float bias[2][B2];
+#pragma unroll
+    for (int bj = 0; bj < B2; ++bj) {
+      const int col = p.n0 + w.col0 + bj * MB + p.lane % MB;
+      const bool there = a.bias && col < a.N;
+      bias[0][bj] = there ? to_float<typename C::T>(a.bias, col) : 0.f;
+      bias[1][bj] = there ? to_float<typename C::T>(a.bias, (int64_t)a.N + col) : 0.f;
+    }
+    auto compute = [&](int bi, int bj, float (&zg)[NACC], float (&zu)[NACC], float (&y)[NACC]) {
+#pragma unroll
+      for (int v = 0; v < NACC; ++v) {
+        zg[v] = fmaf(a.alpha, acc[bi][bj][v], bias[0][bj]);
+        zu[v] = fmaf(a.alpha, acc[bi][bj + B2][v], bias[1][bj]);
+      }
+      if (a.act == ACT_NONE) {
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) y[v] = zg[v] * zu[v];
+      } else if (a.act == ACT_RELU) {
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) y[v] = (zg[v] < 0.f ? 0.f : zg[v]) * zu[v];
+      } else {
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) y[v] = form.value(zg[v]) * zu[v];
+      }
+    };
+    if (W::OS == 2 && a.paired) {
+#pragma unroll
+      for (int bj = 0; bj < B2; bj += W::GB)
+#pragma unroll
+        for (int bi = 0; bi < C::MBLK; ++bi) {
+          float zg[W::GB][NACC], zu[W::GB][NACC], y[W::GB][NACC];
+#pragma unroll
+          for (int x = 0; x < W::GB; ++x) compute(bi, bj + x, zg[x], zu[x], y[x]);
+          if (keeps) {
+            w.store_pair(g, bi, bj, zg, through);
+            w.store_pair(u, bi, bj, zu, through);
+          }
+          w.store_pair(c, bi, bj, y, through);
+        }
+      return;
+    }
+#pragma unroll
+    for (int bj = 0; bj < B2; ++bj)
+#pragma unroll
+      for (int bi = 0; bi < C::MBLK; ++bi) {
+        float zg[NACC], zu[NACC], y[NACC];
+        compute(bi, bj, zg, zu, y);
+        if (keeps) {
+          w.store_one(g, bi, bj, zg, through);
+          w.store_one(u, bi, bj, zu, through);
+        }
+        w.store_one(c, bi, bj, y, through);
+      }
+  }
+};
+
+struct GatedGrad {
+  typedef GatedArgs Args;
+  static constexpr int MOVES = PLACE_ALL;
+  static constexpr bool OWN_END = true, STAYS = false, DUAL = false;
+  template <typename C>
+  static __device__ __attribute__((always_inline)) void touch(const Args&, const TilePlace&, uint32_t (&)[2]) {}
+
+  // (dG and dU may lie where G and U do: a lane reads what it will write, and before)
+  template <typename C, typename Acc, typename Hook>
+  static __device__ __attribute__((always_inline)) void finish(const Args& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p, Hook&&) {
+    constexpr int MB = C::MB, NACC = MB * MB / 64;
+    typedef WaveBlocks<C, C::NBLK> W;
+    const int rows = min(C::BM, a.M - p.m0), cols = min(C::BN, a.N - p.n0);
+    const W w{p.row, p.col, cols, p.lane};
+    const TileMatrix h(a.C, a.ldc, p.m0, p.n0, rows, cols, W::OS);
+    const TileMatrix g(a.preact, a.ld_preact, p.m0, p.n0, rows, cols, W::OS);
+    const TileMatrix u((char*)a.preact + a.far_preact * W::OS, a.ld_preact, p.m0, p.n0, rows, cols, W::OS);
+    const TileMatrix dg(a.dpreact, a.ld_dpreact, p.m0, p.n0, rows, cols, W::OS);
+    const TileMatrix du((char*)a.dpreact + a.far_dpreact * W::OS, a.ld_dpreact, p.m0, p.n0, rows, cols, W::OS);
+    const bool again = a.C != nullptr, through = a.through;
+    const ActForm form(a.act);
+    // x: G, then dG; y: U, then dU; z: C
+    auto compute = [&](int bi, int bj, float (&x)[NACC], float (&y)[NACC], float (&z)[NACC]) {
+#pragma unroll
+      for (int v = 0; v < NACC; ++v) {
+        const float d = a.alpha * acc[bi][bj][v];
+        float value, slope;
+        value_and_slope(form, a.act, x[v], value, slope);
+        z[v] = value * y[v];
+        x[v] = d * y[v] * slope;
+        y[v] = d * value;
+      }
+    };
+    if (W::OS == 2 && a.paired) {
+      constexpr int UNITS = C::MBLK * (C::NBLK / W::GB), EACH = W::HALVES * W::RS;
+      constexpr int AHEAD = UNITS * EACH <= 16 ? UNITS : EACH >= 16 ? 1 : 16 / EACH;
+      uint32_t in_g[AHEAD][W::HALVES][W::RS], in_u[AHEAD][W::HALVES][W::RS];
+#pragma unroll
+      for (int n = 0; n < AHEAD; ++n) {
+        w.request_pair(g, n % C::MBLK, n / C::MBLK * W::GB, in_g[n]);
+        w.request_pair(u, n % C::MBLK, n / C::MBLK * W::GB, in_u[n]);
+      }
+#pragma unroll
+      for (int n = 0; n < UNITS; ++n) {
+        const int bi = n % C::MBLK, bj = n / C::MBLK * W::GB;
+        float x[W::GB][NACC], y[W::GB][NACC], z[W::GB][NACC];
+        w.received_pair(in_g[n % AHEAD], x);
+        w.received_pair(in_u[n % AHEAD], y);
+        if (n + AHEAD < UNITS) {
+          w.request_pair(g, (n + AHEAD) % C::MBLK, (n + AHEAD) / C::MBLK * W::GB, in_g[n % AHEAD]);
+          w.request_pair(u, (n + AHEAD) % C::MBLK, (n + AHEAD) / C::MBLK * W::GB, in_u[n % AHEAD]);
+        }
+#pragma unroll
+        for (int i = 0; i < W::GB; ++i) compute(bi, bj + i, x[i], y[i], z[i]);
+        w.store_pair(dg, bi, bj, x, through);
+        w.store_pair(du, bi, bj, y, through);
+        if (again) w.store_pair(h, bi, bj, z, through);
+      }
+      return;
+    }
+#pragma unroll
+    for (int bj = 0; bj < C::NBLK; ++bj)
+#pragma unroll
+      for (int bi = 0; bi < C::MBLK; ++bi) {
+        uint32_t in_g[NACC], in_u[NACC];
+        float x[NACC], y[NACC], z[NACC];
+        w.request_one(g, bi, bj, in_g);
+        w.request_one(u, bi, bj, in_u);
+        w.received_one(in_g, x);
+        w.received_one(in_u, y);
+        compute(bi, bj, x, y, z);
+        w.store_one(dg, bi, bj, x, through);
+        w.store_one(du, bi, bj, y, through);
+        if (again) w.store_one(h, bi, bj, z, through);
+      }
+  }
+};
+
+// x of every lane group of a block (rows 4 apart) joined: all of them hold the result
+template <int MB, typename Op>
+__device__ __attribute__((always_inline)) inline float over_groups(float x, Op&& op) {
+  if constexpr (MB == 16) {
+    const auto q = __builtin_amdgcn_permlane16_swap(as_u32(x), as_u32(x), false, false);
+    const uint32_t q0 = q[0], q1 = q[1];
+    x = op(as_f32(q0), as_f32(q1));
+  }
+  const auto q = __builtin_amdgcn_permlane32_swap(as_u32(x), as_u32(x), false, false);
+  const uint32_t q0 = q[0], q1 = q[1];
+  return op(as_f32(q0), as_f32(q1));
+}
+
+struct Score {
+  typedef ScoreArgs Args;
+  static constexpr int MOVES = PLACE_ALL;
+  static constexpr bool OWN_END = true, STAYS = true, DUAL = false;
+  template <typename C>
+  static __device__ __attribute__((always_inline)) void touch(const Args&, const TilePlace&, uint32_t (&)[2]) {}
+
+  template <typename C, typename Acc, typename Hook>
+  static __device__ __attribute__((always_inline)) void finish(const Args& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p, Hook&& before_stores) {
+    constexpr int MB = C::MB, NACC = MB * MB / 64;
+    constexpr int SET = score_set(C::WM), SETS = C::WM / SET, PER = SET / MB;      // blocks of a set
+    constexpr float log2e = 1.44269504088896340736f, ln2 = 0.69314718055994530942f;
+    const int lane = p.lane, frow = lane % MB, fgrp = lane / MB;
+    const int first = p.m0 + p.row;                                  // the wave's first row
+    const int rows = min(C::WM, a.M - first);
+    const int slab = first / C::WM;
+    float tops[C::NBLK], sums[C::NBLK], rests[C::NBLK], at_target[C::NBLK], set_top[C::NBLK][SETS];
+    bool hit[C::NBLK];
+    if (a.alpha != 1.f) {
+#pragma unroll
+      for (int bi = 0; bi < C::MBLK; ++bi)
+#pragma unroll
+        for (int bj = 0; bj < C::NBLK; ++bj)
+#pragma unroll
+          for (int v = 0; v < NACC; ++v) acc[bi][bj][v] *= a.alpha;
+    }
+    if (rows < C::WM) {
+#pragma unroll
+      for (int bi = 0; bi < C::MBLK; ++bi)
+#pragma unroll
+        for (int v = 0; v < NACC; ++v)
+          if (bi * MB + block_row_of<C>(v) + 4 * fgrp >= rows)
+#pragma unroll
+            for (int bj = 0; bj < C::NBLK; ++bj) acc[bi][bj][v] = -INFINITY;
+    }
+    auto larger = [](float x, float y) { return fmaxf(x, y); };
+    auto plus = [](float x, float y) { return x + y; };
+#pragma unroll
+    for (int bj = 0; bj < C::NBLK; ++bj) {
+      const int token = p.n0 + p.col + bj * MB + frow;
+      const bool there = token < a.N;
+      float top = -INFINITY;
+#pragma unroll
+      for (int s = 0; s < SETS; ++s) {
+        float t = -INFINITY;
+#pragma unroll
+        for (int b = 0; b < PER; ++b)
+#pragma unroll
+          for (int v = 0; v < NACC; ++v) t = fmaxf(t, acc[s * PER + b][bj][v]);
+        set_top[bj][s] = over_groups<MB>(t, larger);
+        top = fmaxf(top, set_top[bj][s]);
+      }
+      // exp(z - ref) = 2^y, y = log2(e) z - (log2(e) ref rounded), all terms off by one factor 2^off, which is taken out of the sums.  (Where the
+      // rounded product would not be finite the difference is taken first; the column's own choice, so that a token's bits do not depend
+      // on its neighbours.)  The weight in the second sum is y itself, held above -1e4 where the exponential is zero: 0 times minus infinity is
+      // not zero.
+      const float ref = lse_reference(top);
+      const bool far = fabsf(ref) > 1e37f;
+      const float base = far ? 0.f : -(log2e * ref), off = far ? 0.f : fmaf(log2e, ref, base);
+      float sum = 0.f, rest = 0.f;
+      auto reduce = [&](auto&& exponent) {
+#pragma unroll
+        for (int bi = 0; bi < C::MBLK; ++bi) {
+          float part = 0.f, more = 0.f;
+#pragma unroll
+          for (int v = 0; v < NACC; ++v) {
+            const float y = exponent(acc[bi][bj][v]), e = __builtin_amdgcn_exp2f(y);
+            part += e;
+            more = fmaf(e, fmaxf(y, -1e4f), more);
+          }
+          sum += part;
+          rest += more;
+        }
+      };
+      if (__any(far)) reduce([&](float z) { return far ? log2e * (z - ref) : fmaf(log2e, z, base); });
+      else reduce([&](float z) { return fmaf(log2e, z, base); });
+      rest = ln2 * fmaf(-off, sum, rest) * __builtin_amdgcn_exp2f(-off);
+      sum *= __builtin_amdgcn_exp2f(-off);
+      tops[bj] = top;
+      sums[bj] = over_groups<MB>(sum, plus);
+      rests[bj] = over_groups<MB>(rest, plus);
+      hit[bj] = false;
+      at_target[bj] = 0.f;
+      if (a.targets) {
+        const int64_t target = there ? a.targets[token] : -1;
+        const int64_t entry = (int64_t)first + a.row_first;
+        const int at = there && target != a.ignore && target >= entry && target < entry + rows ? (int)(target - entry) - 4 * fgrp : -1;
+        if (__any(at >= 0)) {
+#pragma unroll
+          for (int bi = 0; bi < C::MBLK; ++bi)
+#pragma unroll
+            for (int v = 0; v < NACC; ++v)
+              if (at == bi * MB + block_row_of<C>(v)) {
+                hit[bj] = true;
+                at_target[bj] = acc[bi][bj][v];
+              }
+        }
+      }
+    }
+    before_stores();
+    if (rows <= 0) return;
+#pragma unroll
+    for (int bj = 0; bj < C::NBLK; ++bj) {
+      const int token = p.n0 + p.col + bj * MB + frow;
+      if (token < a.N && fgrp == 0) {
+        a.parts[(int64_t)token * a.slabs + slab] = f32x4{tops[bj], sums[bj], rests[bj], 0.f};
+        if (a.sets) {
+#pragma unroll
+          for (int s = 0; s < SETS; ++s) a.set_max[(int64_t)token * a.sets + slab * SETS + s] = set_top[bj][s];
+        }
+      }
+      if (hit[bj]) a.at_target[token] = at_target[bj];
+    }
+    if (!a.sets) return;
+#pragma unroll
+    for (int bj = 0; bj < C::NBLK; ++bj) {
+      const int token = p.n0 + p.col + bj * MB + frow;
+      const bool there = token < a.N;
+      const float bar = a.bar && there ? a.bar[token] : NAN;
+#pragma unroll
+      for (int s = 0; s < SETS; ++s)
+        if (there && !(set_top[bj][s] <= bar)) {
+          float* to = a.logits + ((int64_t)(slab * SETS + s) * a.tokens + token) * SET + 4 * fgrp;
+#pragma unroll
+          for (int b = 0; b < PER; ++b)
+#pragma unroll
+            for (int q = 0; q < NACC / 4; ++q) {
+              const auto& x = acc[s * PER + b][bj];
+              *(f32x4*)(to + b * MB + 8 * q) = f32x4{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]};
+            }
+        }
+    }
+  }
+};
+
+// Weights of zero are a choice, not a factor: the logits of a token that teaches nothing may be infinite or NaN.
+struct Teach {
+  typedef FusedArgs Args;
+  static constexpr int MOVES = PLACE_ALL;
+  static constexpr bool OWN_END = true, STAYS = false, DUAL = false;
+  template <typename C>
+  static __device__ __attribute__((always_inline)) void touch(const Args&, const TilePlace&, uint32_t (&)[2]) {}
+
+  template <typename C, typename Acc, typename Hook>
+  static __device__ __attribute__((always_inline)) void finish(const Args& a, Acc (&acc)[C::MBLK][C::NBLK], const TilePlace& p, Hook&&) {
+    constexpr int MB = C::MB, NACC = MB * MB / 64;
+    typedef Fused<END_LINEAR, MOVE_NONE> Plain;
+    const float scale = a.scale ? *a.scale : 1.f;
+#pragma unroll
+    for (int bj = 0; bj < C::NBLK; ++bj) {
+      const int token = p.n0 + p.col + bj * MB + p.lane % MB;
+      const bool there = token < a.tokens;
+      const float weight = there ? a.dloss[token] * scale : 0.f;
+      const bool counts = weight != 0.f;
+      const float lse = counts ? a.lse[token] : INFINITY, base = -1.44269504088896340736f * lse;
+#pragma unroll
+      for (int bi = 0; bi < C::MBLK; ++bi)
+#pragma unroll
+        for (int v = 0; v < NACC; ++v) acc[bi][bj][v] = counts ? weight * Plain::template probability<C>(a.alpha * acc[bi][bj][v], lse, base) : 0.f;
+    }
+    Plain::template finish_linear<C, false>(a, acc, p);
+  }
+};
+
+}  // namespace gensor

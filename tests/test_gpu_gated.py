@@ -1,0 +1,242 @@
+"""Gated layers (both projections, the activation and the product of the two in one kernel) and their gradient against the definitions in 64 bits.
+
+Tolerances.  u = 2^-24.  A product's sum of K terms is off by at most e = (K + 4) u sum|a||b| (with its bias); the activations have slopes of at
+most 1.13 and are evaluated to within 16 u |z|, their slopes to within 64 u; products of two such values are off by the sum of either's error
+times the other, and a rounding; a result is rounded once to its type."""
+import gc
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+TORCH = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+ROUND = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 1e-37, "f16": 2.0 ** -25, "bf16": 1e-37}
+
+
+@pytest.fixture(scope="module")
+def gs():
+    from paper_2502_11407_amd import binding
+    yield binding
+    gc.collect()                                 # (other modules count the device memory that is in use)
+
+
+def draw(shape, dtype, seed, sigma=1.0, pad=0):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return torch.empty(tuple(shape[:-1]) + (shape[-1] + pad,), device="cuda").normal_(0.0, sigma, generator=g).to(TORCH[dtype])[..., :shape[-1]]
+
+
+def matrices(n, rows, cols, dtype, layout, pad, values=None):
+    """n matrices of rows x cols between values that nothing may touch: (tensor [n][rows][cols], check).  layout: "rows" side by side in the same
+    rows, "stack" one behind the other, "apart" with a gap between them."""
+    ld = n * cols + pad if layout == "rows" else cols + pad
+    gap = 3 * ld + 5 if layout == "apart" else 0
+    size = rows * ld if layout == "rows" else n * (rows * ld + gap)
+    flat = torch.full((size + 64,), 7.0, dtype=TORCH[dtype], device="cuda")
+    t = flat[32:].as_strided((n, rows, cols), (cols if layout == "rows" else rows * ld + gap, ld, 1), 32)
+    if values is not None:
+        t.copy_(values)
+
+    def untouched():
+        rest = torch.ones_like(flat, dtype=torch.bool)
+        rest.as_strided(t.shape, t.stride(), 32).fill_(False)
+        assert bool((flat[rest] == 7).all())
+    return t, untouched
+
+
+def act64(z, act):
+    if act == "relu":
+        return torch.where(z < 0, torch.zeros_like(z), z)
+    if act == "gelu":
+        return z / (1 + torch.exp(-2 * math.sqrt(2 / math.pi) * (z + 0.044715 * z ** 3)))
+    if act == "silu":
+        return z / (1 + torch.exp(-z))
+    return z
+
+
+def slope64(z, act):
+    if act == "none":
+        return torch.ones_like(z)
+    z = z.detach().clone().requires_grad_(True)
+    (torch.relu(z) if act == "relu" else act64(z, act)).sum().backward()
+    return z.grad
+
+
+def close(got, want, bound, dtype, what=""):
+    got = got.double()
+    limit = 1.01 * bound + ROUND[dtype] * want.abs() + TINY[dtype]
+    bad = ~((got - want).abs() <= limit)
+    assert not bool(bad.any()), (what, int(bad.sum()), float(((got - want).abs() / limit).nan_to_num(1e9).max()), torch.nonzero(bad)[:3].tolist())
+
+
+def check_forward(A, B, bias, act, alpha, out, C, Z, what):
+    a, b = A.double(), B.double()
+    K = a.shape[1]
+    z = [alpha * (a @ b[i]) + (0 if bias is None else bias[i].double()) for i in (0, 1)]
+    e = [(K + 4) * U * (abs(alpha) * (a.abs() @ b[i].abs()) + (0 if bias is None else bias[i].double().abs())) for i in (0, 1)]
+    f = act64(z[0], act)
+    e_f = 1.13 * e[0] + 16 * U * z[0].abs()
+    close(C, f * z[1], e_f * z[1].abs() + f.abs() * e[1] + e_f * e[1] + 2 * U * (f * z[1]).abs(), out, what)
+    if Z is not None:
+        for i in (0, 1):
+            close(Z[i], z[i], e[i], out, (what, "kept", i))
+
+
+SHAPES = [(1, 1, 1), (1, 96, 64), (1, 2048, 768), (2, 7, 3), (3, 520, 776), (5, 33, 17), (8, 256, 200), (9, 100, 128), (31, 64, 129), (64, 64, 64), (65, 130, 257),
+          (100, 1000, 72), (129, 255, 513), (256, 256, 256), (257, 384, 1024), (513, 768, 520), (1030, 1100, 190), (128, 128, 4096), (2048, 1152, 320), (4100, 768, 264)]
+
+
+@pytest.mark.parametrize("dtype,out", [("f16", "f16"), ("bf16", "bf16"), ("f16", "f32"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_forward(gs, dtype, out, M, N, K):
+    """Every activation, both layouts of the weights and where the second matrix lies, with and without biases and kept values, rows of any pitch."""
+    for i, (act, tb, where, bias, keep, pad, alpha) in enumerate([("silu", 0, "rows", False, True, 0, 1.0), ("gelu", 1, "stack", True, False, 8, 1.0),
+                                                                  ("relu", 0, "apart", True, True, 3, -0.75), ("none", 1, "apart", False, True, 1, 2.0),
+                                                                  ("silu", 1, "stack", False, False, 0, 1.0)]):
+        A = draw((M, K), dtype, 100 * i + M, pad=pad)
+        B, _ = matrices(2, *((N, K) if tb else (K, N)), dtype, where, pad, draw((2, N, K) if tb else (2, K, N), dtype, 100 * i + M + 1, 1 / math.sqrt(K)))
+        bv = draw((2, N), dtype, 5, 0.5) if bias else None
+        C, fine = matrices(1, M, N, out, "stack", pad)
+        Z, z_fine = matrices(2, M, N, out, "rows" if where == "rows" else "apart", pad) if keep else (None, lambda: None)
+        gs.gated_gemm(gs.gemm_problem(dtype, M, N, K, transB=tb, out_dtype=out), A, B, C[0], act=act, bias=bv, preact=Z, alpha=alpha)
+        check_forward(A, B.mT if tb else B, bv, act, alpha, out, C[0], Z, (act, tb, where))
+        fine()
+        z_fine()
+
+
+def test_values_of_a_neighbour_matrix_do_not_reach_the_first(gs):
+    """Columns beyond N of the first matrix are read where the second lies: infinities there stay there."""
+    for dtype, N, tb in (("bf16", 40, 0), ("bf16", 40, 1), ("f32", 37, 0), ("f16", 33, 1), ("f16", 300, 1)):
+        M, K = 70, 96
+        A, B = torch.ones((M, K), device="cuda").to(TORCH[dtype]), torch.zeros((2, N, K) if tb else (2, K, N), device="cuda").to(TORCH[dtype])
+        B[0] = 0.125
+        B[1] = float("inf")
+        Z = torch.empty((2, M, N), device="cuda", dtype=TORCH[dtype])
+        C = torch.empty((M, N), device="cuda", dtype=TORCH[dtype])
+        gs.gated_gemm(gs.gemm_problem(dtype, M, N, K, transB=tb, out_dtype=dtype), A, B, C, act="none", preact=Z)
+        assert bool((Z[0] == 12).all()) and bool(torch.isinf(Z[1]).all()) and bool(torch.isinf(C).all())
+
+
+@pytest.mark.parametrize("dtype,out", [("f16", "f16"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("M,N,K", [(1, 1, 1), (1, 2048, 96), (2, 3, 2), (37, 65, 40), (130, 257, 513), (512, 776, 264), (2050, 1536, 384)])
+def test_gradient(gs, dtype, out, M, N, K):
+    for i, (act, tb, where, pad, again) in enumerate([("silu", 1, "rows", 0, True), ("gelu", 0, "stack", 4, True), ("relu", 1, "apart", 1, False), ("none", 0, "rows", 2, True)]):
+        A, B = draw((M, K), dtype, 10 * i + M, pad=pad), draw((N, K) if tb else (K, N), dtype, 10 * i + M + 1, 1 / math.sqrt(K), pad)
+        Z, _ = matrices(2, M, N, out, where, pad, draw((2, M, N), out, 9, 2.0))
+        dZ, fine = matrices(2, M, N, out, "rows", pad)
+        H, h_fine = matrices(1, M, N, out, "stack", pad)
+        p = gs.gemm_problem(dtype, M, N, K, transB=tb, out_dtype=out)
+        gs.gated_act_grad(p, A, B, Z, dZ, act=act, H=H[0] if again else None, alpha=0.5)
+        a, b = A.double(), B.double().t() if tb else B.double()
+        d, e = 0.5 * (a @ b), 0.5 * (K + 4) * U * (a.abs() @ b.abs())
+        g, u = Z[0].double(), Z[1].double()
+        f, e_f = act64(g, act), 16 * U * g.abs()
+        close(dZ[0], d * u * slope64(g, act), 1.13 * e * u.abs() + 64 * U * (d * u).abs(), out, (act, "dG"))
+        close(dZ[1], d * f, e * (f.abs() + e_f) + d.abs() * e_f + 2 * U * (d * f).abs(), out, (act, "dU"))
+        fine()
+        if again:
+            close(H[0], f * u, e_f * u.abs() + 2 * U * (f * u).abs(), out, (act, "H"))
+            h_fine()
+        over, over_fine = matrices(2, M, N, out, where, pad, Z)            # over the values it reads
+        gs.gated_act_grad(p, A, B, over, over, act=act, alpha=0.5)
+        assert torch.equal(over, dZ)
+        over_fine()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "none"])
+def test_gradient_against_differences(gs, act):
+    """Forward and gradient belong together: central differences of the forward itself in fp32.  With a step h the difference is off by h^2 / 6 times the third
+    derivative (below 2 for these activations times |u| <= 2) and 2^-22 |y| / h of rounding, |y| <= 12."""
+    M, N, h = 32, 48, 2.0 ** -6
+    A = torch.ones((M, 1), device="cuda")
+    z = torch.empty((2, N), device="cuda")
+    z[0], z[1] = torch.linspace(-5, 5, N), torch.linspace(2, -2, N).roll(7)
+    p = gs.gemm_problem("f32", M, N, 1)
+
+    def forward(step_g, step_u):
+        y = torch.empty((M, N), device="cuda")
+        gs.gated_gemm(p, A, torch.stack([z[0] + step_g, z[1] + step_u])[:, None, :].contiguous(), y, act=act)
+        return y.double()
+    Z = z[:, None, :].expand(2, M, N).contiguous()
+    dZ = torch.empty_like(Z)
+    D = torch.linspace(-1, 1, M, device="cuda")[:, None].contiguous()
+    gs.gated_act_grad(p, D, torch.ones((1, N), device="cuda"), Z, dZ, act=act)
+    for i, (sg, su) in enumerate(((h, 0.0), (0.0, h))):
+        slope = (forward(sg, su) - forward(-sg, -su)) / (2 * h)
+        limit = h * h / 6 * 4 + 2.0 ** -22 * 12 / h
+        assert float((dZ[i].double() - D.double() * slope).abs().max()) <= limit, i
+
+
+def test_special_values(gs):
+    """NaN and infinities reach the results that they are part of, and no others."""
+    M, N, K = 40, 72, 64
+    A, B = draw((M, K), "bf16", 1), draw((2, K, N), "bf16", 2, 0.125)
+    A[3, 5], A[7, 9], B[1, 11, 20] = float("nan"), float("inf"), float("inf")
+    C, plain = torch.empty((M, N), device="cuda"), torch.empty((M, N), device="cuda")
+    p = gs.gemm_problem("bf16", M, N, K)
+    gs.gated_gemm(p, A, B, C, act="relu")
+    a, b = A.double(), B.double()
+    want = act64(a @ b[0], "relu") * (a @ b[1])
+    clean = torch.isfinite(want)
+    clean[3] = clean[7] = False
+    clean[:, 20] = False
+    assert bool(torch.isnan(C[3]).all()) and not bool(torch.isfinite(C[7]).any()) and bool(torch.isfinite(C[clean]).all())
+    A[3, 5], A[7, 9], B[1, 11, 20] = 0, 0, 0
+    gs.gated_gemm(p, A, B, plain, act="relu")
+    assert torch.equal(C[clean], plain[clean])
+
+
+def test_captured_and_replayed_and_on_another_stream(gs):
+    M, N, K = 200, 264, 136
+    A, B = draw((M, K), "f16", 3), draw((2, N, K), "f16", 4, 0.1)
+    D, W = draw((M, K), "f16", 5), draw((N, K), "f16", 6, 0.1)
+    Z, dZ, C, H = (torch.empty(s, device="cuda", dtype=torch.float16) for s in ((2, M, N), (2, M, N), (M, N), (M, N)))
+    p = gs.gemm_problem("f16", M, N, K, transB=1, out_dtype="f16")
+
+    def step():
+        gs.gated_gemm(p, A, B, C, preact=Z)
+        gs.gated_act_grad(p, D, W, Z, dZ, H=H)
+    step()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in (Z, dZ, C, H)]
+    assert torch.equal(C, H) or float((C.float() - H.float()).abs().max()) <= 2.0 ** -8 * float(C.float().abs().max())
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for n in range(3):
+        for t in (Z, dZ, C, H):
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((Z, dZ, C, H), want)), n
+        A.neg_()                                               # other values for the same graph, and back
+        graph.replay()
+        A.neg_()
+
+
+def test_far_matrices_and_long_outputs(gs):
+    """Weights 1.5 GB from one another; outputs of more than 2^31 elements' bytes, whose last rows count."""
+    K, N, M = 64, 96, 130
+    flat = torch.zeros((750_000_000 + N * K,), device="cuda", dtype=torch.bfloat16)
+    B = flat.as_strided((2, N, K), (750_000_000, K, 1))
+    B.copy_(draw((2, N, K), "bf16", 1, 0.125))
+    A = draw((M, K), "bf16", 2)
+    C = torch.empty((M, N), device="cuda")
+    gs.gated_gemm(gs.gemm_problem("bf16", M, N, K, transB=1), A, B, C)
+    check_forward(A, B.mT, None, "silu", 1.0, "f32", C, None, "far")
+    del flat, B
+    M, N, K = 1_100_000, 2048, 8
+    A, B = draw((M, K), "f16", 3), draw((2, K, N), "f16", 4, 0.3)
+    C = torch.empty((M, N), device="cuda", dtype=torch.float16)
+    gs.gated_gemm(gs.gemm_problem("f16", M, N, K, out_dtype="f16"), A, B, C, act="gelu")
+    for rows in (slice(0, 300), slice(M - 300, M)):
+        check_forward(A[rows], B, None, "gelu", 1.0, "f16", C[rows], None, rows)
