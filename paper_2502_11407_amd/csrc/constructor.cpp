@@ -389,7 +389,7 @@ double predict_rows(const GemmView& v, const gensor_hw& hw, int bm, int bn, int 
 // than units) are computed by `split` workgroups each, every one over 1/split of the k tiles; the parts leave fp32
 // partial tiles in device memory and a dependent launch adds them up.  Infeasible if there is nothing to split.
 double predict(const GemmView& v, const gensor_hw& hw, int bm, int bn, int bk, int wm, int wn, int kg,
-               int vm, int vn, int vec, int stages, int direct, int split) {
+               int vm, int vn, int vec, int stages, int direct, int split, bool narrow = true) {
   if (hw.compute_units < 1) return -1.0;              // rounds of tiles are whole-number divisions by it
   if (v.bsrc == B_CONV && direct && !vec) return split == 1 ? predict_rows(v, hw, bm, bn, wm, wn) : -1.0;
   if (v.bsrc == B_CONV && direct) return split == 1 ? predict_patch(v, hw, bm, bn, bk, wm, wn, kg, stages) : -1.0;
@@ -400,7 +400,7 @@ double predict(const GemmView& v, const gensor_hw& hw, int bm, int bn, int bk, i
   const int mb = kg == g ? 32 : 16;
   // the tiles whose wave groups alternate (Cfg::ALTERNATE): B has a third stage, and 192 columns may be what a launch cuts
   const bool alternate = direct && stages == 2 && e == 2 && mb == 16 && bm == 256 && bn == 256 && bk == 64;
-  if (alternate && split == 1 && narrow_tiles(v, hw.compute_units)) { bn = 192; wm = 64; wn = 96; }
+  if (narrow && alternate && split == 1 && narrow_tiles(v, hw.compute_units)) { bn = 192; wm = 64; wn = 96; }
   const double tiles_m = std::ceil((double)v.M / bm), tiles_n = std::ceil((double)v.N / bn);
   const double tiles = tiles_m * tiles_n * (double)v.batch;
   const int nwaves = (bm / wm) * (bn / wn);
@@ -569,8 +569,8 @@ void keep_choice(std::vector<Choice>* list, const Choice& x) {
 
 }  // namespace
 
-double fused_price(const InstanceDesc& d, const GemmView& v, int split) {
-  return predict(v, kMi355x, d.bm, d.bn, d.bk, d.wm, d.wn, d.kg, d.vm, d.vn, d.vec, d.stages, d.direct, split);
+double fused_price(const InstanceDesc& d, const GemmView& v, int split, bool narrow) {
+  return predict(v, kMi355x, d.bm, d.bn, d.bk, d.wm, d.wn, d.kg, d.vm, d.vn, d.vec, d.stages, d.direct, split, narrow);
 }
 
 gensor_status construct_internal(const gensor_problem* p, const gensor_hw* hw, const gensor_construct_opts* opts,

@@ -19,19 +19,31 @@ using namespace gensor;
 // ------------------------------------------------------------------------------------ gated layers
 namespace {
 
+// The tile that a shape's calls take, remembered: the index in its table, -1 where none serves.
 std::mutex g_gated_mutex;
-std::map<std::array<int64_t, 13>, const GatedDesc*> g_gated_choices;
+std::map<std::array<int64_t, 12>, int> g_gated_choices;
 const size_t kGatedLimit = 4096;
 
-// The cheapest tile of two products at once: priced as one product of twice the columns.
-gensor_status choose_gated(const GemmView& v, bool vec_ok, const LeadingDims& ld, int64_t strideB, const GatedDesc** out) {
-  const std::array<int64_t, 13> key = {v.in_dtype, v.out_dtype, v.bsrc, vec_ok, v.M, v.N, v.K, ld.a, ld.b, ld.c, strideB, 0, 0};
+template <typename F>
+gensor_status remembered(const std::array<int64_t, 12>& key, int* out, F&& find) {
   std::lock_guard<std::mutex> lock(g_gated_mutex);
   auto it = g_gated_choices.find(key);
   if (it == g_gated_choices.end()) {
+    if (g_gated_choices.size() >= kGatedLimit) g_gated_choices.clear();
+    it = g_gated_choices.emplace(key, find()).first;
+  }
+  *out = it->second;
+  return *out >= 0 ? GENSOR_OK : GENSOR_ERR_UNSUPPORTED;
+}
+
+// The cheapest tile of two products at once: priced as one product of twice the columns, without the 192-column form, which such tiles do not have.
+// The 256x256 tile's price is that of its products alone; with its epilogue it takes 1.13 times that beside a 256x128 tile's (bf16, us, 256x256 and
+// 256x128, W [N][K]: 2048 x 5632 x 2048 88 and 82, 3000 x 5400 x 2048 133 and 114, 8192 x 2048 x 768 46 and 53, 20000 x 688 x 256 25 and 28).
+gensor_status choose_gated(const GemmView& v, bool vec_ok, const LeadingDims& ld, int64_t strideB, int* out) {
+  return remembered({0, v.in_dtype, v.out_dtype, v.bsrc, vec_ok, v.M, v.N, v.K, ld.a, ld.b, ld.c, strideB}, out, [&]() {
     GemmView both = v;
     both.N = 2 * v.N;
-    const GatedDesc* best = nullptr;
+    int best = -1;
     double best_us = 1e30;
     for (int i = 0; i < g_num_gated; ++i) {
       const InstanceDesc& d = g_gated[i].d;
@@ -42,14 +54,33 @@ gensor_status choose_gated(const GemmView& v, bool vec_ok, const LeadingDims& ld
       if (((double)strideB + reach) * v.esize >= 2147483647.0) continue;
       const double tiles = (double)((v.M + d.bm - 1) / d.bm) * (double)((2 * v.N + d.bn - 1) / d.bn);
       if (!launch_fits(tiles, d.threads)) continue;
-      const double us = fused_price(d, both, 1);
-      if (us > 0 && us < best_us) { best_us = us; best = &g_gated[i]; }
+      const double us = fused_price(d, both, 1, false) * (d.alternate() ? 1.13 : 1.0);
+      if (us > 0 && us < best_us) { best_us = us; best = i; }
     }
-    if (g_gated_choices.size() >= kGatedLimit) g_gated_choices.clear();
-    it = g_gated_choices.emplace(key, best).first;
-  }
-  *out = it->second;
-  return *out ? GENSOR_OK : GENSOR_ERR_UNSUPPORTED;
+    return best;
+  });
+}
+
+// The tile of a gradient, whose epilogue takes longer than its products: two values read and two or three stored, an exponential, a reciprocal and some
+// thirty operations each, 24 us a round of 256x256 tiles and 0.33 ns an element and unit of smaller ones.  (bf16, us, 256x256, 256x128 and 128x128:
+// 8192 x 2048 x 768 49, 56, 65; 3000 x 5400 x 2048 132, 117, 125; 2048 x 5632 x 2048 62, 75, 75; 8192 x 4096 x 4096 254, 297, 364; 1024 x 4096 x 4096 92, 54, 44.
+// Lines of G and U requested under the products did not help: 8192 x 2048 x 768 56, and 69 against 63 among the gradient's other products.)
+gensor_status choose_gated_grad(const GemmView& v, bool vec_ok, const LeadingDims& ld, int* out) {
+  return remembered({1, v.in_dtype, v.out_dtype, v.bsrc, vec_ok, v.M, v.N, v.K, ld.a, ld.b, ld.c, 0}, out, [&]() {
+    int best = -1;
+    double best_us = 1e30;
+    for (int i = 0; i < g_num_fused; ++i) {
+      const InstanceDesc& d = g_fused[i].d;
+      if (!g_lm_ends[i].gated_grad || !instance_serves(d, v) || (d.vec && !vec_ok) || !offsets_fit(d, v, ld)) continue;
+      if (d.direct && !d.any_k() && v.K % d.bk != 0) continue;
+      const double tiles = (double)((v.M + d.bm - 1) / d.bm) * (double)((v.N + d.bn - 1) / d.bn);
+      if (!launch_fits(tiles, d.threads)) continue;
+      const double price = fused_price(d, v, 1, false), rounds = std::ceil(tiles / gensor_hw_mi355x()->compute_units);
+      const double us = price + rounds * (d.alternate() ? 24.0 : d.bm * d.bn * 0.33e-3);
+      if (price > 0 && us < best_us) { best_us = us; best = i; }
+    }
+    return best;
+  });
 }
 
 template <typename Args>
@@ -100,8 +131,8 @@ extern "C" gensor_status gensor_gated_gemm(const gensor_problem* p, int32_t act,
   if (!A || !B || !C || lda < v.K || ldb < (v.bsrc == B_KC ? v.K : v.N) || ldc < v.N || strideB < 0) return GENSOR_ERR_INVALID_ARG;
   if (preact && (ld_preact < v.N || !disjoint(v.M, v.N, ld_preact, stride_preact) || preact == C || (char*)preact + stride_preact * v.osize == C)) return GENSOR_ERR_INVALID_ARG;
   const LeadingDims ld = {lda, ldb, preact ? std::max(ldc, ld_preact) : ldc};
-  const GatedDesc* g;
-  st = choose_gated(v, vector_ok(v, A, lda, 0, B, ldb, strideB), ld, strideB, &g);
+  int tile;
+  st = choose_gated(v, vector_ok(v, A, lda, 0, B, ldb, strideB), ld, strideB, &tile);
   if (st == GENSOR_ERR_UNSUPPORTED && v.M >= 1 << 20) {
     // more tiles than a launch can have: the rows in two halves
     gensor_problem half = *p;
@@ -116,7 +147,8 @@ extern "C" gensor_status gensor_gated_gemm(const gensor_problem* p, int32_t act,
     return gensor_gated_gemm(&half, act, alpha, A2, lda, B, ldb, strideB, bias, C2, ldc, Z2, ld_preact, stride_preact, hip_stream);
   }
   if (st != GENSOR_OK) return st;
-  GatedArgs a = end_args<GatedArgs>(v, A, lda, B, ldb, C, ldc, alpha, g->d, g->d.bn / 2, 4);
+  const InstanceDesc& d = g_gated[tile].d;
+  GatedArgs a = end_args<GatedArgs>(v, A, lda, B, ldb, C, ldc, alpha, d, d.bn / 2, 4);
   a.strideB = strideB;
   a.act = act;
   a.bias = bias;
@@ -125,7 +157,7 @@ extern "C" gensor_status gensor_gated_gemm(const gensor_problem* p, int32_t act,
   a.far_preact = stride_preact;
   a.paired = pairs(C, ldc, v.N, v.osize) && (!preact || two_pairs(preact, ld_preact, stride_preact, v.N, v.osize));
   a.through = stored_through(v.M, v.N, ldc, v.osize) && (!preact || stored_through(v.M, v.N, ld_preact, v.osize));
-  return launched(g->launch(a, (hipStream_t)hip_stream));
+  return launched(g_gated[tile].launch(a, (hipStream_t)hip_stream));
   });
 }
 
@@ -142,8 +174,8 @@ extern "C" gensor_status gensor_gated_act_grad(const gensor_problem* p, int32_t 
   if (g0 == dg0 && (ld_preact != ld_dpreact || stride_preact != stride_dpreact)) return GENSOR_ERR_INVALID_ARG;
   if (g0 == du0 || u0 == dg0 || (H && (H == g0 || H == u0 || H == dg0 || H == du0))) return GENSOR_ERR_INVALID_ARG;
   const LeadingDims ld = {lda, ldb, std::max({ld_preact, ld_dpreact, H ? ldh : (int64_t)0})};
-  FusedChoice c;
-  st = choose(v, FUSED_LINEAR, vector_ok(v, A, lda, 0, B, ldb, 0), ld, 0, &c);
+  int tile;
+  st = choose_gated_grad(v, vector_ok(v, A, lda, 0, B, ldb, 0), ld, &tile);
   if (st == GENSOR_ERR_UNSUPPORTED && v.M >= 1 << 20) {
     gensor_problem half = *p;
     half.M = (v.M / 2 + 255) / 256 * 256;
@@ -155,7 +187,8 @@ extern "C" gensor_status gensor_gated_act_grad(const gensor_problem* p, int32_t 
                                  (char*)dpreact + h * ld_dpreact * v.osize, ld_dpreact, stride_dpreact, H ? (char*)H + h * ldh * v.osize : nullptr, ldh, hip_stream);
   }
   if (st != GENSOR_OK) return st;
-  GatedArgs a = end_args<GatedArgs>(v, A, lda, B, ldb, H, ldh, alpha, c.f->d, c.f->d.bn, 2);
+  const InstanceDesc& d = g_fused[tile].d;
+  GatedArgs a = end_args<GatedArgs>(v, A, lda, B, ldb, H, ldh, alpha, d, d.bn, 2);
   a.act = act;
   a.preact = (void*)preact;
   a.ld_preact = ld_preact;
@@ -165,7 +198,7 @@ extern "C" gensor_status gensor_gated_act_grad(const gensor_problem* p, int32_t 
   a.far_dpreact = stride_dpreact;
   a.paired = two_pairs(preact, ld_preact, stride_preact, v.N, v.osize) && two_pairs(dpreact, ld_dpreact, stride_dpreact, v.N, v.osize) && (!H || pairs(H, ldh, v.N, v.osize));
   a.through = stored_through(v.M, v.N, ld_dpreact, v.osize) && (!H || stored_through(v.M, v.N, ldh, v.osize));
-  return launched(g_lm_ends[c.f - g_fused].gated_grad(a, (hipStream_t)hip_stream));
+  return launched(g_lm_ends[tile].gated_grad(a, (hipStream_t)hip_stream));
   });
 }
 
@@ -201,118 +234,277 @@ struct AdvanceArgs {
   float *logprob, *lse, *entropy;
 };
 
-// The list of the largest, a lane each, in order; lane 0 the largest.  Entry NONE stands where there is none yet.
-struct TopList {
-  static constexpr int NONE = 0x7fffffff;
-  float value;
-  int entry;
-  __device__ static bool above(float v, int e, float v2, int e2) { return v > v2 || (v == v2 && e < e2); }
-  // puts (v, e), the same in all lanes, where it belongs
-  __device__ void insert(float v, int e) {
-    const int lane = threadIdx.x & 63;
-    const int at = __popcll(__ballot(above(value, entry, v, e)));
-    const float value_before = __shfl_up(value, 1, 64);
-    const int entry_before = __shfl_up(entry, 1, 64);
-    if (lane == at) { value = v; entry = e; }
-    else if (lane > at) { value = value_before; entry = entry_before; }
-  }
-  // every lane offers one; `n` of the list count.  (Which of them are above the n'th is known to all lanes; those are put in one by one.)
-  __device__ void offer(float v, int e, bool there, int n) {
-    // (all lanes ask for the n'th: a lane that is switched off has no value to give)
-    const bool is_above = above(v, e, __shfl(value, n - 1, 64), __shfl(entry, n - 1, 64));
-    uint64_t wanted = __ballot(there && is_above);
-    while (wanted) {
-      const int l = __builtin_ctzll(wanted);
-      insert(__shfl(v, l, 64), __shfl(e, l, 64));
-      const bool still = above(v, e, __shfl(value, n - 1, 64), __shfl(entry, n - 1, 64));
-      wanted &= (wanted - 1) & __ballot(still);
-    }
-  }
-};
+// A logit and its entry as one number, the larger the earlier it is among the largest: the value's order in front, then the lower entry.  0: none.
+__device__ inline uint64_t rank_key(float v, int entry) {
+  const uint32_t u = as_u32(v + 0.f);                                  // (minus zero is zero)
+  return (uint64_t)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (uint32_t)~entry;
+}
+__device__ inline float key_value(uint64_t key) {
+  const uint32_t u = (uint32_t)(key >> 32);
+  return as_f32(u & 0x80000000u ? u & 0x7fffffffu : ~u);
+}
+__device__ inline int key_entry(uint64_t key) { return (int)~(uint32_t)key; }
 
-// A wave per token: joins a piece's parts to what was joined before, and finds the largest logits among the piece's and those so far.  The `top` largest
-// lie in the `top` sets with the largest maxima (equal maxima: those of lower entries): a set that is not one of them has that many larger ones, or
-// equal ones in front of it.
-__global__ __launch_bounds__(256) void advance_kernel(const AdvanceArgs a) {
-  const int lane = threadIdx.x & 63;
-  for (int t = blockIdx.x * 4 + (threadIdx.x >> 6); t < a.tokens; t += gridDim.x * 4) {
+// x of all lanes joined (by an operation whose operands may be swapped): all of them hold the result.  In registers, without LDS.
+template <typename Op>
+__device__ inline float over_lanes(float x, Op&& op) {
+  auto moved = [&](auto ctrl_tag) { return as_f32((uint32_t)__builtin_amdgcn_mov_dpp((int)as_u32(x), decltype(ctrl_tag)::value, 0xF, 0xF, true)); };
+  x = op(x, moved(std::integral_constant<int, 0xB1>{}));               // quad_perm [1,0,3,2]
+  x = op(x, moved(std::integral_constant<int, 0x4E>{}));               // quad_perm [2,3,0,1]
+  x = op(x, moved(std::integral_constant<int, 0x141>{}));              // row_half_mirror
+  x = op(x, moved(std::integral_constant<int, 0x140>{}));              // row_mirror
+  return over_groups<16>(x, op);
+}
+
+// Parts (maximum, sum, weighted sum), a lane each, joined: all lanes hold the result.
+__device__ inline void join_lanes(float& top, float& sum, float& rest) {
+  constexpr float log2e = 1.44269504088896340736f;
+  auto plus = [](float x, float y) { return x + y; };
+  const float all = over_lanes(top, [](float x, float y) { return fmaxf(x, y); });
+  const float d = fabsf(top) == INFINITY ? 0.f : top - lse_reference(all), f = __builtin_amdgcn_exp2f(log2e * d);
+  rest = over_lanes(f > 0.f ? f * fmaf(sum, d, rest) : 0.f, plus);
+  sum = over_lanes(sum * f, plus);
+  top = all;
+}
+
+// The n'th largest of the lanes' values: the least of those that fewer than n are larger than.
+__device__ inline float nth_of_lanes(float x, int n) {
+  int larger = 0;
+#pragma unroll 8
+  for (int i = 0; i < 64; ++i) larger += as_f32((uint32_t)__builtin_amdgcn_readlane((int)as_u32(x), i)) > x;
+  return over_lanes(larger < n ? x : INFINITY, [](float a, float b) { return fminf(a, b); });
+}
+
+// WAVES waves per token join a piece's parts to what was joined before, and find the largest logits among the piece's and those so far.
+//
+// The search.  A bar that no more than a few logits reach is known before any is read: what the pieces so far say (the top'th largest, to be
+// exceeded), or in the first piece the top'th largest of 64 maxima of disjoint groups of sets (to be reached).  Sets whose maximum does not reach it hold
+// none of the largest; the logits of the others that reach it, and the largest so far, are gathered in LDS, and each one's place is the number of
+// those above it: no order in which anything is gathered matters.  (Putting them into a sorted list, a lane each, one by one took 0.3 us apiece: 23 us for
+// one token's five, 43 for the twenty of 301 tokens.)  Where more come up than there is room for -- many equal ones -- they are sought one by one: a scan
+// of all that were kept for the largest below the last found.
+template <int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(const AdvanceArgs a) {
+  constexpr int TOKENS = WAVES == 1 ? 4 : 1, AHEAD = 8, KEYS = WAVES == 1 ? 512 : 1024, SETS = 512;
+  __shared__ float joined[TOKENS][WAVES == 1 ? 1 : 3 * WAVES];
+  __shared__ float group_max[WAVES == 1 ? 1 : WAVES][64];
+  __shared__ int set_list[TOKENS][SETS];
+  __shared__ uint64_t keys[TOKENS][KEYS];
+  __shared__ int counts[2];
+  __shared__ uint64_t found[WAVES];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = WAVES == 1 ? 0 : wave, at = WAVES == 1 ? wave : 0;
+  auto meet = [&]() {
+    if constexpr (WAVES > 1) __syncthreads();
+    else {
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  };
+  // places in a list for the lanes that have something; the count goes on beyond what there is room for
+  int own_counts[2] = {0, 0};
+  auto places = [&](int which, bool mine) -> int {
+    const uint64_t all = __ballot(mine);
+    const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0u));
+    if constexpr (WAVES == 1) {
+      const int first = own_counts[which];
+      own_counts[which] = first + (int)__popcll(all);
+      return first + before;
+    }
+    if (all == 0) return 0;
+    int first = 0;
+    if (lane == 0) first = atomicAdd(&counts[which], (int)__popcll(all));
+    return __builtin_amdgcn_readfirstlane(first) + before;
+  };
+  auto count = [&](int which) { return WAVES == 1 ? own_counts[which] : counts[which]; };
+  for (int t = blockIdx.x * TOKENS + (WAVES == 1 ? wave : 0); t < a.tokens; t += gridDim.x * TOKENS) {
+    // everything that is known where to find is asked for first
+    const float* set_max = a.set_max + (int64_t)t * a.set_pitch;
+    const float* logits = a.logits + (int64_t)t * a.set_pitch * a.set_size;
+    float* values = a.values + (int64_t)t * a.top;
+    int64_t* index = a.index + (int64_t)t * a.top;
+    float m[AHEAD], most = -INFINITY, own_value = 0.f, bar = NAN;
+    int64_t own_entry = -1;
+    f32x4 so_far = {-INFINITY, 0.f, 0.f, 0.f};
+    if (!a.first) so_far = a.state[t];
+    if (a.top) {
+      if (!a.first) {
+        bar = a.bar[t];
+        if (lane < a.top) {
+          own_value = values[lane];
+          own_entry = index[lane];
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int s = 64 * (part + WAVES * u) + lane;
+        m[u] = s < a.sets ? set_max[s] : -INFINITY;
+      }
+    }
     float top = -INFINITY, sum = 0.f, rest = 0.f;
-    for (int s = lane; s < a.slabs; s += 4 * 64) {
+    for (int s = 64 * part + lane; s < a.slabs; s += 4 * 64 * WAVES) {
       f32x4 p[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) p[u] = s + 64 * u < a.slabs ? a.parts[(int64_t)t * a.slab_pitch + s + 64 * u] : f32x4{-INFINITY, 0.f, 0.f, 0.f};
+      for (int u = 0; u < 4; ++u) p[u] = s + 64 * WAVES * u < a.slabs ? a.parts[(int64_t)t * a.slab_pitch + s + 64 * WAVES * u] : f32x4{-INFINITY, 0.f, 0.f, 0.f};
+      // (four parts to one reference)
+      const float both = fmaxf(fmaxf(fmaxf(p[0][0], p[1][0]), fmaxf(p[2][0], p[3][0])), top), r = lse_reference(both);
+      auto scaled = [&](float part_top, float part_sum, float part_rest, float& to_sum, float& to_rest) {
+        const float d = fabsf(part_top) == INFINITY ? 0.f : part_top - r, f = __builtin_amdgcn_exp2f(1.44269504088896340736f * d);
+        to_rest += f > 0.f ? f * fmaf(part_sum, d, part_rest) : 0.f;
+        to_sum += part_sum * f;
+      };
+      float new_sum = 0.f, new_rest = 0.f;
+      scaled(top, sum, rest, new_sum, new_rest);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) join_scores(top, sum, rest, p[u][0], p[u][1], p[u][2]);
+      for (int u = 0; u < 4; ++u) scaled(p[u][0], p[u][1], p[u][2], new_sum, new_rest);
+      top = both; sum = new_sum; rest = new_rest;
     }
+    join_lanes(top, sum, rest);
+    meet();                                                            // (the token before)
+    own_counts[0] = own_counts[1] = 0;
+    if (WAVES > 1 && threadIdx.x < 2) counts[threadIdx.x] = 0;
+    if constexpr (WAVES > 1) {
+      if (a.top) {
 #pragma unroll
-    for (int d = 32; d >= 1; d /= 2) {
-      const float t2 = __shfl_xor(top, d, 64), s2 = __shfl_xor(sum, d, 64), r2 = __shfl_xor(rest, d, 64);
-      // (the same order in both lanes: the same bits)
-      if (lane & d) {
-        float x = t2, y = s2, z = r2;
-        join_scores(x, y, z, top, sum, rest);
-        top = x; sum = y; rest = z;
-      } else {
-        join_scores(top, sum, rest, t2, s2, r2);
+        for (int u = 0; u < AHEAD; ++u) most = fmaxf(most, m[u]);
+        group_max[wave][lane] = most;
+      }
+      if (lane == 0) {
+        joined[0][3 * wave] = top;
+        joined[0][3 * wave + 1] = sum;
+        joined[0][3 * wave + 2] = rest;
+      }
+      meet();
+      top = lane < WAVES ? joined[0][3 * lane] : -INFINITY;
+      sum = lane < WAVES ? joined[0][3 * lane + 1] : 0.f;
+      rest = lane < WAVES ? joined[0][3 * lane + 2] : 0.f;
+      join_lanes(top, sum, rest);
+      most = -INFINITY;
+      if (a.top) {
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) most = fmaxf(most, group_max[v][lane]);
+      }
+    } else {
+      meet();
+      if (a.top) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) most = fmaxf(most, m[u]);
       }
     }
     if (!a.first) {
-      const f32x4 so_far = a.state[t];
       float x = so_far[0], y = so_far[1], z = so_far[2];
       join_scores(x, y, z, top, sum, rest);
       top = x; sum = y; rest = z;
     }
-    if (!a.last && lane == 0) a.state[t] = f32x4{top, sum, rest, 0.f};
     const float ref = lse_reference(top), log_sum = logf(sum);
-    if (a.last && lane == 0) {
-      if (a.lse) a.lse[t] = ref + log_sum;
-      if (a.entropy) a.entropy[t] = log_sum - rest / sum;
-      if (a.logprob) {
-        const int64_t target = a.targets[t];
-        // (the maximum's part first: a target that is the maximum loses log(1 + the others), not a difference of large numbers)
-        a.logprob[t] = target == a.ignore ? 0.f : target >= 0 && target < a.vocab ? (a.at_target[t] - ref) - log_sum : NAN;
+    if (part == 0 && lane == 0) {
+      if (!a.last) {
+        a.state[t] = f32x4{top, sum, rest, 0.f};
+      } else {
+        if (a.lse) a.lse[t] = ref + log_sum;
+        if (a.entropy) a.entropy[t] = log_sum - rest / sum;
+        if (a.logprob) {
+          const int64_t target = a.targets[t];
+          // (the maximum's part first: a target that is the maximum loses log(1 + the others), not a difference of large numbers)
+          a.logprob[t] = target == a.ignore ? 0.f : target >= 0 && target < a.vocab ? (a.at_target[t] - ref) - log_sum : NAN;
+        }
       }
     }
     if (a.top == 0) continue;
 
-    const float bar = a.first ? NAN : a.bar[t];
-    TopList best_sets{-INFINITY, TopList::NONE};
-    for (int s = lane; s < (a.sets + 63) / 64 * 64; s += 4 * 64) {
-      float m[4];
+    // ---- sets that reach the bar
+    const float least = bar != bar ? nth_of_lanes(most, a.top) : -INFINITY;
+    auto reaches = [&](float v) { return v >= least && !(v <= bar); };
+    for (int s0 = 64 * part; s0 < a.sets; s0 += 64 * WAVES * AHEAD) {
+      if (s0 != 64 * part) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) m[u] = s + 64 * u < a.sets ? a.set_max[(int64_t)t * a.set_pitch + s + 64 * u] : -INFINITY;
-#pragma unroll
-      for (int u = 0; u < 4; ++u) best_sets.offer(m[u], s + 64 * u, s + 64 * u < a.sets && !(m[u] <= bar), a.top);
-    }
-    TopList best{-INFINITY, TopList::NONE};
-    if (!a.first && lane < a.top) {
-      const int64_t e = a.index[(int64_t)t * a.top + lane];
-      best.value = a.values[(int64_t)t * a.top + lane];
-      best.entry = e < 0 ? TopList::NONE : (int)e;
-    }
-    const int chosen = min(a.top, __popcll(__ballot(best_sets.entry != TopList::NONE)));
-    const int per = 64 / a.set_size;                                   // sets that the wave looks at together
-    for (int j = 0; j < chosen; j += 4 * per) {
-      float v[4];
-      int e[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int which = j + u * per + lane / a.set_size, set = __shfl(best_sets.entry, which & 63, 64);
-        const bool there = which < chosen;
-        const int entry = set * a.set_size + lane % a.set_size;
-        v[u] = there ? a.logits[((int64_t)set * a.tokens + t) * a.set_size + lane % a.set_size] : -INFINITY;
-        e[u] = there && entry < a.vocab - a.row_first ? a.row_first + entry : TopList::NONE;
+        for (int u = 0; u < AHEAD; ++u) {
+          const int s = s0 + 64 * WAVES * u + lane;
+          m[u] = s < a.sets ? set_max[s] : -INFINITY;
+        }
       }
 #pragma unroll
-      for (int u = 0; u < 4; ++u) best.offer(v[u], e[u], e[u] != TopList::NONE, a.top);
+      for (int u = 0; u < AHEAD; ++u) {
+        const int s = s0 + 64 * WAVES * u + lane;
+        const bool mine = s < a.sets && reaches(m[u]);
+        const int to = places(0, mine);
+        if (mine && to < SETS) set_list[at][to] = s;
+      }
     }
-    const bool full = __shfl(best.entry, a.top - 1, 64) != TopList::NONE;
-    const float least = __shfl(best.value, a.top - 1, 64);
-    if (!a.last && lane == 0) a.bar[t] = full ? least : NAN;
-    if (lane < a.top) {
-      const bool none = best.entry == TopList::NONE;
-      a.index[(int64_t)t * a.top + lane] = none ? -1 : (int64_t)best.entry;
-      a.values[(int64_t)t * a.top + lane] = !a.last ? best.value : none ? NAN : (best.value - ref) - log_sum;
+    // the largest so far
+    const uint64_t own_key = own_entry >= 0 ? rank_key(own_value, (int)own_entry) : 0;
+    if (!a.first && part == 0) {
+      const int to = places(1, own_key != 0);
+      if (own_key) keys[at][to] = own_key;
+    }
+    meet();
+    // ---- their logits that reach it
+    const int size = a.set_size, per = 64 / size;                      // sets that a wave looks at together
+    auto logit = [&](int set, int& entry) -> float {
+      entry = set * size + lane % size;
+      return logits[(int64_t)set * size + lane % size];
+    };
+    const int n_sets = count(0);
+    if (n_sets <= SETS) {
+      for (int j = part * per; j < n_sets; j += 4 * per * WAVES) {
+        float v[4];
+        int e[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int which = j + u * per * WAVES + lane / size;
+          e[u] = -1;
+          v[u] = which < n_sets ? logit(set_list[at][which], e[u]) : NAN;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const bool mine = reaches(v[u]) && e[u] >= 0 && e[u] < a.vocab - a.row_first;
+          const int to = places(1, mine);
+          if (mine && to < KEYS) keys[at][to] = rank_key(v[u], a.row_first + e[u]);
+        }
+      }
+    }
+    meet();
+    const int n = count(1);
+    auto put = [&](int rank, uint64_t key) {
+      index[rank] = key ? (int64_t)key_entry(key) : -1;
+      values[rank] = !key ? NAN : a.last ? (key_value(key) - ref) - log_sum : key_value(key);
+      if (rank == a.top - 1 && !a.last) a.bar[t] = key ? key_value(key) : NAN;
+    };
+    if (n_sets <= SETS && n <= KEYS) {
+      for (int i = 64 * part + lane; i < n; i += 64 * WAVES) {
+        const uint64_t own = keys[at][i];
+        int rank = 0;
+#pragma unroll 4
+        for (int o = 0; o < n; ++o) rank += keys[at][o] > own;
+        if (rank < a.top) put(rank, own);
+      }
+      for (int i = n + 64 * part + lane; i < a.top; i += 64 * WAVES) put(i, 0);
+      continue;
+    }
+    // ---- too many: the largest below the last found, over all sets that were kept, and so on.  
+    uint64_t last = ~0ull;
+    for (int r = 0; r < a.top; ++r) {
+      uint64_t best = own_key < last ? own_key : 0;
+      for (int s = part * per; s < a.sets; s += per * WAVES) {
+        const int set = s + lane / size;
+        if (set >= a.sets || set_max[set] <= bar) continue;
+        int entry;
+        const float v = logit(set, entry);
+        if (v != v || entry >= a.vocab - a.row_first) continue;
+        const uint64_t key = rank_key(v, a.row_first + entry);
+        if (key < last && key > best) best = key;
+      }
+      for (int d = 32; d >= 1; d /= 2) {
+        const uint64_t other = __shfl_xor((unsigned long long)best, d, 64);
+        best = other > best ? other : best;
+      }
+      if constexpr (WAVES > 1) {
+        if (lane == 0) found[wave] = best;
+        meet();
+        for (int w = 0; w < WAVES; ++w) best = found[w] > best ? found[w] : best;
+        meet();
+      }
+      if (part == 0 && lane == 0) put(r, best);
+      last = best;
     }
   }
 }
@@ -323,6 +515,8 @@ namespace {
 
 // Logits of a piece at most, where the largest are asked for
 const size_t kScoreBytes = (size_t)256 << 20;
+// ... of which a first piece that may keep them all
+const size_t kHeadBytes = (size_t)32 << 20;
 
 struct ScorePlan {
   int64_t slabs, sets;             // of a piece
@@ -404,6 +598,12 @@ gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, co
     piece = std::max<int64_t>(1, piece / 2 / d.bm) * d.bm;
   }
   const ScorePlan pl = score_plan(d, T, piece, out.top);
+  // Nothing is known of the first piece's logits, so all of them are kept: it is one round of tiles, after which few are above a token's bar.
+  int64_t rows = piece;
+  if (out.top && piece * T * 4 > (int64_t)kHeadBytes) {
+    const int64_t tiles_n = (T + d.bn - 1) / d.bn, round = gensor_hw_mi355x()->compute_units;
+    rows = std::min(piece, std::max<int64_t>(1, round / tiles_n) * d.bm);
+  }
   char* at = (char*)workspace;
   f32x4* state = (f32x4*)at;
   float* bar = (float*)(at + round_up((size_t)T * 16, 256));
@@ -412,8 +612,8 @@ gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, co
   float* maxima = (float*)(at + head + pl.parts);
   float* logits = (float*)(at + head + pl.parts + pl.maxima);
   const unsigned blocks = (unsigned)std::min<int64_t>((T + 3) / 4, 1 << 20);
-  for (int64_t entry = 0; entry < V; entry += piece) {
-    const int64_t rows = std::min(piece, V - entry);
+  for (int64_t entry = 0; entry < V; entry += rows, rows = piece) {
+    rows = std::min(rows, V - entry);
     const bool first = entry == 0, last = entry + rows == V;
     const GemmView q = prob_view(dtype, rows, T, D);
     ScoreArgs a = end_args<ScoreArgs>(q, (const char*)W + entry * ldw * size_of(dtype), ldw, X, ldx, nullptr, 0, scale, d, d.bn, 4);
@@ -422,6 +622,7 @@ gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, co
     a.tokens = (int32_t)T;
     a.row_first = (int32_t)entry;
     a.vocab = (int32_t)V;
+    a.weighted = out.entropy != nullptr;
     a.slabs = (int32_t)pl.slabs;
     a.sets = (int32_t)pl.sets;
     a.parts = parts;
@@ -456,7 +657,9 @@ gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, co
     v.logprob = out.logprob;
     v.lse = out.lse;
     v.entropy = out.entropy;
-    hipLaunchKernelGGL(advance_kernel, dim3(blocks), dim3(256), 0, s, v);
+    if (T <= 64) hipLaunchKernelGGL(advance_kernel<16>, dim3((unsigned)T), dim3(1024), 0, s, v);
+    else if (T <= 1024) hipLaunchKernelGGL(advance_kernel<4>, dim3((unsigned)T), dim3(256), 0, s, v);
+    else hipLaunchKernelGGL(advance_kernel<1>, dim3(blocks), dim3(256), 0, s, v);
     if (hipGetLastError() != hipSuccess) return GENSOR_ERR_DEVICE;
   }
   return GENSOR_OK;

@@ -97,8 +97,8 @@ inline bool launch_fits(double workgroups, int threads) { return workgroups * th
 bool vector_ok(const GemmView& v, const void* A, int64_t lda, int64_t strideA, const void* B, int64_t ldb, int64_t strideB);
 
 // The cost model's time of a tile on a product whose result is consumed in place (that is, of the product), microseconds; not
-// positive: the tile does not serve.
-double fused_price(const InstanceDesc& d, const GemmView& v, int split);
+// positive: the tile does not serve.  narrow: where 192-column forms of the 256x256 tiles would be launched, their price.
+double fused_price(const InstanceDesc& d, const GemmView& v, int split, bool narrow = true);
 
 // gensor_construct with more inputs: whether the operands allow 16-byte vector accesses, the view (ViewMode) a
 // pointwise convolution is taken in, and, where only tiles whose offsets reach are wanted, the leading dimensions.

@@ -12,6 +12,9 @@
 
 namespace gensor {
 
+// of a lambda that holds what it names by reference: called, these would lie in memory, a tile's descriptors among them
+#define GENSOR_INLINE __attribute__((always_inline))
+
 struct GatedArgs : KernelArgs {
   int32_t act;
   const void* bias;                // [2][N] of the input type, or null
@@ -25,10 +28,11 @@ struct ScoreArgs : KernelArgs {
   const int64_t* targets;
   int64_t ignore;
   int32_t tokens, row_first, vocab;        // row_first: vocabulary entry of row 0
+  int32_t weighted;                        // the weighted sum is wanted
   int32_t slabs, sets;                     // of a token's row of `parts` and of `set_max` (0: the largest are not asked for)
   f32x4* parts;                            // [token][slab of C::WM rows]: maximum, sum, weighted sum
   float* set_max;                          // [token][set of rows]
-  float* logits;                           // [set][token][rows of a set]
+  float* logits;                           // [token][set][rows of a set]: what is read of a token lies close together
   const float* bar;                        // logits of sets whose maximum is not above a token's are not needed (NaN, or null: all are)
   float* at_target;
 };
@@ -84,18 +88,12 @@ struct Paired {
 
 template <typename C> static constexpr __device__ int block_row_of(int v) { return C::MB == 32 ? 8 * (v / 4) + v % 4 : v; }
 
-// A matrix beside C, seen from a tile.
-struct TileMatrix {
-  __amdgpu_buffer_rsrc_t r;
-  uint32_t pitch;
-  __device__ TileMatrix(const void* base, int64_t ld, int64_t row, int64_t col, int rows, int cols, int size)
-      : r(__builtin_amdgcn_make_buffer_rsrc((void*)(base ? (const char*)base + (row * ld + col) * size : nullptr), 0, base ? records(ld, rows, cols, size) : 0u, 0x00020000u)),
-        pitch((uint32_t)(ld * size)) {}
-  static __device__ uint32_t records(int64_t ld, int rows, int cols, int size) {
-    const int64_t bytes = ((int64_t)(rows - 1) * ld + cols) * size;
-    return bytes <= 0 ? 0u : bytes > 0x7fffffffll ? 0x7fffffffu : (uint32_t)bytes;
-  }
-};
+// The descriptor of a matrix beside C, from the tile's first place to its last.  (Null: nothing is read and nothing written.)
+__device__ __attribute__((always_inline)) inline __amdgpu_buffer_rsrc_t tile_matrix(const void* base, int64_t ld, int64_t row, int64_t col, int rows, int cols, int size) {
+  const int64_t bytes = base ? ((int64_t)(rows - 1) * ld + cols) * size : 0;
+  return __builtin_amdgcn_make_buffer_rsrc((void*)(base ? (const char*)base + (row * ld + col) * size : nullptr), 0,
+                                           bytes <= 0 ? 0u : bytes > 0x7fffffffll ? 0x7fffffffu : (uint32_t)bytes, 0x00020000u);
+}
 
 // One wave's blocks of a matrix beside C: MBLK x BLOCKS of them, the first column at `col` of the tile.
 template <typename C, int BLOCKS>
@@ -108,104 +106,82 @@ struct WaveBlocks {
   int row0, col0, cols, lane;
 
   // ---- pairs (16-bit types, rows of whole dwords): unit (bi, bj .. bj + GB - 1)
-  __device__ __attribute__((always_inline)) uint32_t at_pair(const TileMatrix& t, int bi, int bj) const {
+  __device__ __attribute__((always_inline)) uint32_t at_pair(uint32_t pitch, int bi, int bj) const {
     const int c = col0 + bj * MB + P::column(lane);
-    return c < cols ? (uint32_t)(c * OS) + (uint32_t)(row0 + bi * MB + P::row(lane)) * t.pitch : OOB;
+    return c < cols ? (uint32_t)(c * OS) + (uint32_t)(row0 + bi * MB + P::row(lane)) * pitch : OOB;
   }
-  __device__ __attribute__((always_inline)) void request_pair(const TileMatrix& t, int bi, int bj, uint32_t (&in)[HALVES][RS]) const {
-    const uint32_t at = at_pair(t, bi, bj);
+  __device__ __attribute__((always_inline)) void request_pair(__amdgpu_buffer_rsrc_t r, uint32_t pitch, int bi, int bj, uint32_t (&in)[HALVES][RS]) const {
+    const uint32_t at = at_pair(pitch, bi, bj);
 #pragma unroll
     for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-      for (int i = 0; i < RS; ++i) in[h][i] = __builtin_amdgcn_raw_buffer_load_b32(t.r, at + (uint32_t)(block_row_of<C>(2 * h) + 4 * i) * t.pitch, 0, 0);
+      for (int i = 0; i < RS; ++i) in[h][i] = __builtin_amdgcn_raw_buffer_load_b32(r, at + (uint32_t)(block_row_of<C>(2 * h) + 4 * i) * pitch, 0, 0);
   }
-  __device__ __attribute__((always_inline)) void received_pair(const uint32_t (&in)[HALVES][RS], float (&x)[GB][NACC]) const {
+  // rows 2h and 2h + 1 of the blocks
+  __device__ __attribute__((always_inline)) void received_half(const uint32_t (&in)[RS], float (&x)[GB][2]) const {
     if constexpr (OS == 2) {
+      uint32_t w[RS];
 #pragma unroll
-      for (int h = 0; h < HALVES; ++h) {
-        uint32_t w[RS];
+      for (int i = 0; i < RS; ++i) w[i] = in[i];
+      P::scatter(w);
 #pragma unroll
-        for (int i = 0; i < RS; ++i) w[i] = in[h][i];
-        P::scatter(w);
-#pragma unroll
-        for (int g = 0; g < GB; ++g) {
-          const uint32_t t = P::trade(w[g]);
-          x[g][2 * h] = from_pair<OutT>(t, 0);
-          x[g][2 * h + 1] = from_pair<OutT>(t, 1);
-        }
+      for (int g = 0; g < GB; ++g) {
+        const uint32_t t = P::trade(w[g]);
+        x[g][0] = from_pair<OutT>(t, 0);
+        x[g][1] = from_pair<OutT>(t, 1);
       }
     }
   }
-  __device__ __attribute__((always_inline)) void store_pair(const TileMatrix& t, int bi, int bj, const float (&val)[GB][NACC], bool through) const {
+  __device__ __attribute__((always_inline)) void store_half(__amdgpu_buffer_rsrc_t r, uint32_t pitch, uint32_t at, int h, const float (&val)[GB][2], bool through) const {
     if constexpr (OS == 2) {
-      const uint32_t at = at_pair(t, bi, bj);
+      uint32_t w[RS];
 #pragma unroll
-      for (int h = 0; h < HALVES; ++h) {
-        uint32_t w[RS];
+      for (int g = 0; g < GB; ++g) w[g] = P::trade(pack_out<OutT>(val[g][0], val[g][1]));
+      P::gather(w);
 #pragma unroll
-        for (int g = 0; g < GB; ++g) w[g] = P::trade(pack_out<OutT>(val[g][2 * h], val[g][2 * h + 1]));
-        P::gather(w);
-#pragma unroll
-        for (int i = 0; i < RS; ++i) {
-          const uint32_t off = at + (uint32_t)(block_row_of<C>(2 * h) + 4 * i) * t.pitch;
-          if (through) __builtin_amdgcn_raw_buffer_store_b32(w[i], t.r, off, 0, 16);
-          else __builtin_amdgcn_raw_buffer_store_b32(w[i], t.r, off, 0, 0);
-        }
+      for (int i = 0; i < RS; ++i) {
+        const uint32_t off = at + (uint32_t)(block_row_of<C>(2 * h) + 4 * i) * pitch;
+        if (through) __builtin_amdgcn_raw_buffer_store_b32(w[i], r, off, 0, 16);
+        else __builtin_amdgcn_raw_buffer_store_b32(w[i], r, off, 0, 0);
       }
     }
   }
   // ---- single elements: block (bi, bj)
-  __device__ __attribute__((always_inline)) uint32_t at_one(const TileMatrix& t, int bi, int bj) const {
+  __device__ __attribute__((always_inline)) uint32_t at_one(uint32_t pitch, int bi, int bj) const {
     const int c = col0 + bj * MB + lane % MB;
-    return c < cols ? (uint32_t)(c * OS) + (uint32_t)(row0 + bi * MB + 4 * (lane / MB)) * t.pitch : OOB;
+    return c < cols ? (uint32_t)(c * OS) + (uint32_t)(row0 + bi * MB + 4 * (lane / MB)) * pitch : OOB;
   }
-  __device__ __attribute__((always_inline)) void request_one(const TileMatrix& t, int bi, int bj, uint32_t (&in)[NACC]) const {
-    const uint32_t at = at_one(t, bi, bj);
+  __device__ __attribute__((always_inline)) void request_one(__amdgpu_buffer_rsrc_t r, uint32_t pitch, int bi, int bj, uint32_t (&in)[NACC]) const {
+    const uint32_t at = at_one(pitch, bi, bj);
 #pragma unroll
     for (int v = 0; v < NACC; ++v) {
-      if constexpr (OS == 4) in[v] = __builtin_amdgcn_raw_buffer_load_b32(t.r, at + (uint32_t)block_row_of<C>(v) * t.pitch, 0, 0);
-      else in[v] = __builtin_amdgcn_raw_buffer_load_b16(t.r, at + (uint32_t)block_row_of<C>(v) * t.pitch, 0, 0);
+      if constexpr (OS == 4) in[v] = __builtin_amdgcn_raw_buffer_load_b32(r, at + (uint32_t)block_row_of<C>(v) * pitch, 0, 0);
+      else in[v] = __builtin_amdgcn_raw_buffer_load_b16(r, at + (uint32_t)block_row_of<C>(v) * pitch, 0, 0);
     }
   }
   __device__ __attribute__((always_inline)) void received_one(const uint32_t (&in)[NACC], float (&x)[NACC]) const {
 #pragma unroll
     for (int v = 0; v < NACC; ++v) x[v] = from_bits<OutT>(in[v]);
   }
-  __device__ __attribute__((always_inline)) void store_one(const TileMatrix& t, int bi, int bj, const float (&val)[NACC], bool through) const {
-    const uint32_t at = at_one(t, bi, bj);
+  __device__ __attribute__((always_inline)) void store_one(__amdgpu_buffer_rsrc_t r, uint32_t pitch, int bi, int bj, const float (&val)[NACC], bool through) const {
+    const uint32_t at = at_one(pitch, bi, bj);
 #pragma unroll
     for (int v = 0; v < NACC; ++v) {
-      const uint32_t off = at + (uint32_t)block_row_of<C>(v) * t.pitch;
+      const uint32_t off = at + (uint32_t)block_row_of<C>(v) * pitch;
       if constexpr (OS == 4) {
-        if (through) __builtin_amdgcn_raw_buffer_store_b32(as_u32(val[v]), t.r, off, 0, 16);
-        else __builtin_amdgcn_raw_buffer_store_b32(as_u32(val[v]), t.r, off, 0, 0);
+        if (through) __builtin_amdgcn_raw_buffer_store_b32(as_u32(val[v]), r, off, 0, 16);
+        else __builtin_amdgcn_raw_buffer_store_b32(as_u32(val[v]), r, off, 0, 0);
       } else {
         uint16_t bits;
         store_out<OutT>(&bits, 0, val[v]);
-        if (through) __builtin_amdgcn_raw_buffer_store_b16(bits, t.r, off, 0, 16);
-        else __builtin_amdgcn_raw_buffer_store_b16(bits, t.r, off, 0, 0);
+        if (through) __builtin_amdgcn_raw_buffer_store_b16(bits, r, off, 0, 16);
+        else __builtin_amdgcn_raw_buffer_store_b16(bits, r, off, 0, 0);
       }
     }
   }
 };
 
 // ---------------------------------------------------------------- the ends
-// act's value and slope at z, from one exponential
-__device__ inline void value_and_slope(const ActForm& form, int act, float z, float& value, float& slope) {
-  if (act == ACT_NONE) {
-    value = z;
-    slope = 1.f;
-  } else if (act == ACT_RELU) {
-    value = z < 0.f ? 0.f : z;
-    slope = z > 0.f ? 1.f : 0.f;
-  } else {
-    float q;
-    const float s = form.sigmoid(z, q);
-    value = z * s;
-    slope = fmaf(z * s * (1.f - s), fmaf(3.f * form.c2, q, form.c1), s);
-  }
-}
-
 struct Gated {
   typedef GatedArgs Args;
   static constexpr int MOVES = PLACE_ALL;
@@ -219,9 +195,10 @@ struct Gated {
     typedef WaveBlocks<C, B2> W;
     const int rows = min(C::BM, a.M - p.m0), cols = min(C::BN / 2, a.N - p.n0);
     const W w{p.row, p.col / 2, cols, p.lane};
-    const TileMatrix c(a.C, a.ldc, p.m0, p.n0, rows, cols, W::OS);
-    const TileMatrix g(a.preact, a.ld_preact, p.m0, p.n0, rows, cols, W::OS);
-    const TileMatrix u(a.preact ? (char*)a.preact + a.far_preact * W::OS : nullptr, a.ld_preact, p.m0, p.n0, rows, cols, W::OS);
+    const uint32_t pitch_c = (uint32_t)(a.ldc * W::OS), pitch_z = (uint32_t)(a.ld_preact * W::OS);
+    const __amdgpu_buffer_rsrc_t c = tile_matrix(a.C, a.ldc, p.m0, p.n0, rows, cols, W::OS);
+    const __amdgpu_buffer_rsrc_t g = tile_matrix(a.preact, a.ld_preact, p.m0, p.n0, rows, cols, W::OS);
+    const __amdgpu_buffer_rsrc_t u = tile_matrix(a.preact ? (char*)a.preact + a.far_preact * W::OS : nullptr, a.ld_preact, p.m0, p.n0, rows, cols, W::OS);
     const bool keeps = a.preact != nullptr, through = a.through;
     const ActForm form(a.act);
     float bias[2][B2];
@@ -232,51 +209,53 @@ struct Gated {
       bias[0][bj] = there ? to_float<typename C::T>(a.bias, col) : 0.f;
       bias[1][bj] = there ? to_float<typename C::T>(a.bias, (int64_t)a.N + col) : 0.f;
     }
-    auto compute = [&](int bi, int bj, float (&zg)[NACC], float (&zu)[NACC], float (&y)[NACC]) {
+    // (every index is a constant: accumulators that are indexed in a loop would lie in memory)
+    auto compute = [&](auto bi, auto bj, auto first, auto& zg, auto& zu, auto& y) GENSOR_INLINE {
+      constexpr int N = sizeof(y) / sizeof(float);
 #pragma unroll
-      for (int v = 0; v < NACC; ++v) {
-        zg[v] = fmaf(a.alpha, acc[bi][bj][v], bias[0][bj]);
-        zu[v] = fmaf(a.alpha, acc[bi][bj + B2][v], bias[1][bj]);
+      for (int v = 0; v < N; ++v) {
+        zg[v] = fmaf(a.alpha, acc[bi][bj][first + v], bias[0][bj]);
+        zu[v] = fmaf(a.alpha, acc[bi][bj + B2][first + v], bias[1][bj]);
       }
       if (a.act == ACT_NONE) {
 #pragma unroll
-        for (int v = 0; v < NACC; ++v) y[v] = zg[v] * zu[v];
+        for (int v = 0; v < N; ++v) y[v] = zg[v] * zu[v];
       } else if (a.act == ACT_RELU) {
 #pragma unroll
-        for (int v = 0; v < NACC; ++v) y[v] = (zg[v] < 0.f ? 0.f : zg[v]) * zu[v];
+        for (int v = 0; v < N; ++v) y[v] = (zg[v] < 0.f ? 0.f : zg[v]) * zu[v];
       } else {
 #pragma unroll
-        for (int v = 0; v < NACC; ++v) y[v] = form.value(zg[v]) * zu[v];
+        for (int v = 0; v < N; ++v) y[v] = form.value(zg[v]) * zu[v];
       }
     };
     if (W::OS == 2 && a.paired) {
-#pragma unroll
-      for (int bj = 0; bj < B2; bj += W::GB)
-#pragma unroll
-        for (int bi = 0; bi < C::MBLK; ++bi) {
-          float zg[W::GB][NACC], zu[W::GB][NACC], y[W::GB][NACC];
-#pragma unroll
-          for (int x = 0; x < W::GB; ++x) compute(bi, bj + x, zg[x], zu[x], y[x]);
+      static_for<B2 / W::GB * C::MBLK>([&](auto n) GENSOR_INLINE {
+        constexpr std::integral_constant<int, n % C::MBLK> bi{};
+        constexpr int bj = n / C::MBLK * W::GB;
+        const uint32_t at_g = w.at_pair(pitch_z, bi, bj), at_u = w.at_pair(pitch_z, bi, bj), at_c = w.at_pair(pitch_c, bi, bj);
+        static_for<W::HALVES>([&](auto h) GENSOR_INLINE {
+          float zg[W::GB][2], zu[W::GB][2], y[W::GB][2];
+          static_for<W::GB>([&](auto i) GENSOR_INLINE { compute(bi, std::integral_constant<int, bj + i>{}, std::integral_constant<int, 2 * h>{}, zg[i], zu[i], y[i]); });
           if (keeps) {
-            w.store_pair(g, bi, bj, zg, through);
-            w.store_pair(u, bi, bj, zu, through);
+            w.store_half(g, pitch_z, at_g, h, zg, through);
+            w.store_half(u, pitch_z, at_u, h, zu, through);
           }
-          w.store_pair(c, bi, bj, y, through);
-        }
+          w.store_half(c, pitch_c, at_c, h, y, through);
+        });
+      });
       return;
     }
-#pragma unroll
-    for (int bj = 0; bj < B2; ++bj)
-#pragma unroll
-      for (int bi = 0; bi < C::MBLK; ++bi) {
-        float zg[NACC], zu[NACC], y[NACC];
-        compute(bi, bj, zg, zu, y);
-        if (keeps) {
-          w.store_one(g, bi, bj, zg, through);
-          w.store_one(u, bi, bj, zu, through);
-        }
-        w.store_one(c, bi, bj, y, through);
+    static_for<B2 * C::MBLK>([&](auto n) GENSOR_INLINE {
+      constexpr std::integral_constant<int, n % C::MBLK> bi{};
+      constexpr std::integral_constant<int, n / C::MBLK> bj{};
+      float zg[NACC], zu[NACC], y[NACC];
+      compute(bi, bj, std::integral_constant<int, 0>{}, zg, zu, y);
+      if (keeps) {
+        w.store_one(g, pitch_z, bi, bj, zg, through);
+        w.store_one(u, pitch_z, bi, bj, zu, through);
       }
+      w.store_one(c, pitch_c, bi, bj, y, through);
+    });
   }
 };
 
@@ -294,67 +273,97 @@ struct GatedGrad {
     typedef WaveBlocks<C, C::NBLK> W;
     const int rows = min(C::BM, a.M - p.m0), cols = min(C::BN, a.N - p.n0);
     const W w{p.row, p.col, cols, p.lane};
-    const TileMatrix h(a.C, a.ldc, p.m0, p.n0, rows, cols, W::OS);
-    const TileMatrix g(a.preact, a.ld_preact, p.m0, p.n0, rows, cols, W::OS);
-    const TileMatrix u((char*)a.preact + a.far_preact * W::OS, a.ld_preact, p.m0, p.n0, rows, cols, W::OS);
-    const TileMatrix dg(a.dpreact, a.ld_dpreact, p.m0, p.n0, rows, cols, W::OS);
-    const TileMatrix du((char*)a.dpreact + a.far_dpreact * W::OS, a.ld_dpreact, p.m0, p.n0, rows, cols, W::OS);
+    const uint32_t pitch_h = (uint32_t)(a.ldc * W::OS), pitch_z = (uint32_t)(a.ld_preact * W::OS), pitch_d = (uint32_t)(a.ld_dpreact * W::OS);
+    const __amdgpu_buffer_rsrc_t h = tile_matrix(a.C, a.ldc, p.m0, p.n0, rows, cols, W::OS);
+    const __amdgpu_buffer_rsrc_t g = tile_matrix(a.preact, a.ld_preact, p.m0, p.n0, rows, cols, W::OS);
+    const __amdgpu_buffer_rsrc_t u = tile_matrix((char*)a.preact + a.far_preact * W::OS, a.ld_preact, p.m0, p.n0, rows, cols, W::OS);
+    const __amdgpu_buffer_rsrc_t dg = tile_matrix(a.dpreact, a.ld_dpreact, p.m0, p.n0, rows, cols, W::OS);
+    const __amdgpu_buffer_rsrc_t du = tile_matrix((char*)a.dpreact + a.far_dpreact * W::OS, a.ld_dpreact, p.m0, p.n0, rows, cols, W::OS);
     const bool again = a.C != nullptr, through = a.through;
     const ActForm form(a.act);
-    // x: G, then dG; y: U, then dU; z: C
-    auto compute = [&](int bi, int bj, float (&x)[NACC], float (&y)[NACC], float (&z)[NACC]) {
+    // x: G, then dG; y: U, then dU; z: C.  The value and the slope of gelu and silu come from one exponential.
+    auto compute = [&](auto bi, auto bj, auto first, auto& x, auto& y, auto& z) GENSOR_INLINE {
+      constexpr int N = sizeof(x) / sizeof(float);
+      auto each = [&](auto&& value_and_slope) GENSOR_INLINE {
 #pragma unroll
-      for (int v = 0; v < NACC; ++v) {
-        const float d = a.alpha * acc[bi][bj][v];
-        float value, slope;
-        value_and_slope(form, a.act, x[v], value, slope);
-        z[v] = value * y[v];
-        x[v] = d * y[v] * slope;
-        y[v] = d * value;
+        for (int v = 0; v < N; ++v) {
+          const float d = a.alpha * acc[bi][bj][first + v], u = y[v];
+          float value, slope;
+          value_and_slope(x[v], value, slope);
+          z[v] = value * u;
+          x[v] = d * u * slope;
+          y[v] = d * value;
+        }
+      };
+      if (a.act == ACT_NONE) {
+        each([&](float g, float& value, float& slope) GENSOR_INLINE { value = g; slope = 1.f; });
+      } else if (a.act == ACT_RELU) {
+        each([&](float g, float& value, float& slope) GENSOR_INLINE { value = g < 0.f ? 0.f : g; slope = g > 0.f ? 1.f : 0.f; });
+      } else {
+        each([&](float g, float& value, float& slope) GENSOR_INLINE {
+          float q;
+          const float s = form.sigmoid(g, q);
+          value = g * s;
+          slope = fmaf(value * (1.f - s), fmaf(3.f * form.c2, q, form.c1), s);
+        });
       }
     };
+    // (every index is a constant: accumulators that are indexed in a loop would lie in memory)
     if (W::OS == 2 && a.paired) {
       constexpr int UNITS = C::MBLK * (C::NBLK / W::GB), EACH = W::HALVES * W::RS;
       constexpr int AHEAD = UNITS * EACH <= 16 ? UNITS : EACH >= 16 ? 1 : 16 / EACH;
       uint32_t in_g[AHEAD][W::HALVES][W::RS], in_u[AHEAD][W::HALVES][W::RS];
-#pragma unroll
-      for (int n = 0; n < AHEAD; ++n) {
-        w.request_pair(g, n % C::MBLK, n / C::MBLK * W::GB, in_g[n]);
-        w.request_pair(u, n % C::MBLK, n / C::MBLK * W::GB, in_u[n]);
-      }
-#pragma unroll
-      for (int n = 0; n < UNITS; ++n) {
-        const int bi = n % C::MBLK, bj = n / C::MBLK * W::GB;
-        float x[W::GB][NACC], y[W::GB][NACC], z[W::GB][NACC];
-        w.received_pair(in_g[n % AHEAD], x);
-        w.received_pair(in_u[n % AHEAD], y);
-        if (n + AHEAD < UNITS) {
-          w.request_pair(g, (n + AHEAD) % C::MBLK, (n + AHEAD) / C::MBLK * W::GB, in_g[n % AHEAD]);
-          w.request_pair(u, (n + AHEAD) % C::MBLK, (n + AHEAD) / C::MBLK * W::GB, in_u[n % AHEAD]);
+      static_for<AHEAD>([&](auto n) GENSOR_INLINE {
+        w.request_pair(g, pitch_z, n % C::MBLK, n / C::MBLK * W::GB, in_g[n]);
+        w.request_pair(u, pitch_z, n % C::MBLK, n / C::MBLK * W::GB, in_u[n]);
+      });
+      static_for<UNITS>([&](auto n) GENSOR_INLINE {
+        constexpr std::integral_constant<int, n % C::MBLK> bi{};
+        constexpr int bj = n / C::MBLK * W::GB, next = n + AHEAD;
+        uint32_t got_g[W::HALVES][W::RS], got_u[W::HALVES][W::RS];
+        static_for<W::HALVES * W::RS>([&](auto i) GENSOR_INLINE {
+          got_g[i / W::RS][i % W::RS] = in_g[n % AHEAD][i / W::RS][i % W::RS];
+          got_u[i / W::RS][i % W::RS] = in_u[n % AHEAD][i / W::RS][i % W::RS];
+        });
+        if constexpr (next < UNITS) {
+          w.request_pair(g, pitch_z, next % C::MBLK, next / C::MBLK * W::GB, in_g[n % AHEAD]);
+          w.request_pair(u, pitch_z, next % C::MBLK, next / C::MBLK * W::GB, in_u[n % AHEAD]);
         }
-#pragma unroll
-        for (int i = 0; i < W::GB; ++i) compute(bi, bj + i, x[i], y[i], z[i]);
-        w.store_pair(dg, bi, bj, x, through);
-        w.store_pair(du, bi, bj, y, through);
-        if (again) w.store_pair(h, bi, bj, z, through);
-      }
+        const uint32_t at_g = w.at_pair(pitch_d, bi, bj), at_u = w.at_pair(pitch_d, bi, bj), at_h = w.at_pair(pitch_h, bi, bj);
+        static_for<W::HALVES>([&](auto half) GENSOR_INLINE {
+          float x[W::GB][2], y[W::GB][2], z[W::GB][2];
+          w.received_half(got_g[half], x);
+          w.received_half(got_u[half], y);
+          static_for<W::GB>([&](auto i) GENSOR_INLINE { compute(bi, std::integral_constant<int, bj + i>{}, std::integral_constant<int, 2 * half>{}, x[i], y[i], z[i]); });
+          w.store_half(dg, pitch_d, at_g, half, x, through);
+          w.store_half(du, pitch_d, at_u, half, y, through);
+          if (again) w.store_half(h, pitch_h, at_h, half, z, through);
+        });
+      });
       return;
     }
-#pragma unroll
-    for (int bj = 0; bj < C::NBLK; ++bj)
-#pragma unroll
-      for (int bi = 0; bi < C::MBLK; ++bi) {
-        uint32_t in_g[NACC], in_u[NACC];
-        float x[NACC], y[NACC], z[NACC];
-        w.request_one(g, bi, bj, in_g);
-        w.request_one(u, bi, bj, in_u);
-        w.received_one(in_g, x);
-        w.received_one(in_u, y);
-        compute(bi, bj, x, y, z);
-        w.store_one(dg, bi, bj, x, through);
-        w.store_one(du, bi, bj, y, through);
-        if (again) w.store_one(h, bi, bj, z, through);
+    constexpr int BLOCKS = C::MBLK * C::NBLK, AHEAD = BLOCKS * NACC <= 16 ? BLOCKS : 16 / NACC;
+    uint32_t in_g[AHEAD][NACC], in_u[AHEAD][NACC];
+    static_for<AHEAD>([&](auto n) GENSOR_INLINE {
+      w.request_one(g, pitch_z, n % C::MBLK, n / C::MBLK, in_g[n]);
+      w.request_one(u, pitch_z, n % C::MBLK, n / C::MBLK, in_u[n]);
+    });
+    static_for<BLOCKS>([&](auto n) GENSOR_INLINE {
+      constexpr std::integral_constant<int, n % C::MBLK> bi{};
+      constexpr std::integral_constant<int, n / C::MBLK> bj{};
+      constexpr int next = n + AHEAD;
+      float x[NACC], y[NACC], z[NACC];
+      w.received_one(in_g[n % AHEAD], x);
+      w.received_one(in_u[n % AHEAD], y);
+      if constexpr (next < BLOCKS) {
+        w.request_one(g, pitch_z, next % C::MBLK, next / C::MBLK, in_g[n % AHEAD]);
+        w.request_one(u, pitch_z, next % C::MBLK, next / C::MBLK, in_u[n % AHEAD]);
       }
+      compute(bi, bj, std::integral_constant<int, 0>{}, x, y, z);
+      w.store_one(dg, pitch_d, bi, bj, x, through);
+      w.store_one(du, pitch_d, bi, bj, y, through);
+      if (again) w.store_one(h, pitch_h, bi, bj, z, through);
+    });
   }
 };
 
@@ -387,8 +396,14 @@ struct Score {
     const int first = p.m0 + p.row;                                  // the wave's first row
     const int rows = min(C::WM, a.M - first);
     const int slab = first / C::WM;
-    float tops[C::NBLK], sums[C::NBLK], rests[C::NBLK], at_target[C::NBLK], set_top[C::NBLK][SETS];
+    float tops[C::NBLK], sums[C::NBLK], rests[C::NBLK], at_target[C::NBLK], set_top[C::NBLK][SETS], bar[C::NBLK];
     bool hit[C::NBLK];
+    // (asked for early: nothing waits for it until everything is computed)
+#pragma unroll
+    for (int bj = 0; bj < C::NBLK; ++bj) {
+      const int token = p.n0 + p.col + bj * MB + frow;
+      bar[bj] = a.bar && token < a.N ? a.bar[token] : NAN;
+    }
     if (a.alpha != 1.f) {
 #pragma unroll
       for (int bi = 0; bi < C::MBLK; ++bi)
@@ -425,13 +440,15 @@ struct Score {
       }
       // exp(z - ref) = 2^y, y = log2(e) z - (log2(e) ref rounded), all terms off by one factor 2^off, which is taken out of the sums.  (Where the
       // rounded product would not be finite the difference is taken first; the column's own choice, so that a token's bits do not depend
-      // on its neighbours.)  The weight in the second sum is y itself, held above -1e4 where the exponential is zero: 0 times minus infinity is
-      // not zero.
+      // on its neighbours.)  The weight in the second sum is y itself; where a logit is minus infinity, or a row none, that is 0 times minus infinity,
+      // and the sums are taken again with weights that are held above -1e4.
       const float ref = lse_reference(top);
       const bool far = fabsf(ref) > 1e37f;
       const float base = far ? 0.f : -(log2e * ref), off = far ? 0.f : fmaf(log2e, ref, base);
       float sum = 0.f, rest = 0.f;
-      auto reduce = [&](auto&& exponent) {
+      auto reduce = [&](auto weighted_tag, auto&& exponent, auto&& weight) {
+        constexpr bool weighted = decltype(weighted_tag)::value;
+        sum = rest = 0.f;
 #pragma unroll
         for (int bi = 0; bi < C::MBLK; ++bi) {
           float part = 0.f, more = 0.f;
@@ -439,14 +456,24 @@ struct Score {
           for (int v = 0; v < NACC; ++v) {
             const float y = exponent(acc[bi][bj][v]), e = __builtin_amdgcn_exp2f(y);
             part += e;
-            more = fmaf(e, fmaxf(y, -1e4f), more);
+            if constexpr (weighted) more = fmaf(e, weight(y), more);
           }
           sum += part;
           rest += more;
         }
       };
-      if (__any(far)) reduce([&](float z) { return far ? log2e * (z - ref) : fmaf(log2e, z, base); });
-      else reduce([&](float z) { return fmaf(log2e, z, base); });
+      auto near_ref = [&](float z) { return fmaf(log2e, z, base); };
+      auto any_ref = [&](float z) { return far ? log2e * (z - ref) : fmaf(log2e, z, base); };
+      auto itself = [](float y) { return y; };
+      auto finite = [](float y) { return fmaxf(y, -1e4f); };
+      if (!a.weighted) {
+        if (__any(far)) reduce(std::false_type{}, any_ref, itself);
+        else reduce(std::false_type{}, near_ref, itself);
+      } else {
+        if (__any(far)) reduce(std::true_type{}, any_ref, finite);
+        else reduce(std::true_type{}, near_ref, itself);
+        if (__any(rest != rest)) reduce(std::true_type{}, any_ref, finite);
+      }
       rest = ln2 * fmaf(-off, sum, rest) * __builtin_amdgcn_exp2f(-off);
       sum *= __builtin_amdgcn_exp2f(-off);
       tops[bj] = top;
@@ -478,8 +505,11 @@ struct Score {
       if (token < a.N && fgrp == 0) {
         a.parts[(int64_t)token * a.slabs + slab] = f32x4{tops[bj], sums[bj], rests[bj], 0.f};
         if (a.sets) {
+          typedef float maxima_t __attribute__((ext_vector_type(SETS)));
+          maxima_t m;
 #pragma unroll
-          for (int s = 0; s < SETS; ++s) a.set_max[(int64_t)token * a.sets + slab * SETS + s] = set_top[bj][s];
+          for (int s = 0; s < SETS; ++s) m[s] = set_top[bj][s];
+          *(maxima_t*)(a.set_max + (int64_t)token * a.sets + slab * SETS) = m;
         }
       }
       if (hit[bj]) a.at_target[token] = at_target[bj];
@@ -489,11 +519,11 @@ struct Score {
     for (int bj = 0; bj < C::NBLK; ++bj) {
       const int token = p.n0 + p.col + bj * MB + frow;
       const bool there = token < a.N;
-      const float bar = a.bar && there ? a.bar[token] : NAN;
+      if (!__any(there && !(tops[bj] <= bar[bj]))) continue;
 #pragma unroll
       for (int s = 0; s < SETS; ++s)
-        if (there && !(set_top[bj][s] <= bar)) {
-          float* to = a.logits + ((int64_t)(slab * SETS + s) * a.tokens + token) * SET + 4 * fgrp;
+        if (there && !(set_top[bj][s] <= bar[bj])) {
+          float* to = a.logits + ((int64_t)token * a.sets + slab * SETS + s) * SET + 4 * fgrp;
 #pragma unroll
           for (int b = 0; b < PER; ++b)
 #pragma unroll
