@@ -719,35 +719,86 @@ struct TeacherEntries {
   int bad;
 };
 
-// Fills them, all 256 threads of a workgroup: a wave takes four entries at a time, whose rows of W it reads side by side with the token's row of X.
+// Fills them, all 256 threads of a workgroup: a wave takes four entries at a time, whose rows of W it reads side by side with the token's row of X, two
+// vectors a lane of each requested together.  Bound by those rows, from the last-level cache: 4096 tokens' sixteen entries of width 768 in 16 bits are 100 MB.
 template <typename T, bool VEC>
 __device__ inline void teacher_entries(const TeacherArgs& a, int t, TeacherEntries& e) {
   constexpr int ES = ElemSize<T>::value, EPC = 16 / ES;
-  const int i = threadIdx.x, lane = i & 63, wave = i >> 6;
+  const int i = threadIdx.x, lane = i & 63, wave = __builtin_amdgcn_readfirstlane(i >> 6);
+  auto plus = [](float x, float y) { return x + y; };
   __syncthreads();                                                   // (the token before)
   if (i == 0) e.bad = 0;
   __syncthreads();
   if (i < a.k) {
     const int64_t at = a.index[(int64_t)t * a.k + i];
+    const float q = a.teacher[(int64_t)t * a.k + i];
     const bool there = at >= 0 && at < a.V;
     e.entry[i] = there ? (int)at : -1;
     if (at < -1 || at >= a.V) e.bad = 1;                             // (any of the threads that find one)
-    e.log_p[i] = there ? a.teacher[(int64_t)t * a.k + i] : -INFINITY;
+    e.log_p[i] = there ? q : -INFINITY;
   }
   __syncthreads();
-  if (wave == 0) {
+  const char* x = a.X + (int64_t)t * a.ldx * ES;
+  for (int j = 4 * wave; j < a.k; j += 16) {
+    const char* w[4];
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) w[u] = a.W + (int64_t)(j + u < a.k ? max(e.entry[j + u], 0) : 0) * a.ldw * ES;
+    if constexpr (VEC) {
+      for (int c = lane * EPC; c < a.D; c += 2 * 64 * EPC) {
+        const int c2 = c + 64 * EPC;
+        u32x4 xv[2], wv[4][2];
+        xv[0] = *(const u32x4*)(x + (int64_t)c * ES);
+        xv[1] = c2 < a.D ? *(const u32x4*)(x + (int64_t)c2 * ES) : u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          wv[u][0] = *(const u32x4*)(w[u] + (int64_t)c * ES);
+          wv[u][1] = c2 < a.D ? *(const u32x4*)(w[u] + (int64_t)c2 * ES) : u32x4{0u, 0u, 0u, 0u};
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int n = 0; n < EPC; ++n) {
+              if constexpr (ES == 4) acc[u] = fmaf(as_f32(xv[h][n]), as_f32(wv[u][h][n]), acc[u]);
+              else acc[u] = fmaf(from_pair<T>(xv[h][n / 2], n & 1), from_pair<T>(wv[u][h][n / 2], n & 1), acc[u]);
+            }
+      }
+    } else {
+      for (int c = lane; c < a.D; c += 4 * 64) {
+        float xv[4], wv[4][4];
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          const bool there = c + 64 * h < a.D;
+          xv[h] = there ? to_float<T>(x, c + 64 * h) : 0.f;
+#pragma unroll
+          for (int u = 0; u < 4; ++u) wv[u][h] = there ? to_float<T>(w[u], c + 64 * h) : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int h = 0; h < 4; ++h) acc[u] = fmaf(xv[h], wv[u][h], acc[u]);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const float z = over_lanes(acc[u], plus);
+      if (lane == 0 && j + u < a.k) e.z[j + u] = a.scale * z;
+    }
+  }
+  if (wave == 3) {                                                   // (it has the fewest entries)
     float shift = 0.f;
     if (a.normalize) {
       float top = -INFINITY, sum = 0.f;
       for (int j = lane; j < a.k; j += 64) {
         if (e.entry[j] >= 0) e.log_p[j] *= a.scale;
-        top = e.log_p[j] > top || e.log_p[j] != e.log_p[j] ? e.log_p[j] : top;
+        top = fmaxf(top, e.log_p[j]);
       }
-      for (int d = 32; d >= 1; d /= 2) top = fmaxf(top, __shfl_xor(top, d, 64));
+      top = over_lanes(top, [](float x, float y) { return fmaxf(x, y); });
       if (top > -INFINITY)
         for (int j = lane; j < a.k; j += 64) sum += expf(e.log_p[j] - top);
-      for (int d = 32; d >= 1; d /= 2) sum += __shfl_xor(sum, d, 64);
-      shift = top > -INFINITY ? top + logf(sum) : 0.f;
+      shift = top > -INFINITY ? top + logf(over_lanes(sum, plus)) : 0.f;
     }
     float mass = 0.f;
     for (int j = lane; j < a.k; j += 64) {
@@ -756,41 +807,8 @@ __device__ inline void teacher_entries(const TeacherArgs& a, int t, TeacherEntri
       e.p[j] = expf(q);
       mass += e.p[j];
     }
-    for (int d = 32; d >= 1; d /= 2) mass += __shfl_xor(mass, d, 64);
+    mass = over_lanes(mass, plus);
     if (lane == 0) e.mass = mass;
-  }
-  const char* x = a.X + (int64_t)t * a.ldx * ES;
-  for (int j = 4 * wave; j < a.k; j += 16) {
-    const char* w[4];
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int u = 0; u < 4; ++u) w[u] = a.W + (int64_t)(j + u < a.k ? max(e.entry[j + u], 0) : 0) * a.ldw * ES;
-    if constexpr (VEC) {
-      for (int c = lane * EPC; c < a.D; c += 64 * EPC) {
-        const u32x4 xv = *(const u32x4*)(x + (int64_t)c * ES);
-        u32x4 wv[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) wv[u] = *(const u32x4*)(w[u] + (int64_t)c * ES);
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int n = 0; n < EPC; ++n) {
-            if constexpr (ES == 4) acc[u] = fmaf(as_f32(xv[n]), as_f32(wv[u][n]), acc[u]);
-            else acc[u] = fmaf(from_pair<T>(xv[n / 2], n & 1), from_pair<T>(wv[u][n / 2], n & 1), acc[u]);
-          }
-      }
-    } else {
-      for (int c = lane; c < a.D; c += 64) {
-        const float xv = to_float<T>(x, c);
-#pragma unroll
-        for (int u = 0; u < 4; ++u) acc[u] = fmaf(xv, to_float<T>(w[u], c), acc[u]);
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      for (int d = 32; d >= 1; d /= 2) acc[u] += __shfl_xor(acc[u], d, 64);
-      if (lane == 0 && j + u < a.k) e.z[j + u] = a.scale * acc[u];
-    }
   }
   __syncthreads();
 }
@@ -805,7 +823,7 @@ __global__ __launch_bounds__(256) void teacher_loss_kernel(const TeacherArgs a) 
     float loss = 0.f;
     // (entries that are none and probabilities of zero by choice: their logarithms and logits may be infinite)
     for (int j = threadIdx.x; j < a.k; j += 64) loss += e.p[j] == 0.f ? 0.f : e.p[j] * ((e.log_p[j] - e.z[j]) + lse);
-    for (int d = 32; d >= 1; d /= 2) loss += __shfl_xor(loss, d, 64);
+    loss = over_lanes(loss, [](float x, float y) { return x + y; });
     if (threadIdx.x == 0) a.loss[t] = e.bad ? NAN : loss;
   }
 }
