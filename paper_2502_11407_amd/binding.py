@@ -552,13 +552,16 @@ def xent_backward(X, W, targets, lse, dloss, dX, dW, ignore_index: int = -100, s
 # ---- a language model's gated layers, the scores of its vocabulary, and learning from a teacher.  The launches go to the current device: tensors
 # of another one are refused.
 def _on_current_device(stream, **tensors):
-    import torch
-    here = torch.cuda.current_device()
+    """The stream as a hipStream_t, once all tensors are found to be on its device."""
+    if _current is None:
+        _stream_ptr()
+    here = _current[0]()
     if stream is not None and stream.device_index != here:
         raise ValueError(f"stream: one of the current device, {here}, is wanted, got device {stream.device_index}")
     for name, t in tensors.items():
         if t is not None and t.get_device() != here:
             raise ValueError(f"{name}: a tensor on the current device, {here}, is wanted, got {t.device}")
+    return stream.cuda_stream if stream is not None else _current[1](here)
 
 
 def _act(act: str) -> int:
@@ -591,9 +594,9 @@ def gated_gemm(p: Problem, A, B, Cout, act: str = "silu", bias=None, preact=None
     ldz, far_z = (0, 0) if preact is None else _two(preact, M, N, out, "preact")
     if bias is not None and (bias.shape != (2, N) or not bias.is_contiguous() or bias.dtype is not dtype or not bias.is_cuda):
         raise ValueError(f"bias: a contiguous device tensor of {(2, N)} {dtype} is wanted, got {tuple(bias.shape)} {bias.dtype} on {bias.device}")
-    _on_current_device(stream, A=A, B=B, C=Cout, bias=bias, preact=preact)
+    st_ptr = _on_current_device(stream, A=A, B=B, C=Cout, bias=bias, preact=preact)
     st = lib.gensor_gated_gemm(C.byref(p), code, alpha, A.data_ptr(), lda, B.data_ptr(), ldb, far, None if bias is None else bias.data_ptr(), Cout.data_ptr(), ldc,
-                               None if preact is None else preact.data_ptr(), ldz, far_z, _stream_ptr(stream))
+                               None if preact is None else preact.data_ptr(), ldz, far_z, st_ptr)
     if st:
         _check(st, "gensor_gated_gemm")
 
@@ -610,9 +613,9 @@ def gated_act_grad(p: Problem, A, B, preact, dpreact, act: str = "silu", H=None,
     ldz, far_z = _two(preact, M, N, out, "preact")
     ldd, far_d = _two(dpreact, M, N, out, "dpreact")
     ldh = 0 if H is None else _matrix(H, M, N, out, "H")
-    _on_current_device(stream, A=A, B=B, preact=preact, dpreact=dpreact, H=H)
+    st_ptr = _on_current_device(stream, A=A, B=B, preact=preact, dpreact=dpreact, H=H)
     st = lib.gensor_gated_act_grad(C.byref(p), code, alpha, A.data_ptr(), lda, B.data_ptr(), ldb, preact.data_ptr(), ldz, far_z, dpreact.data_ptr(), ldd, far_d,
-                                   None if H is None else H.data_ptr(), ldh, _stream_ptr(stream))
+                                   None if H is None else H.data_ptr(), ldh, st_ptr)
     if st:
         _check(st, "gensor_gated_act_grad")
 
@@ -643,12 +646,12 @@ def logprobs(X, W, targets=None, logprob=None, lse=None, entropy=None, top_index
     if top_index is not None and top == 0:
         raise ValueError("top_index: room for one alternative at least is wanted")
     ws_ptr, ws_len = _ws(workspace)
-    _on_current_device(stream, X=X, W=W, targets=targets, logprob=logprob, lse=lse, entropy=entropy, top_index=top_index, top_logprob=top_logprob, workspace=workspace)
+    st_ptr = _on_current_device(stream, X=X, W=W, targets=targets, logprob=logprob, lse=lse, entropy=entropy, top_index=top_index, top_logprob=top_logprob, workspace=workspace)
     _check(lib.gensor_logprobs(dt, T, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, scale, None if targets is None else _vector(targets, T, "torch.int64", "targets"),
                                ignore_index, None if logprob is None else _vector(logprob, T, "torch.float32", "logprob"),
                                None if lse is None else _vector(lse, T, "torch.float32", "lse"), None if entropy is None else _vector(entropy, T, "torch.float32", "entropy"),
                                top, None if top == 0 else _table(top_index, (T, top), "torch.int64", "top_index"),
-                               None if top == 0 else _table(top_logprob, (T, top), "torch.float32", "top_logprob"), ws_ptr, ws_len, _stream_ptr(stream)), "gensor_logprobs")
+                               None if top == 0 else _table(top_logprob, (T, top), "torch.float32", "top_logprob"), ws_ptr, ws_len, st_ptr), "gensor_logprobs")
 
 
 def distill_workspace_bytes(dtype: str, T: int, V: int, D: int, k: int, backward: bool = False) -> int:
@@ -660,28 +663,27 @@ def _distill(X, W, index, teacher, stream, **tensors):
     dt, dtype = _code(X, "X"), X.dtype
     ldx, ldw = _matrix(X, T, D, dtype, "X"), _matrix(W, V, D, dtype, "W")
     at, q = _table(index, (T, k), "torch.int64", "index"), _table(teacher, (T, k), "torch.float32", "teacher")
-    _on_current_device(stream, X=X, W=W, index=index, teacher=teacher, **tensors)
-    return dt, T, V, D, ldx, ldw, k, at, q
+    return dt, T, V, D, ldx, ldw, k, at, q, _on_current_device(stream, X=X, W=W, index=index, teacher=teacher, **tensors)
 
 
 def distill_forward(X, W, index, teacher, loss, lse, scale: float = 1.0, normalize: bool = True, stream=None, workspace=None):
     """loss[t] = sum_j p_j (log p_j - z[index_j] + lse) of the logits z = scale X W^T, which are not kept, against a teacher's entries: index [T][k] int64 (-1: none)
     and their log probabilities teacher [T][k] fp32; p = softmax of scale * teacher over the token's entries, or exp(teacher) as it is.  loss and lse [T]
     fp32, either may be None.  `workspace`: distill_workspace_bytes(...) bytes."""
-    dt, T, V, D, ldx, ldw, k, at, q = _distill(X, W, index, teacher, stream, loss=loss, lse=lse, workspace=workspace)
+    dt, T, V, D, ldx, ldw, k, at, q, st_ptr = _distill(X, W, index, teacher, stream, loss=loss, lse=lse, workspace=workspace)
     ws_ptr, ws_len = _ws(workspace)
     _check(lib.gensor_distill_forward(dt, T, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, scale, k, at, q, 1 if normalize else 0,
                                       None if loss is None else _vector(loss, T, "torch.float32", "loss"),
-                                      None if lse is None else _vector(lse, T, "torch.float32", "lse"), ws_ptr, ws_len, _stream_ptr(stream)), "gensor_distill_forward")
+                                      None if lse is None else _vector(lse, T, "torch.float32", "lse"), ws_ptr, ws_len, st_ptr), "gensor_distill_forward")
 
 
 def distill_backward(X, W, index, teacher, lse, dloss, dX, dW, scale: float = 1.0, normalize: bool = True, stream=None, workspace=None):
     """dX = G W and dW = G^T X with G[t][v] = dloss[t] scale (P exp(z[t][v] - lse[t]) - sum of p_j over index_j == v), P = sum_j p_j; dX or dW may be None.
     `workspace`: distill_workspace_bytes(..., backward=True) bytes, or less for smaller pieces of the vocabulary."""
-    dt, T, V, D, ldx, ldw, k, at, q = _distill(X, W, index, teacher, stream, lse=lse, dloss=dloss, dX=dX, dW=dW, workspace=workspace)
+    dt, T, V, D, ldx, ldw, k, at, q, st_ptr = _distill(X, W, index, teacher, stream, lse=lse, dloss=dloss, dX=dX, dW=dW, workspace=workspace)
     ws_ptr, ws_len = _ws(workspace)
     _check(lib.gensor_distill_backward(dt, T, V, D, X.data_ptr(), ldx, W.data_ptr(), ldw, scale, k, at, q, 1 if normalize else 0,
                                        _vector(lse, T, "torch.float32", "lse"), _vector(dloss, T, "torch.float32", "dloss"),
                                        None if dX is None else dX.data_ptr(), 0 if dX is None else _matrix(dX, T, D, X.dtype, "dX"),
                                        None if dW is None else dW.data_ptr(), 0 if dW is None else _matrix(dW, V, D, X.dtype, "dW"),
-                                       ws_ptr, ws_len, _stream_ptr(stream)), "gensor_distill_backward")
+                                       ws_ptr, ws_len, st_ptr), "gensor_distill_backward")

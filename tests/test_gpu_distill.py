@@ -244,3 +244,31 @@ def test_captured_and_replayed(gs):
         X.neg_()
         graph.replay()
         X.neg_()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_operands_and_gradients_that_start_anywhere(gs, dtype):
+    """Rows of any pitch from any element on; what lies around the gradients stays as it is."""
+    T, V, D, k = 45, 700, 72, 5
+    X, W, index, q = inputs(dtype, T, V, D, k, 0, 31)
+    loss, lse = forward(gs, X, W, index, q)
+    dloss = torch.full((T,), 1.0 / T, device="cuda")
+
+    def placed(rows, first, pad, values=None):
+        flat = torch.full((rows * (D + pad) + 16,), 7.0, device="cuda").to(TORCH[dtype])
+        v = flat.as_strided((rows, D), (D + pad, 1), first)
+        if values is not None:
+            v.copy_(values)
+        return flat, v
+    for first, pad in ((1, 1), (3, 0), (8, 8)):
+        x, w = placed(T, first, pad, X)[1], placed(V, first, pad, W)[1]
+        (flat_x, dX), (flat_w, dW) = placed(T, first, pad), placed(V, first, pad)
+        out, out_lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+        gs.distill_forward(x, w, index, q, out, out_lse, workspace=workspace(gs.distill_workspace_bytes(dtype, T, V, D, k)))
+        check_forward(out, out_lse, reference(X, W, index, q, 1.0, True))
+        gs.distill_backward(x, w, index, q, out_lse, dloss, dX, dW, workspace=workspace(gs.distill_workspace_bytes(dtype, T, V, D, k, backward=True)))
+        check_gradient(dtype, X, W, index, q, 1.0, True, out_lse, dloss, dX, dW)
+        for flat, v in ((flat_x, dX), (flat_w, dW)):
+            rest = torch.ones_like(flat, dtype=torch.bool)
+            rest.as_strided(v.shape, v.stride(), first).fill_(False)
+            assert bool((flat[rest] == 7).all())

@@ -240,3 +240,42 @@ def test_far_matrices_and_long_outputs(gs):
     gs.gated_gemm(gs.gemm_problem("f16", M, N, K, out_dtype="f16"), A, B, C, act="gelu")
     for rows in (slice(0, 300), slice(M - 300, M)):
         check_forward(A[rows], B, None, "gelu", 1.0, "f16", C[rows], None, rows)
+
+
+@pytest.mark.parametrize("dtype,out", [("bf16", "bf16"), ("f16", "f32"), ("f32", "f32")])
+def test_operands_and_results_that_start_anywhere(gs, dtype, out):
+    M, N, K = 70, 90, 136
+    for first, pad in ((1, 0), (3, 1), (2, 2)):
+        def placed(shape, dt, values=None):
+            flat = torch.full((shape[0] * shape[1] * (shape[2] + pad) + 16,), 7.0, device="cuda").to(TORCH[dt])
+            v = flat.as_strided(shape, (shape[1] * (shape[2] + pad), shape[2] + pad, 1), first)
+            if values is not None:
+                v.copy_(values)
+            return v, flat
+        for tb in (0, 1):
+            A, B = placed((1, M, K), dtype, draw((1, M, K), dtype, 1))[0][0], placed((2, N, K) if tb else (2, K, N), dtype, draw((2, N, K) if tb else (2, K, N), dtype, 2, 0.1))[0]
+            (C, flat_c), (Z, flat_z) = placed((1, M, N), out), placed((2, M, N), out)
+            gs.gated_gemm(gs.gemm_problem(dtype, M, N, K, transB=tb, out_dtype=out), A, B, C[0], preact=Z)
+            check_forward(A, B.mT if tb else B, None, "silu", 1.0, out, C[0], Z, (first, pad, tb))
+            D, W = placed((1, M, K), dtype, draw((1, M, K), dtype, 3))[0][0], placed((1, N, K) if tb else (1, K, N), dtype, draw((1, N, K) if tb else (1, K, N), dtype, 4, 0.1))[0][0]
+            (dZ, flat_d), (H, flat_h) = placed((2, M, N), out), placed((1, M, N), out)
+            gs.gated_act_grad(gs.gemm_problem(dtype, M, N, K, transB=tb, out_dtype=out), D, W, Z, dZ, H=H[0])
+            d, e = D.double() @ (W.mT if tb else W).double(), (K + 4) * U * (D.double().abs() @ (W.mT if tb else W).double().abs())
+            g, u = Z[0].double(), Z[1].double()
+            f, e_f = act64(g, "silu"), 16 * U * g.abs()
+            close(dZ[0], d * u * slope64(g, "silu"), 1.13 * e * u.abs() + 64 * U * (d * u).abs(), out, "dG")
+            close(dZ[1], d * f, e * (f.abs() + e_f) + d.abs() * e_f + 2 * U * (d * f).abs(), out, "dU")
+            close(H[0], f * u, e_f * u.abs() + 2 * U * (f * u).abs(), out, "H")
+            for flat, v in ((flat_c, C), (flat_z, Z), (flat_d, dZ), (flat_h, H)):
+                rest = torch.ones_like(flat, dtype=torch.bool)
+                rest.as_strided(v.shape, v.stride(), first).fill_(False)
+                assert bool((flat[rest] == 7).all())
+
+
+def test_one_matrix_for_both_and_no_distance(gs):
+    """strideB = 0: both products are of one matrix."""
+    M, N, K = 33, 48, 64
+    A, B = draw((M, K), "f32", 1), draw((1, N, K), "f32", 2, 0.125).expand(2, N, K)
+    C = torch.empty((M, N), device="cuda")
+    gs.gated_gemm(gs.gemm_problem("f32", M, N, K, transB=1), A, B, C)
+    check_forward(A, B.mT, None, "silu", 1.0, "f32", C, None, "one matrix")

@@ -249,3 +249,32 @@ def test_rows_far_apart(gs):
     far.copy_(X)
     t = targets_for(T, V, 4)
     check(scores(gs, far, W, t, 8), X, W, t, 8)
+
+
+@pytest.mark.parametrize("T,V,D,top", [(1100, 3001, 4, 64), (1500, 30_000, 4, 9), (65, 20_000, 4, 33), (1025, 700, 3, 1)])
+def test_equal_logits_of_many_tokens(gs, T, V, D, top):
+    """More logits reach the bar than there is room for, with one wave a token and with several, in one piece and over many."""
+    X, W = operands("bf16", T, V, D, 13, coarse=True)
+    t = targets_for(T, V, 13)
+    check(scores(gs, X, W, t, top), X, W, t, top)
+    small = gs.logprobs_workspace_bytes("bf16", T, V, D, top) // 3 // 256 * 256
+    check(scores(gs, X, W, t, top, room=small), X, W, t, top)
+    X.zero_()
+    assert torch.equal(scores(gs, X, W, t, top)["top_index"], torch.arange(top, device="cuda").expand(T, top))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "f32"])
+def test_operands_that_start_anywhere(gs, dtype):
+    T, V, D, top = 37, 611, 64, 7
+    X, W = operands(dtype, T, V, D, 21)
+    t = targets_for(T, V, 21)
+    want = scores(gs, X, W, t, top)
+    for first, pad in ((1, 1), (3, 0), (1, 8)):
+        def moved(m):
+            flat = torch.full((m.shape[0] * (D + pad) + 8,), float("nan"), device="cuda").to(m.dtype)
+            v = flat.as_strided(m.shape, (D + pad, 1), first)
+            v.copy_(m)
+            return v
+        out = scores(gs, moved(X), moved(W), t, top)
+        check(out, X, W, t, top)
+        assert torch.equal(out["top_index"], want["top_index"])

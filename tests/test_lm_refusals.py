@@ -112,17 +112,15 @@ def test_binding_checks_shapes_and_types(gs):
 
 
 def test_tensors_of_another_device_are_refused(gs, monkeypatch):
-    import torch
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(gs, "_current", (lambda: 1, lambda device: 100 + device))
 
     class On:
         def __init__(self, n):
-            self.n, self.device, self.device_index = n, f"cuda:{n}", n
+            self.n, self.device, self.device_index, self.cuda_stream = n, f"cuda:{n}", n, 7
 
         def get_device(self):
             return self.n
-    gs._on_current_device(None, A=On(1), B=None)
-    gs._on_current_device(On(1), A=On(1))
+    assert gs._on_current_device(None, A=On(1), B=None) == 101 and gs._on_current_device(On(1), A=On(1)) == 7
     with pytest.raises(ValueError, match="B: "):
         gs._on_current_device(None, A=On(1), B=On(0))
     with pytest.raises(ValueError, match="stream: "):
