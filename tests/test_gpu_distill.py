@@ -272,3 +272,13 @@ def test_operands_and_gradients_that_start_anywhere(gs, dtype):
             rest = torch.ones_like(flat, dtype=torch.bool)
             rest.as_strided(v.shape, v.stride(), first).fill_(False)
             assert bool((flat[rest] == 7).all())
+
+
+def test_more_tokens_than_a_launch_has_workgroups_for(gs):
+    T, V, D, k = 1_100_003, 7, 3, 2
+    X, W, index, q = inputs("f32", T, V, D, k, 0, 41)
+    loss, lse = forward(gs, X, W, index, q)
+    check_forward(loss, lse, reference(X, W, index, q, 1.0, True))
+    dloss = torch.full((T,), 1.0, device="cuda")
+    dX, dW = backward(gs, X, W, index, q, lse, dloss)
+    check_gradient("f32", X, W, index, q, 1.0, True, lse, dloss, dX, dW)

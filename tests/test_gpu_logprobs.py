@@ -278,3 +278,10 @@ def test_operands_that_start_anywhere(gs, dtype):
         out = scores(gs, moved(X), moved(W), t, top)
         check(out, X, W, t, top)
         assert torch.equal(out["top_index"], want["top_index"])
+
+
+def test_more_tokens_than_a_launch_has_workgroups_for(gs):
+    T, V, D, top = 4_300_001, 5, 2, 2
+    X, W = operands("f32", T, V, D, 17)
+    t = targets_for(T, V, 17)
+    check(scores(gs, X, W, t, top), X, W, t, top)
