@@ -284,8 +284,8 @@ __device__ inline float nth_of_lanes(float x, int n) {
 // one token's five, 43 for the twenty of 301 tokens.)  Where more come up than there is room for -- many equal ones -- they are sought one by one: a scan
 // of all that were kept for the largest below the last found.
 //
-// Bound by a chain of loads (parts and maxima, then the sets) and by the vector unit.  us: one token's five of 50257 (16 waves) 8.6, 301 tokens' twenty of
-// 5003 (4 waves; with 16 15.7) 8.3, 4096 tokens' eight (a wave each) 9 to 21 a piece, without alternatives 7.
+// Bound by a chain of loads (parts and maxima, then the sets) and by the vector unit.  us: one token's five of 50257 (8 waves) 6.8, 301 tokens' twenty of
+// 5003 (4 waves) 8.3, 4096 tokens' eight (a wave each) 9 to 21 a piece, without alternatives 7.
 template <int WAVES>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(const AdvanceArgs a) {
   constexpr int TOKENS = WAVES == 1 ? 4 : 1, AHEAD = 8, KEYS = WAVES == 1 ? 512 : 1024, SETS = 512;
@@ -660,8 +660,8 @@ gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, co
     v.logprob = out.logprob;
     v.lse = out.lse;
     v.entropy = out.entropy;
-    // (more waves a token than compute units need do its work over again)
-    if (T <= 64) hipLaunchKernelGGL(advance_kernel<16>, dim3((unsigned)T), dim3(1024), 0, s, v);
+    // (waves do part of the work over again: one token's 6.8 us with 8, 7.1 with 4, 9.0 with 16; 301 tokens' 8.3 with 4, 15.7 with 16)
+    if (T <= 256) hipLaunchKernelGGL(advance_kernel<8>, dim3((unsigned)T), dim3(512), 0, s, v);
     else if (T <= 1024) hipLaunchKernelGGL(advance_kernel<4>, dim3((unsigned)T), dim3(256), 0, s, v);
     else hipLaunchKernelGGL(advance_kernel<1>, dim3(blocks), dim3(256), 0, s, v);
     if (hipGetLastError() != hipSuccess) return GENSOR_ERR_DEVICE;

@@ -285,3 +285,23 @@ def test_more_tokens_than_a_launch_has_workgroups_for(gs):
     X, W = operands("f32", T, V, D, 17)
     t = targets_for(T, V, 17)
     check(scores(gs, X, W, t, top), X, W, t, top)
+
+
+@pytest.mark.parametrize("T", [1, 256, 257, 1024, 1025])
+def test_waves_a_token(gs, T):
+    """On either side of the counts of tokens at which their number of waves changes, in one piece and in several."""
+    V, D, top = 4001, 48, 11
+    X, W = operands("f16", T, V, D, 23)
+    t = targets_for(T, V, 23)
+    n = gs.logprobs_workspace_bytes("f16", T, V, D, top)
+    for room in (n, n // 4 // 256 * 256):
+        check(scores(gs, X, W, t, top, room=room), X, W, t, top)
+
+
+def test_sums_in_pieces_without_alternatives(gs):
+    T, V, D = 300, 9001, 64
+    X, W = operands("bf16", T, V, D, 27)
+    t = targets_for(T, V, 27)
+    n = gs.logprobs_workspace_bytes("bf16", T, V, D, 0)
+    for part in (1.0, 0.5, 0.25):
+        check(scores(gs, X, W, t, 0, 1 / 0.7, room=int(n * part) // 256 * 256), X, W, t, 0, 1 / 0.7)
