@@ -52,7 +52,7 @@ gensor_status gensor_gated_act_grad(const gensor_problem* p, int32_t act, float 
  * wanted with logprob.  A NaN among a token's logits makes its log probabilities and entropy NaN; it is no alternative, and entry -1 stands where fewer than
  * `top` others are.  (An infinite largest logit: lse is that, what is a difference of infinities NaN.)
  * The workspace (256-byte aligned) holds, beside sums, the logits of a piece of the vocabulary that may be among the largest.
- * gensor_logprobs_workspace_bytes asks for what pieces of 256 MiB at most want, for any leading dimensions; with less the pieces are smaller.
+ * gensor_logprobs_workspace_bytes asks for what pieces of 384 MiB at most want, for any leading dimensions; with less the pieces are smaller.
  * WORKSPACE if not even one row of tiles fits.
  */
 #define GENSOR_TOP_MAX 64

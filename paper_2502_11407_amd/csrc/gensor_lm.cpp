@@ -218,6 +218,9 @@ __device__ inline void join_scores(float& top, float& sum, float& rest, float to
   top = both;
 }
 
+// (the last of a part's four values is not used, and not read: its register would be another's before it arrives)
+typedef float f32x3 __attribute__((ext_vector_type(3)));
+
 struct AdvanceArgs {
   const f32x4* parts;              // of this piece
   const float* set_max;
@@ -228,7 +231,7 @@ struct AdvanceArgs {
   float* bar;                      // [tokens]: a later logit is among the largest only above it
   float* values;                   // [tokens][top]: the largest logits so far; log probabilities in the end
   int64_t* index;
-  const int64_t* targets;
+  const int64_t* targets;          // (memory that may be read, too, where logprob is NULL)
   int64_t ignore;
   const float* at_target;
   float *logprob, *lse, *entropy;
@@ -267,26 +270,38 @@ __device__ inline void join_lanes(float& top, float& sum, float& rest) {
   top = all;
 }
 
-// The n'th largest of the lanes' values: the least of those that fewer than n are larger than.
+// The smallest number above a number (NaN above infinity, which no number reaches)
+__device__ inline float next_above(float x) {
+  const uint32_t u = as_u32(x + 0.f);
+  return as_f32(u & 0x80000000u ? u - 1 : u + 1);
+}
+
+// A number that n of the lanes' values reach, the largest with 20 bits (so a little below the n'th largest: another instruction a bit, where
+// counting for each value those above it takes three a lane)
 __device__ inline float nth_of_lanes(float x, int n) {
-  int larger = 0;
-#pragma unroll 8
-  for (int i = 0; i < 64; ++i) larger += as_f32((uint32_t)__builtin_amdgcn_readlane((int)as_u32(x), i)) > x;
-  return over_lanes(larger < n ? x : INFINITY, [](float a, float b) { return fminf(a, b); });
+  const uint32_t key = (uint32_t)(rank_key(x, 0) >> 32);
+  uint32_t found = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 12; --bit) {
+    const uint32_t higher = found | 1u << bit;
+    if ((int)__popcll(__ballot(key >= higher)) >= n) found = higher;
+  }
+  return found > 0x007fffffu ? key_value((uint64_t)found << 32) : -INFINITY;
 }
 
 // WAVES waves per token join a piece's parts to what was joined before, and find the largest logits among the piece's and those so far.
 //
 // The search.  A bar that no more than a few logits reach is known before any is read: what the pieces so far say (the top'th largest, to be
-// exceeded), or in the first piece the top'th largest of 64 maxima of disjoint groups of sets (to be reached).  Sets whose maximum does not reach it hold
-// none of the largest; the logits of the others that reach it, and the largest so far, are gathered in LDS, and each one's place is the number of
-// those above it: no order in which anything is gathered matters.  (Putting them into a sorted list, a lane each, one by one took 0.3 us apiece: 23 us for
-// one token's five, 43 for the twenty of 301 tokens.)  Where more come up than there is room for -- many equal ones -- they are sought one by one: a scan
-// of all that were kept for the largest below the last found.
+// exceeded), and the top'th largest of 64 maxima of disjoint groups of this piece's sets (to be reached; sought only where it is the higher one, mostly in the
+// first two pieces: 4096 tokens' second 21 us without, 12 with).  Sets whose maximum does not reach it hold none of the largest; the logits of the others
+// that reach it, and the largest so far, are gathered in LDS, and each one's place is the number of those above it: no order in which anything is gathered
+// matters.  (Putting them into a sorted list, a lane each, one by one took 0.3 us apiece: 23 us for one token's five, 43 for the twenty of 301 tokens.)
+// Where more come up than there is room for -- many equal ones -- they are sought one by one: a scan of all that were kept for the largest below the last
+// found.
 //
 // Bound by a chain of loads (parts and maxima, then the sets) and by the vector unit.  us: one token's five of 50257 (8 waves) 6.8, 301 tokens' twenty of
 // 5003 (4 waves) 8.3, 4096 tokens' eight (a wave each) 9 to 21 a piece, without alternatives 7.
-template <int WAVES>
+template <int WAVES, bool TOP>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(const AdvanceArgs a) {
   constexpr int TOKENS = WAVES == 1 ? 4 : 1, AHEAD = 8, KEYS = WAVES == 1 ? 512 : 1024, SETS = 512;
   __shared__ float joined[TOKENS][WAVES == 1 ? 1 : 3 * WAVES];
@@ -307,47 +322,57 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
   int own_counts[2] = {0, 0};
   auto places = [&](int which, bool mine) -> int {
     const uint64_t all = __ballot(mine);
+    if (all == 0) return 0;
     const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0u));
     if constexpr (WAVES == 1) {
       const int first = own_counts[which];
       own_counts[which] = first + (int)__popcll(all);
       return first + before;
     }
-    if (all == 0) return 0;
     int first = 0;
     if (lane == 0) first = atomicAdd(&counts[which], (int)__popcll(all));
     return __builtin_amdgcn_readfirstlane(first) + before;
   };
   auto count = [&](int which) { return WAVES == 1 ? own_counts[which] : counts[which]; };
   for (int t = blockIdx.x * TOKENS + (WAVES == 1 ? wave : 0); t < a.tokens; t += gridDim.x * TOKENS) {
-    // everything that is known where to find is asked for first
+    // everything that is known where to find is asked for first, and without a condition: what is not there is replaced afterwards
     const float* set_max = a.set_max + (int64_t)t * a.set_pitch;
     const float* logits = a.logits + (int64_t)t * a.set_pitch * a.set_size;
     float* values = a.values + (int64_t)t * a.top;
     int64_t* index = a.index + (int64_t)t * a.top;
+    const f32x4* parts = a.parts + (int64_t)t * a.slab_pitch;
+    f32x3 p[4];
+    auto ask = [&](int s) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) p[u] = *(const f32x3*)(parts + min(s + 64 * WAVES * u, a.slabs - 1));
+    };
+    ask(64 * part + lane);
+    const f32x3 so_far = *(const f32x3*)(a.state + t);
+    const int64_t target = a.targets[t];
+    const float at_target = a.at_target[t];
     float m[AHEAD], most = -INFINITY, own_value = 0.f, bar = NAN;
     int64_t own_entry = -1;
-    f32x4 so_far = {-INFINITY, 0.f, 0.f, 0.f};
-    if (!a.first) so_far = a.state[t];
-    if (a.top) {
-      if (!a.first) {
-        bar = a.bar[t];
-        if (lane < a.top) {
-          own_value = values[lane];
-          own_entry = index[lane];
-        }
-      }
+    auto ask_sets = [&](int s) {
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        const int s = 64 * (part + WAVES * u) + lane;
-        m[u] = s < a.sets ? set_max[s] : -INFINITY;
-      }
+      for (int u = 0; u < AHEAD; ++u) m[u] = set_max[min(s + 64 * WAVES * u, a.sets - 1)];
+    };
+    auto set_there = [&](int s) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        if (s + 64 * WAVES * u >= a.sets) m[u] = -INFINITY;
+    };
+    if constexpr (TOP) {
+      ask_sets(64 * part + lane);
+      bar = a.bar[t];
+      own_value = values[min(lane, a.top - 1)];
+      own_entry = index[min(lane, a.top - 1)];
     }
     float top = -INFINITY, sum = 0.f, rest = 0.f;
-    for (int s = 64 * part + lane; s < a.slabs; s += 4 * 64 * WAVES) {
-      f32x4 p[4];
+    for (int s0 = 64 * part; s0 < a.slabs; s0 += 4 * 64 * WAVES) {
+      if (s0 != 64 * part) ask(s0 + lane);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) p[u] = s + 64 * WAVES * u < a.slabs ? a.parts[(int64_t)t * a.slab_pitch + s + 64 * WAVES * u] : f32x4{-INFINITY, 0.f, 0.f, 0.f};
+      for (int u = 0; u < 4; ++u)
+        if (s0 + lane + 64 * WAVES * u >= a.slabs) p[u] = f32x3{-INFINITY, 0.f, 0.f};
       // (four parts to one reference)
       const float both = fmaxf(fmaxf(fmaxf(p[0][0], p[1][0]), fmaxf(p[2][0], p[3][0])), top), r = lse_reference(both);
       auto scaled = [&](float part_top, float part_sum, float part_rest, float& to_sum, float& to_rest) {
@@ -361,12 +386,17 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
       for (int u = 0; u < 4; ++u) scaled(p[u][0], p[u][1], p[u][2], new_sum, new_rest);
       top = both; sum = new_sum; rest = new_rest;
     }
+    if constexpr (TOP) {
+      set_there(64 * part + lane);
+      if (a.first || lane >= a.top) own_entry = -1;
+      if (a.first) bar = NAN;
+    }
     join_lanes(top, sum, rest);
     meet();                                                            // (the token before)
     own_counts[0] = own_counts[1] = 0;
     if (WAVES > 1 && threadIdx.x < 2) counts[threadIdx.x] = 0;
     if constexpr (WAVES > 1) {
-      if (a.top) {
+      if constexpr (TOP) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) most = fmaxf(most, m[u]);
         group_max[wave][lane] = most;
@@ -382,13 +412,13 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
       rest = lane < WAVES ? joined[0][3 * lane + 2] : 0.f;
       join_lanes(top, sum, rest);
       most = -INFINITY;
-      if (a.top) {
+      if constexpr (TOP) {
 #pragma unroll
         for (int v = 0; v < WAVES; ++v) most = fmaxf(most, group_max[v][lane]);
       }
     } else {
       meet();
-      if (a.top) {
+      if constexpr (TOP) {
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) most = fmaxf(most, m[u]);
       }
@@ -406,31 +436,28 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
         if (a.lse) a.lse[t] = ref + log_sum;
         if (a.entropy) a.entropy[t] = log_sum - rest / sum;
         if (a.logprob) {
-          const int64_t target = a.targets[t];
           // (the maximum's part first: a target that is the maximum loses log(1 + the others), not a difference of large numbers)
-          a.logprob[t] = target == a.ignore ? 0.f : target >= 0 && target < a.vocab ? (a.at_target[t] - ref) - log_sum : NAN;
+          a.logprob[t] = target == a.ignore ? 0.f : target >= 0 && target < a.vocab ? (at_target - ref) - log_sum : NAN;
         }
       }
     }
-    if (a.top == 0) continue;
+    if constexpr (!TOP) continue;
 
     // ---- sets that reach the bar
-    const float least = bar != bar ? nth_of_lanes(most, a.top) : -INFINITY;
-    auto reaches = [&](float v) { return v >= least && !(v <= bar); };
+    const float least = bar != bar || (int)__popcll(__ballot(most > bar)) >= a.top ? nth_of_lanes(most, a.top) : next_above(bar);
+    auto reaches = [&](float v) { return v >= least; };
     for (int s0 = 64 * part; s0 < a.sets; s0 += 64 * WAVES * AHEAD) {
       if (s0 != 64 * part) {
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) {
-          const int s = s0 + 64 * WAVES * u + lane;
-          m[u] = s < a.sets ? set_max[s] : -INFINITY;
-        }
+        ask_sets(s0 + lane);
+        set_there(s0 + lane);
       }
+      uint32_t hits = 0;
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) {
-        const int s = s0 + 64 * WAVES * u + lane;
-        const bool mine = s < a.sets && reaches(m[u]);
-        const int to = places(0, mine);
-        if (mine && to < SETS) set_list[at][to] = s;
+      for (int u = 0; u < AHEAD; ++u) hits |= reaches(m[u]) && s0 + lane + 64 * WAVES * u < a.sets ? 1u << u : 0u;
+      while (__any(hits != 0)) {
+        const int to = places(0, hits != 0);
+        if (hits != 0 && to < SETS) set_list[at][to] = s0 + lane + 64 * WAVES * __builtin_ctz(hits);
+        hits &= hits - 1;
       }
     }
     // the largest so far
@@ -454,12 +481,12 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
           const int which = j + u * per * WAVES + lane / size;
-          e[u] = -1;
+          e[u] = 0;
           v[u] = which < n_sets ? logit(set_list[at][which], e[u]) : NAN;
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const bool mine = reaches(v[u]) && e[u] >= 0 && e[u] < a.vocab - a.row_first;
+          const bool mine = reaches(v[u]) && e[u] < a.vocab - a.row_first;
           const int to = places(1, mine);
           if (mine && to < KEYS) keys[at][to] = rank_key(v[u], a.row_first + e[u]);
         }
@@ -516,8 +543,9 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
 
 namespace {
 
-// Logits of a piece at most, where the largest are asked for
-const size_t kScoreBytes = (size_t)256 << 20;
+// Logits of a piece at most, where the largest are asked for.  (4096 tokens over 50257 entries, eight alternatives, f16, us: 128 MiB 395, 256 361, 384 350,
+// 512 354, 1024 350.)
+const size_t kScoreBytes = (size_t)384 << 20;
 // ... of which a first piece that may keep them all
 const size_t kHeadBytes = (size_t)32 << 20;
 
@@ -654,16 +682,21 @@ gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, co
     v.bar = bar;
     v.values = out.top_logprob;
     v.index = out.top_index;
-    v.targets = targets;
+    v.targets = out.logprob ? targets : (const int64_t*)state;
     v.ignore = ignore;
     v.at_target = at_target;
     v.logprob = out.logprob;
     v.lse = out.lse;
     v.entropy = out.entropy;
     // (waves do part of the work over again: one token's 6.8 us with 8, 7.1 with 4, 9.0 with 16; 301 tokens' 8.3 with 4, 15.7 with 16)
-    if (T <= 256) hipLaunchKernelGGL(advance_kernel<8>, dim3((unsigned)T), dim3(512), 0, s, v);
-    else if (T <= 1024) hipLaunchKernelGGL(advance_kernel<4>, dim3((unsigned)T), dim3(256), 0, s, v);
-    else hipLaunchKernelGGL(advance_kernel<1>, dim3(blocks), dim3(256), 0, s, v);
+    auto advance = [&](auto with_top) {
+      constexpr bool TOP = decltype(with_top)::value;
+      if (T <= 256) hipLaunchKernelGGL((advance_kernel<8, TOP>), dim3((unsigned)T), dim3(512), 0, s, v);
+      else if (T <= 1024) hipLaunchKernelGGL((advance_kernel<4, TOP>), dim3((unsigned)T), dim3(256), 0, s, v);
+      else hipLaunchKernelGGL((advance_kernel<1, TOP>), dim3(blocks), dim3(256), 0, s, v);
+    };
+    if (out.top) advance(std::true_type{});
+    else advance(std::false_type{});
     if (hipGetLastError() != hipSuccess) return GENSOR_ERR_DEVICE;
   }
   return GENSOR_OK;

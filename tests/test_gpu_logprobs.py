@@ -305,3 +305,17 @@ def test_sums_in_pieces_without_alternatives(gs):
     n = gs.logprobs_workspace_bytes("bf16", T, V, D, 0)
     for part in (1.0, 0.5, 0.25):
         check(scores(gs, X, W, t, 0, 1 / 0.7, room=int(n * part) // 256 * 256), X, W, t, 0, 1 / 0.7)
+
+
+@pytest.mark.parametrize("T", [3, 300, 1500])
+@pytest.mark.parametrize("coarse", [False, True])
+def test_larger_logits_in_later_pieces(gs, T, coarse):
+    """Hundreds of a later piece's logits are above the largest so far, among them many equal ones."""
+    V, D, top = 8003, 16, 9
+    X, W = operands("bf16", T, V, D, 31, coarse=coarse)
+    W[V // 4:] *= 4
+    W[3 * V // 4:] *= 2
+    t = targets_for(T, V, 31)
+    n = gs.logprobs_workspace_bytes("bf16", T, V, D, top)
+    for room in (n, n // 5 // 256 * 256, n // 12 // 256 * 256):
+        check(scores(gs, X, W, t, top, room=room), X, W, t, top)
