@@ -303,7 +303,7 @@ __device__ inline float nth_of_lanes(float x, int n) {
 // 5003 (4 waves) 8.3, 4096 tokens' eight (a wave each) 9 to 21 a piece, without alternatives 7.
 template <int WAVES, bool TOP>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(const AdvanceArgs a) {
-  constexpr int TOKENS = WAVES == 1 ? 4 : 1, AHEAD = 8, KEYS = WAVES == 1 ? 512 : 1024, SETS = 512;
+  constexpr int TOKENS = WAVES == 1 ? 4 : 1, AHEAD = WAVES == 1 ? 12 : 8, KEYS = WAVES == 1 ? 512 : 1024, SETS = 512;
   __shared__ float joined[TOKENS][WAVES == 1 ? 1 : 3 * WAVES];
   __shared__ float group_max[WAVES == 1 ? 1 : WAVES][64];
   __shared__ int set_list[TOKENS][SETS];
@@ -628,13 +628,16 @@ gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, co
     if (piece <= d.bm) return GENSOR_ERR_WORKSPACE;
     piece = std::max<int64_t>(1, piece / 2 / d.bm) * d.bm;
   }
-  const ScorePlan pl = score_plan(d, T, piece, out.top);
   // Nothing is known of the first piece's logits, so all of them are kept: it is one round of tiles, after which few are above a token's bar.
   int64_t rows = piece;
-  if (out.top && piece * T * 4 > (int64_t)kHeadBytes) {
-    const int64_t tiles_n = (T + d.bn - 1) / d.bn, round = gensor_hw_mi355x()->compute_units;
-    rows = std::min(piece, std::max<int64_t>(1, round / tiles_n) * d.bm);
+  if (out.top) {
+    const int64_t tiles_n = (T + d.bn - 1) / d.bn, units = gensor_hw_mi355x()->compute_units;
+    if (piece * T * 4 > (int64_t)kHeadBytes) rows = std::min(piece, std::max<int64_t>(1, units / tiles_n) * d.bm);
+    // The others are whole rounds, where that makes them no more: a launch's last round leaves units idle.  (3000 tokens over 50257 entries 265 us without, 246 with.)
+    const int64_t whole = piece / d.bm * tiles_n / units * units / tiles_n * d.bm, rest = V - rows;
+    if (whole > 0 && (rest + whole - 1) / whole == (rest + piece - 1) / piece) piece = whole;
   }
+  const ScorePlan pl = score_plan(d, T, std::max(rows, piece), out.top);
   char* at = (char*)workspace;
   f32x4* state = (f32x4*)at;
   float* bar = (float*)(at + round_up((size_t)T * 16, 256));
@@ -693,6 +696,7 @@ gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, co
       constexpr bool TOP = decltype(with_top)::value;
       if (T <= 256) hipLaunchKernelGGL((advance_kernel<8, TOP>), dim3((unsigned)T), dim3(512), 0, s, v);
       else if (T <= 1024) hipLaunchKernelGGL((advance_kernel<4, TOP>), dim3((unsigned)T), dim3(256), 0, s, v);
+      else if (T <= 2048) hipLaunchKernelGGL((advance_kernel<2, TOP>), dim3((unsigned)T), dim3(128), 0, s, v);
       else hipLaunchKernelGGL((advance_kernel<1, TOP>), dim3(blocks), dim3(256), 0, s, v);
     };
     if (out.top) advance(std::true_type{});
