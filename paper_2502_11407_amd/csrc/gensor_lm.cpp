@@ -276,15 +276,21 @@ __device__ inline float next_above(float x) {
   return as_f32(u & 0x80000000u ? u - 1 : u + 1);
 }
 
-// A number that n of the lanes' values reach, the largest with 20 bits (so a little below the n'th largest: another instruction a bit, where
-// counting for each value those above it takes three a lane)
-__device__ inline float nth_of_lanes(float x, int n) {
-  const uint32_t key = (uint32_t)(rank_key(x, 0) >> 32);
+// A number that n of the lanes' values (COUNT each) reach, the largest with 20 bits (so a little below the n'th largest: an instruction or two a bit,
+// where counting for each value those above it takes three a lane)
+template <int COUNT>
+__device__ inline float nth_of_lanes(const float (&x)[COUNT], int n) {
+  uint32_t key[COUNT];
+#pragma unroll
+  for (int c = 0; c < COUNT; ++c) key[c] = (uint32_t)(rank_key(x[c], 0) >> 32);
   uint32_t found = 0;
 #pragma unroll
   for (int bit = 31; bit >= 12; --bit) {
     const uint32_t higher = found | 1u << bit;
-    if ((int)__popcll(__ballot(key >= higher)) >= n) found = higher;
+    int reach = 0;
+#pragma unroll
+    for (int c = 0; c < COUNT; ++c) reach += (int)__popcll(__ballot(key[c] >= higher));
+    if (reach >= n) found = higher;
   }
   return found > 0x007fffffu ? key_value((uint64_t)found << 32) : -INFINITY;
 }
@@ -296,20 +302,19 @@ __device__ inline float nth_of_lanes(float x, int n) {
 // first two pieces: 4096 tokens' second 21 us without, 12 with).  Sets whose maximum does not reach it hold none of the largest; the logits of the others
 // that reach it, and the largest so far, are gathered in LDS, and each one's place is the number of those above it: no order in which anything is gathered
 // matters.  (Putting them into a sorted list, a lane each, one by one took 0.3 us apiece: 23 us for one token's five, 43 for the twenty of 301 tokens.)
-// Where more come up than there is room for -- many equal ones -- they are sought one by one: a scan of all that were kept for the largest below the last
-// found.
+// Where more come up than there is room for -- many equal ones, as of a padded batch's tokens of zeros -- all that were kept are looked through in their
+// order.
 //
 // Bound by a chain of loads (parts and maxima, then the sets) and by the vector unit.  us: one token's five of 50257 (8 waves) 6.8, 301 tokens' twenty of
 // 5003 (4 waves) 8.3, 4096 tokens' eight (a wave each) 9 to 21 a piece, without alternatives 7.
 template <int WAVES, bool TOP>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(const AdvanceArgs a) {
-  constexpr int TOKENS = WAVES == 1 ? 4 : 1, AHEAD = WAVES == 1 ? 12 : 8, KEYS = WAVES == 1 ? 512 : 1024, SETS = 512;
+  constexpr int TOKENS = WAVES == 1 ? 4 : 1, AHEAD = WAVES == 1 ? 12 : 8, KEYS = WAVES == 1 ? 512 : 1024, SETS = 512, GROUPS = 4;
   __shared__ float joined[TOKENS][WAVES == 1 ? 1 : 3 * WAVES];
   __shared__ float group_max[WAVES == 1 ? 1 : WAVES][64];
   __shared__ int set_list[TOKENS][SETS];
   __shared__ uint64_t keys[TOKENS][KEYS];
   __shared__ int counts[2];
-  __shared__ uint64_t found[WAVES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = WAVES == 1 ? 0 : wave, at = WAVES == 1 ? wave : 0;
   auto meet = [&]() {
     if constexpr (WAVES > 1) __syncthreads();
@@ -350,8 +355,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
     const f32x3 so_far = *(const f32x3*)(a.state + t);
     const int64_t target = a.targets[t];
     const float at_target = a.at_target[t];
-    float m[AHEAD], most = -INFINITY, own_value = 0.f, bar = NAN;
+    float m[AHEAD], most[GROUPS], own_value = 0.f, bar = NAN;
     int64_t own_entry = -1;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) most[g] = -INFINITY;
     auto ask_sets = [&](int s) {
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u) m[u] = set_max[min(s + 64 * WAVES * u, a.sets - 1)];
@@ -388,6 +395,10 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
     }
     if constexpr (TOP) {
       set_there(64 * part + lane);
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) most[u % GROUPS] = fmaxf(most[u % GROUPS], m[u]);
+#pragma unroll 4
+      for (int s = 64 * (part + WAVES * AHEAD) + lane; s < a.sets; s += 64 * WAVES) most[0] = fmaxf(most[0], set_max[s]);
       if (a.first || lane >= a.top) own_entry = -1;
       if (a.first) bar = NAN;
     }
@@ -397,9 +408,7 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
     if (WAVES > 1 && threadIdx.x < 2) counts[threadIdx.x] = 0;
     if constexpr (WAVES > 1) {
       if constexpr (TOP) {
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) most = fmaxf(most, m[u]);
-        group_max[wave][lane] = most;
+        group_max[wave][lane] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
       }
       if (lane == 0) {
         joined[0][3 * wave] = top;
@@ -411,17 +420,14 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
       sum = lane < WAVES ? joined[0][3 * lane + 1] : 0.f;
       rest = lane < WAVES ? joined[0][3 * lane + 2] : 0.f;
       join_lanes(top, sum, rest);
-      most = -INFINITY;
       if constexpr (TOP) {
 #pragma unroll
-        for (int v = 0; v < WAVES; ++v) most = fmaxf(most, group_max[v][lane]);
+        for (int g = 0; g < GROUPS; ++g) most[g] = -INFINITY;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v) most[v % GROUPS] = fmaxf(most[v % GROUPS], group_max[v][lane]);
       }
     } else {
       meet();
-      if constexpr (TOP) {
-#pragma unroll
-        for (int u = 0; u < AHEAD; ++u) most = fmaxf(most, m[u]);
-      }
     }
     if (!a.first) {
       float x = so_far[0], y = so_far[1], z = so_far[2];
@@ -444,7 +450,18 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
     if constexpr (!TOP) continue;
 
     // ---- sets that reach the bar
-    const float least = bar != bar || (int)__popcll(__ballot(most > bar)) >= a.top ? nth_of_lanes(most, a.top) : next_above(bar);
+    // (many are sought among more groups, of which fewer hold two of them)
+    float least = next_above(bar);
+    if (a.top > 24) {
+      int above = 0;
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) above += (int)__popcll(__ballot(most[g] > bar));
+      if (bar != bar || above >= a.top) least = nth_of_lanes(most, a.top);
+    } else {
+#pragma unroll
+      for (int g = 1; g < GROUPS; ++g) most[0] = fmaxf(most[0], most[g]);
+      if (bar != bar || (int)__popcll(__ballot(most[0] > bar)) >= a.top) least = nth_of_lanes<1>({most[0]}, a.top);
+    }
     auto reaches = [&](float v) { return v >= least; };
     for (int s0 = 64 * part; s0 < a.sets; s0 += 64 * WAVES * AHEAD) {
       if (s0 != 64 * part) {
@@ -510,32 +527,82 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
       for (int i = n + 64 * part + lane; i < a.top; i += 64 * WAVES) put(i, 0);
       continue;
     }
-    // ---- too many: the largest below the last found, over all sets that were kept, and so on.  
-    uint64_t last = ~0ull;
-    for (int r = 0; r < a.top; ++r) {
-      uint64_t best = own_key < last ? own_key : 0;
-      for (int s = part * per; s < a.sets; s += per * WAVES) {
-        const int set = s + lane / size;
-        if (set >= a.sets || set_max[set] <= bar) continue;
-        int entry;
-        const float v = logit(set, entry);
-        if (v != v || entry >= a.vocab - a.row_first) continue;
-        const uint64_t key = rank_key(v, a.row_first + entry);
-        if (key < last && key > best) best = key;
+    // ---- too many: set after set in the order of their entries, and as often as there might be no room for more, those that are not among the largest
+    // go, after which only larger logits are taken (an equal one's entry is higher)
+    constexpr int ROOM = (KEYS - GENSOR_TOP_MAX) / (64 * WAVES), AT_ONCE = ROOM < 4 ? ROOM : 4, OWN = KEYS / (64 * WAVES);
+    static_assert(AT_ONCE >= 1 && OWN >= 1, "room for what is looked at together");
+    auto only_largest = [&](int m) -> int {
+      uint64_t own[OWN];
+      int rank[OWN];
+#pragma unroll
+      for (int k = 0; k < OWN; ++k) {
+        const int i = 64 * (part + WAVES * k) + lane;
+        own[k] = i < m ? keys[at][i] : 0;
+        rank[k] = 0;
       }
-      for (int d = 32; d >= 1; d /= 2) {
-        const uint64_t other = __shfl_xor((unsigned long long)best, d, 64);
-        best = other > best ? other : best;
+#pragma unroll 8
+      for (int o = 0; o < m; ++o) {
+        const uint64_t other = keys[at][o];
+#pragma unroll
+        for (int k = 0; k < OWN; ++k) rank[k] += other > own[k];
       }
-      if constexpr (WAVES > 1) {
-        if (lane == 0) found[wave] = best;
-        meet();
-        for (int w = 0; w < WAVES; ++w) best = found[w] > best ? found[w] : best;
-        meet();
-      }
-      if (part == 0 && lane == 0) put(r, best);
-      last = best;
+      meet();
+      const int left = min(m, a.top);
+#pragma unroll
+      for (int k = 0; k < OWN; ++k)
+        if (own[k] && rank[k] < left) keys[at][rank[k]] = own[k];
+      own_counts[1] = left;
+      if (WAVES > 1 && threadIdx.x == 0) counts[1] = left;
+      meet();
+      return left;
+    };
+    meet();                                                            // (everyone has read the counts)
+    own_counts[1] = 0;
+    if (WAVES > 1 && threadIdx.x == 0) counts[1] = 0;
+    meet();
+    if (!a.first && part == 0) {
+      const int to = places(1, own_key != 0);
+      if (own_key) keys[at][to] = own_key;
     }
+    float taken = least;
+    constexpr int CHUNK = 64 * WAVES;
+    for (int c0 = 0; c0 < a.sets; c0 += CHUNK) {
+      // (sets none of which holds one are passed over together)
+      const int own_set = c0 + 64 * part + lane;
+      const float own_max = own_set < a.sets ? set_max[own_set] : NAN;
+      auto some = [&]() { return WAVES > 1 ? __syncthreads_or(own_max >= taken) != 0 : __any(own_max >= taken) != 0; };
+      if (!some()) continue;
+      for (int s0 = c0; s0 < min(c0 + CHUNK, a.sets); s0 += AT_ONCE * per * WAVES) {
+        meet();
+        const int so_many = count(1);
+        meet();
+        if (so_many > KEYS - AT_ONCE * 64 * WAVES) {
+          only_largest(so_many);                                       // (more than GENSOR_TOP_MAX: `top` are left)
+          const float next = next_above(key_value(keys[at][a.top - 1]));
+          if (!(next <= taken)) taken = next;
+          if (!some()) break;
+        }
+        float v[AT_ONCE];
+        int e[AT_ONCE];
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+          const int set = s0 + (part + u * WAVES) * per + lane / size;
+          e[u] = 0;
+          v[u] = set < min(c0 + CHUNK, a.sets) && set_max[set] >= taken ? logit(set, e[u]) : NAN;
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u) {
+          const bool mine = v[u] >= taken && e[u] < a.vocab - a.row_first;
+          const int to = places(1, mine);
+          if (mine) keys[at][to] = rank_key(v[u], a.row_first + e[u]);
+        }
+      }
+    }
+    meet();
+    const int so_many = count(1);
+    meet();
+    const int left = only_largest(so_many);
+    for (int i = 64 * part + lane; i < a.top; i += 64 * WAVES) put(i, i < left ? keys[at][i] : 0);
   }
 }
 

@@ -319,3 +319,45 @@ def test_larger_logits_in_later_pieces(gs, T, coarse):
     n = gs.logprobs_workspace_bytes("bf16", T, V, D, top)
     for room in (n, n // 5 // 256 * 256, n // 12 // 256 * 256):
         check(scores(gs, X, W, t, top, room=room), X, W, t, top)
+
+
+@pytest.mark.parametrize("T,V", [(1, 40_001), (6, 9001), (300, 9001), (1200, 40_001), (2200, 20_011)])
+@pytest.mark.parametrize("top", [8, 25, 64])
+@pytest.mark.parametrize("order", ["padded", "rising", "falling"])
+def test_many_candidates(gs, T, V, top, order):
+    """More logits than there is room for reach any bar that is known beforehand: a padded batch's tokens of zeros, whose logits are all equal, and
+    logits in the order of their entries, with equal ones among them."""
+    D = 16
+    X, W = operands("bf16", T, V, D, 33)
+    if order == "padded":
+        X[T // 2:] = 0
+    else:
+        X = torch.ones_like(X)
+        rank = torch.arange(V, device="cuda") if order == "rising" else torch.arange(V, device="cuda").flip(0)
+        W = torch.zeros((V, D), device="cuda")
+        W[:, 0], W[:, 1] = (rank // 512) / 16.0, (rank % 512 // 2) / 4096.0
+        W = W.bfloat16()
+    t = targets_for(T, V, 33)
+    n = gs.logprobs_workspace_bytes("bf16", T, V, D, top)
+    for room in (n, n // 7 // 256 * 256):
+        check(scores(gs, X, W, t, top, room=room), X, W, t, top)
+
+
+@pytest.mark.parametrize("T", [2, 1100])
+def test_infinite_logits_among_many_equal(gs, T):
+    """Hundreds of logits are plus infinity, or minus infinity, or NaN: the lowest of the equal entries, and -1 where no other is left."""
+    V, D, top = 5003, 8, 40
+    X, W = torch.zeros((T, D), device="cuda"), torch.zeros((V, D), device="cuda")
+    X[:, 0] = 1.0
+    W[1::2, 0] = math.inf
+    for rest in (0.0, -math.inf, math.nan):
+        W[0::2, 0] = rest
+        out = scores(gs, X, W, targets_for(T, V, 5), top)
+        assert torch.equal(out["top_index"], torch.arange(1, 2 * top, 2, device="cuda").expand(T, top))
+    W.fill_(math.nan)
+    W[7::1000] = 0.0
+    W[7::1000, 0] = -math.inf
+    out = scores(gs, X, W, targets_for(T, V, 5), top)
+    want = torch.full((top,), -1, device="cuda")
+    want[:5] = torch.arange(7, V, 1000, device="cuda")[:5]
+    assert torch.equal(out["top_index"], want.expand(T, top))
