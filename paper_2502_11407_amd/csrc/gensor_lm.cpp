@@ -226,7 +226,7 @@ struct AdvanceArgs {
   const float* set_max;
   const float* logits;
   int32_t slabs, slab_pitch, sets, set_pitch, set_size;
-  int32_t tokens, row_first, vocab, top, first, last;
+  int32_t token_first, tokens, row_first, vocab, top, first, last;
   f32x4* state;                    // [tokens]: joined so far
   float* bar;                      // [tokens]: a later logit is among the largest only above it
   float* values;                   // [tokens][top]: the largest logits so far; log probabilities in the end
@@ -339,271 +339,269 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
     return __builtin_amdgcn_readfirstlane(first) + before;
   };
   auto count = [&](int which) { return WAVES == 1 ? own_counts[which] : counts[which]; };
-  for (int t = blockIdx.x * TOKENS + (WAVES == 1 ? wave : 0); t < a.tokens; t += gridDim.x * TOKENS) {
-    // everything that is known where to find is asked for first, and without a condition: what is not there is replaced afterwards
-    const float* set_max = a.set_max + (int64_t)t * a.set_pitch;
-    const float* logits = a.logits + (int64_t)t * a.set_pitch * a.set_size;
-    float* values = a.values + (int64_t)t * a.top;
-    int64_t* index = a.index + (int64_t)t * a.top;
-    const f32x4* parts = a.parts + (int64_t)t * a.slab_pitch;
-    f32x3 p[4];
-    auto ask = [&](int s) {
+  const int t = a.token_first + blockIdx.x * TOKENS + (WAVES == 1 ? wave : 0);
+  if (t >= a.tokens) return;
+  // everything that is known where to find is asked for first, and without a condition: what is not there is replaced afterwards
+  const float* set_max = a.set_max + (int64_t)t * a.set_pitch;
+  const float* logits = a.logits + (int64_t)t * a.set_pitch * a.set_size;
+  float* values = a.values + (int64_t)t * a.top;
+  int64_t* index = a.index + (int64_t)t * a.top;
+  const f32x4* parts = a.parts + (int64_t)t * a.slab_pitch;
+  f32x3 p[4];
+  auto ask = [&](int s) {
 #pragma unroll
-      for (int u = 0; u < 4; ++u) p[u] = *(const f32x3*)(parts + min(s + 64 * WAVES * u, a.slabs - 1));
-    };
-    ask(64 * part + lane);
-    const f32x3 so_far = *(const f32x3*)(a.state + t);
-    const int64_t target = a.targets[t];
-    const float at_target = a.at_target[t];
-    float m[AHEAD], most[GROUPS], own_value = 0.f, bar = NAN;
-    int64_t own_entry = -1;
+    for (int u = 0; u < 4; ++u) p[u] = *(const f32x3*)(parts + min(s + 64 * WAVES * u, a.slabs - 1));
+  };
+  ask(64 * part + lane);
+  const f32x3 so_far = *(const f32x3*)(a.state + t);
+  const int64_t target = a.targets[t];
+  const float at_target = a.at_target[t];
+  float m[AHEAD], most[GROUPS], own_value = 0.f, bar = NAN;
+  int64_t own_entry = -1;
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g) most[g] = -INFINITY;
-    auto ask_sets = [&](int s) {
+  for (int g = 0; g < GROUPS; ++g) most[g] = -INFINITY;
+  auto ask_sets = [&](int s) {
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) m[u] = set_max[min(s + 64 * WAVES * u, a.sets - 1)];
-    };
-    auto set_there = [&](int s) {
+    for (int u = 0; u < AHEAD; ++u) m[u] = set_max[min(s + 64 * WAVES * u, a.sets - 1)];
+  };
+  auto set_there = [&](int s) {
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u)
-        if (s + 64 * WAVES * u >= a.sets) m[u] = -INFINITY;
-    };
-    if constexpr (TOP) {
-      ask_sets(64 * part + lane);
-      bar = a.bar[t];
-      own_value = values[min(lane, a.top - 1)];
-      own_entry = index[min(lane, a.top - 1)];
-    }
-    float top = -INFINITY, sum = 0.f, rest = 0.f;
-    for (int s0 = 64 * part; s0 < a.slabs; s0 += 4 * 64 * WAVES) {
-      if (s0 != 64 * part) ask(s0 + lane);
-#pragma unroll
-      for (int u = 0; u < 4; ++u)
-        if (s0 + lane + 64 * WAVES * u >= a.slabs) p[u] = f32x3{-INFINITY, 0.f, 0.f};
-      // (four parts to one reference)
-      const float both = fmaxf(fmaxf(fmaxf(p[0][0], p[1][0]), fmaxf(p[2][0], p[3][0])), top), r = lse_reference(both);
-      auto scaled = [&](float part_top, float part_sum, float part_rest, float& to_sum, float& to_rest) {
-        const float d = fabsf(part_top) == INFINITY ? 0.f : part_top - r, f = __builtin_amdgcn_exp2f(1.44269504088896340736f * d);
-        to_rest += f > 0.f ? f * fmaf(part_sum, d, part_rest) : 0.f;
-        to_sum += part_sum * f;
-      };
-      float new_sum = 0.f, new_rest = 0.f;
-      scaled(top, sum, rest, new_sum, new_rest);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) scaled(p[u][0], p[u][1], p[u][2], new_sum, new_rest);
-      top = both; sum = new_sum; rest = new_rest;
-    }
-    if constexpr (TOP) {
-      set_there(64 * part + lane);
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) most[u % GROUPS] = fmaxf(most[u % GROUPS], m[u]);
-#pragma unroll 4
-      for (int s = 64 * (part + WAVES * AHEAD) + lane; s < a.sets; s += 64 * WAVES) most[0] = fmaxf(most[0], set_max[s]);
-      if (a.first || lane >= a.top) own_entry = -1;
-      if (a.first) bar = NAN;
-    }
-    join_lanes(top, sum, rest);
-    meet();                                                            // (the token before)
-    own_counts[0] = own_counts[1] = 0;
-    if (WAVES > 1 && threadIdx.x < 2) counts[threadIdx.x] = 0;
-    if constexpr (WAVES > 1) {
-      if constexpr (TOP) {
-        group_max[wave][lane] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-      }
-      if (lane == 0) {
-        joined[0][3 * wave] = top;
-        joined[0][3 * wave + 1] = sum;
-        joined[0][3 * wave + 2] = rest;
-      }
-      meet();
-      top = lane < WAVES ? joined[0][3 * lane] : -INFINITY;
-      sum = lane < WAVES ? joined[0][3 * lane + 1] : 0.f;
-      rest = lane < WAVES ? joined[0][3 * lane + 2] : 0.f;
-      join_lanes(top, sum, rest);
-      if constexpr (TOP) {
-#pragma unroll
-        for (int g = 0; g < GROUPS; ++g) most[g] = -INFINITY;
-#pragma unroll
-        for (int v = 0; v < WAVES; ++v) most[v % GROUPS] = fmaxf(most[v % GROUPS], group_max[v][lane]);
-      }
-    } else {
-      meet();
-    }
-    if (!a.first) {
-      float x = so_far[0], y = so_far[1], z = so_far[2];
-      join_scores(x, y, z, top, sum, rest);
-      top = x; sum = y; rest = z;
-    }
-    const float ref = lse_reference(top), log_sum = logf(sum);
-    if (part == 0 && lane == 0) {
-      if (!a.last) {
-        a.state[t] = f32x4{top, sum, rest, 0.f};
-      } else {
-        if (a.lse) a.lse[t] = ref + log_sum;
-        if (a.entropy) a.entropy[t] = log_sum - rest / sum;
-        if (a.logprob) {
-          // (the maximum's part first: a target that is the maximum loses log(1 + the others), not a difference of large numbers)
-          a.logprob[t] = target == a.ignore ? 0.f : target >= 0 && target < a.vocab ? (at_target - ref) - log_sum : NAN;
-        }
-      }
-    }
-    if constexpr (!TOP) continue;
-
-    // ---- sets that reach the bar
-    // (many are sought among more groups, of which fewer hold two of them)
-    float least = next_above(bar);
-    if (a.top > 24) {
-      int above = 0;
-#pragma unroll
-      for (int g = 0; g < GROUPS; ++g) above += (int)__popcll(__ballot(most[g] > bar));
-      if (bar != bar || above >= a.top) least = nth_of_lanes(most, a.top);
-    } else {
-#pragma unroll
-      for (int g = 1; g < GROUPS; ++g) most[0] = fmaxf(most[0], most[g]);
-      if (bar != bar || (int)__popcll(__ballot(most[0] > bar)) >= a.top) least = nth_of_lanes<1>({most[0]}, a.top);
-    }
-    auto reaches = [&](float v) { return v >= least; };
-    for (int s0 = 64 * part; s0 < a.sets; s0 += 64 * WAVES * AHEAD) {
-      if (s0 != 64 * part) {
-        ask_sets(s0 + lane);
-        set_there(s0 + lane);
-      }
-      uint32_t hits = 0;
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) hits |= reaches(m[u]) && s0 + lane + 64 * WAVES * u < a.sets ? 1u << u : 0u;
-      while (__any(hits != 0)) {
-        const int to = places(0, hits != 0);
-        if (hits != 0 && to < SETS) set_list[at][to] = s0 + lane + 64 * WAVES * __builtin_ctz(hits);
-        hits &= hits - 1;
-      }
-    }
-    // the largest so far
-    const uint64_t own_key = own_entry >= 0 ? rank_key(own_value, (int)own_entry) : 0;
-    if (!a.first && part == 0) {
-      const int to = places(1, own_key != 0);
-      if (own_key) keys[at][to] = own_key;
-    }
-    meet();
-    // ---- their logits that reach it
-    const int size = a.set_size, per = 64 / size;                      // sets that a wave looks at together
-    auto logit = [&](int set, int& entry) -> float {
-      entry = set * size + lane % size;
-      return logits[(int64_t)set * size + lane % size];
-    };
-    const int n_sets = count(0);
-    if (n_sets <= SETS) {
-      for (int j = part * per; j < n_sets; j += 4 * per * WAVES) {
-        float v[4];
-        int e[4];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const int which = j + u * per * WAVES + lane / size;
-          e[u] = 0;
-          v[u] = which < n_sets ? logit(set_list[at][which], e[u]) : NAN;
-        }
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          const bool mine = reaches(v[u]) && e[u] < a.vocab - a.row_first;
-          const int to = places(1, mine);
-          if (mine && to < KEYS) keys[at][to] = rank_key(v[u], a.row_first + e[u]);
-        }
-      }
-    }
-    meet();
-    const int n = count(1);
-    auto put = [&](int rank, uint64_t key) {
-      index[rank] = key ? (int64_t)key_entry(key) : -1;
-      values[rank] = !key ? NAN : a.last ? (key_value(key) - ref) - log_sum : key_value(key);
-      if (rank == a.top - 1 && !a.last) a.bar[t] = key ? key_value(key) : NAN;
-    };
-    if (n_sets <= SETS && n <= KEYS) {
-      for (int i = 64 * part + lane; i < n; i += 64 * WAVES) {
-        const uint64_t own = keys[at][i];
-        int rank = 0;
-#pragma unroll 4
-        for (int o = 0; o < n; ++o) rank += keys[at][o] > own;
-        if (rank < a.top) put(rank, own);
-      }
-      for (int i = n + 64 * part + lane; i < a.top; i += 64 * WAVES) put(i, 0);
-      continue;
-    }
-    // ---- too many: set after set in the order of their entries, and as often as there might be no room for more, those that are not among the largest
-    // go, after which only larger logits are taken (an equal one's entry is higher)
-    constexpr int ROOM = (KEYS - GENSOR_TOP_MAX) / (64 * WAVES), AT_ONCE = ROOM < 4 ? ROOM : 4, OWN = KEYS / (64 * WAVES);
-    static_assert(AT_ONCE >= 1 && OWN >= 1, "room for what is looked at together");
-    auto only_largest = [&](int m) -> int {
-      uint64_t own[OWN];
-      int rank[OWN];
-#pragma unroll
-      for (int k = 0; k < OWN; ++k) {
-        const int i = 64 * (part + WAVES * k) + lane;
-        own[k] = i < m ? keys[at][i] : 0;
-        rank[k] = 0;
-      }
-#pragma unroll 8
-      for (int o = 0; o < m; ++o) {
-        const uint64_t other = keys[at][o];
-#pragma unroll
-        for (int k = 0; k < OWN; ++k) rank[k] += other > own[k];
-      }
-      meet();
-      const int left = min(m, a.top);
-#pragma unroll
-      for (int k = 0; k < OWN; ++k)
-        if (own[k] && rank[k] < left) keys[at][rank[k]] = own[k];
-      own_counts[1] = left;
-      if (WAVES > 1 && threadIdx.x == 0) counts[1] = left;
-      meet();
-      return left;
-    };
-    meet();                                                            // (everyone has read the counts)
-    own_counts[1] = 0;
-    if (WAVES > 1 && threadIdx.x == 0) counts[1] = 0;
-    meet();
-    if (!a.first && part == 0) {
-      const int to = places(1, own_key != 0);
-      if (own_key) keys[at][to] = own_key;
-    }
-    float taken = least;
-    constexpr int CHUNK = 64 * WAVES;
-    for (int c0 = 0; c0 < a.sets; c0 += CHUNK) {
-      // (sets none of which holds one are passed over together)
-      const int own_set = c0 + 64 * part + lane;
-      const float own_max = own_set < a.sets ? set_max[own_set] : NAN;
-      auto some = [&]() { return WAVES > 1 ? __syncthreads_or(own_max >= taken) != 0 : __any(own_max >= taken) != 0; };
-      if (!some()) continue;
-      for (int s0 = c0; s0 < min(c0 + CHUNK, a.sets); s0 += AT_ONCE * per * WAVES) {
-        meet();
-        const int so_many = count(1);
-        meet();
-        if (so_many > KEYS - AT_ONCE * 64 * WAVES) {
-          only_largest(so_many);                                       // (more than GENSOR_TOP_MAX: `top` are left)
-          const float next = next_above(key_value(keys[at][a.top - 1]));
-          if (!(next <= taken)) taken = next;
-          if (!some()) break;
-        }
-        float v[AT_ONCE];
-        int e[AT_ONCE];
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-          const int set = s0 + (part + u * WAVES) * per + lane / size;
-          e[u] = 0;
-          v[u] = set < min(c0 + CHUNK, a.sets) && set_max[set] >= taken ? logit(set, e[u]) : NAN;
-        }
-#pragma unroll
-        for (int u = 0; u < AT_ONCE; ++u) {
-          const bool mine = v[u] >= taken && e[u] < a.vocab - a.row_first;
-          const int to = places(1, mine);
-          if (mine) keys[at][to] = rank_key(v[u], a.row_first + e[u]);
-        }
-      }
-    }
-    meet();
-    const int so_many = count(1);
-    meet();
-    const int left = only_largest(so_many);
-    for (int i = 64 * part + lane; i < a.top; i += 64 * WAVES) put(i, i < left ? keys[at][i] : 0);
+    for (int u = 0; u < AHEAD; ++u)
+      if (s + 64 * WAVES * u >= a.sets) m[u] = -INFINITY;
+  };
+  if constexpr (TOP) {
+    ask_sets(64 * part + lane);
+    bar = a.bar[t];
+    own_value = values[min(lane, a.top - 1)];
+    own_entry = index[min(lane, a.top - 1)];
   }
+  float top = -INFINITY, sum = 0.f, rest = 0.f;
+  for (int s0 = 64 * part; s0 < a.slabs; s0 += 4 * 64 * WAVES) {
+    if (s0 != 64 * part) ask(s0 + lane);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (s0 + lane + 64 * WAVES * u >= a.slabs) p[u] = f32x3{-INFINITY, 0.f, 0.f};
+    // (four parts to one reference)
+    const float both = fmaxf(fmaxf(fmaxf(p[0][0], p[1][0]), fmaxf(p[2][0], p[3][0])), top), r = lse_reference(both);
+    auto scaled = [&](float part_top, float part_sum, float part_rest, float& to_sum, float& to_rest) {
+      const float d = fabsf(part_top) == INFINITY ? 0.f : part_top - r, f = __builtin_amdgcn_exp2f(1.44269504088896340736f * d);
+      to_rest += f > 0.f ? f * fmaf(part_sum, d, part_rest) : 0.f;
+      to_sum += part_sum * f;
+    };
+    float new_sum = 0.f, new_rest = 0.f;
+    scaled(top, sum, rest, new_sum, new_rest);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) scaled(p[u][0], p[u][1], p[u][2], new_sum, new_rest);
+    top = both; sum = new_sum; rest = new_rest;
+  }
+  if constexpr (TOP) {
+    set_there(64 * part + lane);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) most[u % GROUPS] = fmaxf(most[u % GROUPS], m[u]);
+#pragma unroll 4
+    for (int s = 64 * (part + WAVES * AHEAD) + lane; s < a.sets; s += 64 * WAVES) most[0] = fmaxf(most[0], set_max[s]);
+    if (a.first || lane >= a.top) own_entry = -1;
+    if (a.first) bar = NAN;
+  }
+  join_lanes(top, sum, rest);
+  if (WAVES > 1 && threadIdx.x < 2) counts[threadIdx.x] = 0;
+  if constexpr (WAVES > 1) {
+    if constexpr (TOP) {
+      group_max[wave][lane] = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+    }
+    if (lane == 0) {
+      joined[0][3 * wave] = top;
+      joined[0][3 * wave + 1] = sum;
+      joined[0][3 * wave + 2] = rest;
+    }
+    meet();
+    top = lane < WAVES ? joined[0][3 * lane] : -INFINITY;
+    sum = lane < WAVES ? joined[0][3 * lane + 1] : 0.f;
+    rest = lane < WAVES ? joined[0][3 * lane + 2] : 0.f;
+    join_lanes(top, sum, rest);
+    if constexpr (TOP) {
+#pragma unroll
+      for (int g = 0; g < GROUPS; ++g) most[g] = -INFINITY;
+#pragma unroll
+      for (int v = 0; v < WAVES; ++v) most[v % GROUPS] = fmaxf(most[v % GROUPS], group_max[v][lane]);
+    }
+  } else {
+    meet();
+  }
+  if (!a.first) {
+    float x = so_far[0], y = so_far[1], z = so_far[2];
+    join_scores(x, y, z, top, sum, rest);
+    top = x; sum = y; rest = z;
+  }
+  const float ref = lse_reference(top), log_sum = logf(sum);
+  if (part == 0 && lane == 0) {
+    if (!a.last) {
+      a.state[t] = f32x4{top, sum, rest, 0.f};
+    } else {
+      if (a.lse) a.lse[t] = ref + log_sum;
+      if (a.entropy) a.entropy[t] = log_sum - rest / sum;
+      if (a.logprob) {
+        // (the maximum's part first: a target that is the maximum loses log(1 + the others), not a difference of large numbers)
+        a.logprob[t] = target == a.ignore ? 0.f : target >= 0 && target < a.vocab ? (at_target - ref) - log_sum : NAN;
+      }
+    }
+  }
+  if constexpr (!TOP) return;
+
+  // ---- sets that reach the bar
+  // (many are sought among more groups, of which fewer hold two of them)
+  float least = next_above(bar);
+  if (a.top > 24) {
+    int above = 0;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) above += (int)__popcll(__ballot(most[g] > bar));
+    if (bar != bar || above >= a.top) least = nth_of_lanes(most, a.top);
+  } else {
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) most[0] = fmaxf(most[0], most[g]);
+    if (bar != bar || (int)__popcll(__ballot(most[0] > bar)) >= a.top) least = nth_of_lanes<1>({most[0]}, a.top);
+  }
+  auto reaches = [&](float v) { return v >= least; };
+  for (int s0 = 64 * part; s0 < a.sets; s0 += 64 * WAVES * AHEAD) {
+    if (s0 != 64 * part) {
+      ask_sets(s0 + lane);
+      set_there(s0 + lane);
+    }
+    uint32_t hits = 0;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) hits |= reaches(m[u]) && s0 + lane + 64 * WAVES * u < a.sets ? 1u << u : 0u;
+    while (__any(hits != 0)) {
+      const int to = places(0, hits != 0);
+      if (hits != 0 && to < SETS) set_list[at][to] = s0 + lane + 64 * WAVES * __builtin_ctz(hits);
+      hits &= hits - 1;
+    }
+  }
+  // the largest so far
+  const uint64_t own_key = own_entry >= 0 ? rank_key(own_value, (int)own_entry) : 0;
+  if (!a.first && part == 0) {
+    const int to = places(1, own_key != 0);
+    if (own_key) keys[at][to] = own_key;
+  }
+  meet();
+  // ---- their logits that reach it
+  const int size = a.set_size, per = 64 / size;                      // sets that a wave looks at together
+  auto logit = [&](int set, int& entry) -> float {
+    entry = set * size + lane % size;
+    return logits[(int64_t)set * size + lane % size];
+  };
+  const int n_sets = count(0);
+  if (n_sets <= SETS) {
+    for (int j = part * per; j < n_sets; j += 4 * per * WAVES) {
+      float v[4];
+      int e[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int which = j + u * per * WAVES + lane / size;
+        e[u] = 0;
+        v[u] = which < n_sets ? logit(set_list[at][which], e[u]) : NAN;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const bool mine = reaches(v[u]) && e[u] < a.vocab - a.row_first;
+        const int to = places(1, mine);
+        if (mine && to < KEYS) keys[at][to] = rank_key(v[u], a.row_first + e[u]);
+      }
+    }
+  }
+  meet();
+  const int n = count(1);
+  auto put = [&](int rank, uint64_t key) {
+    index[rank] = key ? (int64_t)key_entry(key) : -1;
+    values[rank] = !key ? NAN : a.last ? (key_value(key) - ref) - log_sum : key_value(key);
+    if (rank == a.top - 1 && !a.last) a.bar[t] = key ? key_value(key) : NAN;
+  };
+  if (n_sets <= SETS && n <= KEYS) {
+    for (int i = 64 * part + lane; i < n; i += 64 * WAVES) {
+      const uint64_t own = keys[at][i];
+      int rank = 0;
+#pragma unroll 4
+      for (int o = 0; o < n; ++o) rank += keys[at][o] > own;
+      if (rank < a.top) put(rank, own);
+    }
+    for (int i = n + 64 * part + lane; i < a.top; i += 64 * WAVES) put(i, 0);
+    return;
+  }
+  // ---- too many: set after set in the order of their entries, and as often as there might be no room for more, those that are not among the largest
+  // go, after which only larger logits are taken (an equal one's entry is higher)
+  constexpr int ROOM = (KEYS - GENSOR_TOP_MAX) / (64 * WAVES), AT_ONCE = ROOM < 4 ? ROOM : 4, OWN = KEYS / (64 * WAVES);
+  static_assert(AT_ONCE >= 1 && OWN >= 1, "room for what is looked at together");
+  auto only_largest = [&](int m) -> int {
+    uint64_t own[OWN];
+    int rank[OWN];
+#pragma unroll
+    for (int k = 0; k < OWN; ++k) {
+      const int i = 64 * (part + WAVES * k) + lane;
+      own[k] = i < m ? keys[at][i] : 0;
+      rank[k] = 0;
+    }
+#pragma unroll 4
+    for (int o = 0; o < m; ++o) {
+      const uint64_t other = keys[at][o];
+#pragma unroll
+      for (int k = 0; k < OWN; ++k) rank[k] += other > own[k];
+    }
+    meet();
+    const int left = min(m, a.top);
+#pragma unroll
+    for (int k = 0; k < OWN; ++k)
+      if (own[k] && rank[k] < left) keys[at][rank[k]] = own[k];
+    own_counts[1] = left;
+    if (WAVES > 1 && threadIdx.x == 0) counts[1] = left;
+    meet();
+    return left;
+  };
+  meet();                                                            // (everyone has read the counts)
+  own_counts[1] = 0;
+  if (WAVES > 1 && threadIdx.x == 0) counts[1] = 0;
+  meet();
+  if (!a.first && part == 0) {
+    const int to = places(1, own_key != 0);
+    if (own_key) keys[at][to] = own_key;
+  }
+  float taken = least;
+  constexpr int CHUNK = 64 * WAVES;
+  for (int c0 = 0; c0 < a.sets; c0 += CHUNK) {
+    // (sets none of which holds one are passed over together)
+    const int own_set = c0 + 64 * part + lane;
+    const float own_max = own_set < a.sets ? set_max[own_set] : NAN;
+    auto some = [&]() { return WAVES > 1 ? __syncthreads_or(own_max >= taken) != 0 : __any(own_max >= taken) != 0; };
+    if (!some()) continue;
+    for (int s0 = c0; s0 < min(c0 + CHUNK, a.sets); s0 += AT_ONCE * per * WAVES) {
+      meet();
+      const int so_many = count(1);
+      meet();
+      if (so_many > KEYS - AT_ONCE * 64 * WAVES) {
+        only_largest(so_many);                                       // (more than GENSOR_TOP_MAX: `top` are left)
+        const float next = next_above(key_value(keys[at][a.top - 1]));
+        if (!(next <= taken)) taken = next;
+        if (!some()) break;
+      }
+      float v[AT_ONCE];
+      int e[AT_ONCE];
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const int set = s0 + (part + u * WAVES) * per + lane / size;
+        e[u] = 0;
+        v[u] = set < min(c0 + CHUNK, a.sets) && set_max[set] >= taken ? logit(set, e[u]) : NAN;
+      }
+#pragma unroll
+      for (int u = 0; u < AT_ONCE; ++u) {
+        const bool mine = v[u] >= taken && e[u] < a.vocab - a.row_first;
+        const int to = places(1, mine);
+        if (mine) keys[at][to] = rank_key(v[u], a.row_first + e[u]);
+      }
+    }
+  }
+  meet();
+  const int so_many = count(1);
+  meet();
+  const int left = only_largest(so_many);
+  for (int i = 64 * part + lane; i < a.top; i += 64 * WAVES) put(i, i < left ? keys[at][i] : 0);
 }
 
 }  // namespace gensor
@@ -712,7 +710,6 @@ gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, co
   f32x4* parts = (f32x4*)(at + head);
   float* maxima = (float*)(at + head + pl.parts);
   float* logits = (float*)(at + head + pl.parts + pl.maxima);
-  const unsigned blocks = (unsigned)std::min<int64_t>((T + 3) / 4, 1 << 20);
   for (int64_t entry = 0; entry < V; entry += rows, rows = piece) {
     rows = std::min(rows, V - entry);
     const bool first = entry == 0, last = entry + rows == V;
@@ -764,7 +761,11 @@ gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, co
       if (T <= 256) hipLaunchKernelGGL((advance_kernel<8, TOP>), dim3((unsigned)T), dim3(512), 0, s, v);
       else if (T <= 1024) hipLaunchKernelGGL((advance_kernel<4, TOP>), dim3((unsigned)T), dim3(256), 0, s, v);
       else if (T <= 2048) hipLaunchKernelGGL((advance_kernel<2, TOP>), dim3((unsigned)T), dim3(128), 0, s, v);
-      else hipLaunchKernelGGL((advance_kernel<1, TOP>), dim3(blocks), dim3(256), 0, s, v);
+      else
+        for (int64_t t = 0; t < T; t += 4 << 20) {
+          v.token_first = (int32_t)t;
+          hipLaunchKernelGGL((advance_kernel<1, TOP>), dim3((unsigned)((std::min<int64_t>(T - t, 4 << 20) + 3) / 4)), dim3(256), 0, s, v);
+        }
     };
     if (out.top) advance(std::true_type{});
     else advance(std::false_type{});
