@@ -299,14 +299,15 @@ __device__ inline float nth_of_lanes(const float (&x)[COUNT], int n) {
 //
 // The search.  A bar that no more than a few logits reach is known before any is read: what the pieces so far say (the top'th largest, to be
 // exceeded), and the top'th largest of 64 maxima of disjoint groups of this piece's sets (to be reached; sought only where it is the higher one, mostly in the
-// first two pieces: 4096 tokens' second 21 us without, 12 with).  Sets whose maximum does not reach it hold none of the largest; the logits of the others
+// first two pieces: 4096 tokens' second 21 us without, 13 with).  Sets whose maximum does not reach it hold none of the largest; the logits of the others
 // that reach it, and the largest so far, are gathered in LDS, and each one's place is the number of those above it: no order in which anything is gathered
 // matters.  (Putting them into a sorted list, a lane each, one by one took 0.3 us apiece: 23 us for one token's five, 43 for the twenty of 301 tokens.)
 // Where more come up than there is room for -- many equal ones, as of a padded batch's tokens of zeros -- all that were kept are looked through in their
 // order.
 //
-// Bound by a chain of loads (parts and maxima, then the sets) and by the vector unit.  us: one token's five of 50257 (8 waves) 6.8, 301 tokens' twenty of
-// 5003 (4 waves) 8.3, 4096 tokens' eight (a wave each) 9 to 21 a piece, without alternatives 7.
+// Bound by a chain of loads (parts and maxima, then the sets) and by the vector unit.  us: one token's five of 50257 (8 waves) 4.9, 301 tokens' twenty of
+// 5003 (4 waves) 6.6, 4096 tokens' eight (a wave each) 9 to 11 a piece, without alternatives 6.6.  (With the tokens in a loop, whose constants take registers:
+// 154 in place of 67, three workgroups a unit where there is work for four, 13 a piece.)
 template <int WAVES, bool TOP>
 __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(const AdvanceArgs a) {
   constexpr int TOKENS = WAVES == 1 ? 4 : 1, AHEAD = WAVES == 1 ? 12 : 8, KEYS = WAVES == 1 ? 512 : 1024, SETS = 512, GROUPS = 4;
@@ -608,8 +609,8 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
 
 namespace {
 
-// Logits of a piece at most, where the largest are asked for.  (4096 tokens over 50257 entries, eight alternatives, f16, us: 128 MiB 395, 256 361, 384 350,
-// 512 354, 1024 350.)
+// Logits of a piece at most, where the largest are asked for.  (4096 tokens over 50257 entries, eight alternatives, f16, us: 128 MiB 355, 256 327, 384 316,
+// 512 320, 1024 311.)
 const size_t kScoreBytes = (size_t)384 << 20;
 // ... of which a first piece that may keep them all
 const size_t kHeadBytes = (size_t)32 << 20;
@@ -755,12 +756,12 @@ gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, co
     v.logprob = out.logprob;
     v.lse = out.lse;
     v.entropy = out.entropy;
-    // (waves do part of the work over again: one token's 6.8 us with 8, 7.1 with 4, 9.0 with 16; 301 tokens' 8.3 with 4, 15.7 with 16)
+    // (waves do part of the work over again.  The whole call over 50257 entries, us, eight alternatives and fifty, with 1, 4 and 8 waves: one token 24.4, 21.7,
+    // 21.9 and 32.1, 24.7, 24.1; 256 tokens 39.7, 36.6, 36.6 and 50.0, 39.9, 39.0; 1024 109.6, 110.2, 113.2 and 129, 120, 124; 4096 312, 332, 358 and 356, 375, 415)
     auto advance = [&](auto with_top) {
       constexpr bool TOP = decltype(with_top)::value;
       if (T <= 256) hipLaunchKernelGGL((advance_kernel<8, TOP>), dim3((unsigned)T), dim3(512), 0, s, v);
       else if (T <= 1024) hipLaunchKernelGGL((advance_kernel<4, TOP>), dim3((unsigned)T), dim3(256), 0, s, v);
-      else if (T <= 2048) hipLaunchKernelGGL((advance_kernel<2, TOP>), dim3((unsigned)T), dim3(128), 0, s, v);
       else
         for (int64_t t = 0; t < T; t += 4 << 20) {
           v.token_first = (int32_t)t;

@@ -391,8 +391,8 @@ __device__ __attribute__((always_inline)) inline float over_groups(float x, Op&&
 // The logits' reduction of END_LSE with one more sum, and, for the largest entries, the maxima of sets of 32 rows and the logits of the sets whose
 // maximum is above the token's bar (a set in 70 behind the first piece).  Sums and maxima of a token lie side by side for the wave that joins them.
 // Bound by the products under the power limit (16 of a tile's 21 to 24 us), then by the vector unit.  4096 tokens over 50257 entries of width 768, f16, us
-// with the join: lse 290 (1.09 PFLOP/s), with entropy 300, with the log probabilities of targets 301, with eight alternatives 364, all together 348 to 388 (four
-// pieces; matrix units busy 46 %); one token 17.4, which is reading W at 4.4 TB/s.
+// with the join: lse 268 (1.18 PFLOP/s), with entropy 277, with the log probabilities of targets 278, with eight alternatives 311, all together 333 (three
+// pieces; matrix units busy 45 %); one token 17.4, which is reading W at 4.4 TB/s.
 struct Score {
   typedef ScoreArgs Args;
   static constexpr int MOVES = PLACE_ALL;
