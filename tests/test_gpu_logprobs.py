@@ -361,3 +361,31 @@ def test_infinite_logits_among_many_equal(gs, T):
     want = torch.full((top,), -1, device="cuda")
     want[:5] = torch.arange(7, V, 1000, device="cuda")[:5]
     assert torch.equal(out["top_index"], want.expand(T, top))
+
+
+def test_two_streams_at_once(gs):
+    """Calls that overlap, each with a workspace of its own, give what they give alone."""
+    shapes = [(700, 20_000, 128, 8), (3, 30_000, 64, 64), (1300, 6000, 96, 20)]
+    calls, want = [], []
+    for n, (T, V, D, top) in enumerate(shapes):
+        X, W = operands("f16", T, V, D, 40 + n)
+        t = targets_for(T, V, 40 + n)
+        out = {"logprob": torch.empty(T, device="cuda"), "entropy": torch.empty(T, device="cuda"), "top_index": torch.empty((T, top), dtype=torch.int64, device="cuda"),
+               "top_logprob": torch.empty((T, top), device="cuda")}
+        ws = workspace(gs.logprobs_workspace_bytes("f16", T, V, D, top))
+        calls.append((lambda X=X, W=W, t=t, ws=ws, out=out: gs.logprobs(X, W, targets=t, ignore_index=IGNORE, workspace=ws, **out), out, torch.cuda.Stream()))
+        calls[-1][0]()
+        torch.cuda.synchronize()
+        want.append({k: v.clone() for k, v in out.items()})
+    for _ in range(3):
+        for call, out, stream in calls:
+            for v in out.values():
+                v.fill_(-5)
+        torch.cuda.synchronize()
+        for call, out, stream in calls:
+            with torch.cuda.stream(stream):
+                call()
+                call()
+        torch.cuda.synchronize()
+        for (call, out, stream), w in zip(calls, want):
+            assert all(torch.equal(out[k], w[k]) for k in out)
