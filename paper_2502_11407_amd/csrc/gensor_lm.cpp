@@ -694,11 +694,13 @@ gensor_status run_scores(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, co
     if (piece <= d.bm) return GENSOR_ERR_WORKSPACE;
     piece = std::max<int64_t>(1, piece / 2 / d.bm) * d.bm;
   }
-  // Nothing is known of the first piece's logits, so all of them are kept: it is one round of tiles, after which few are above a token's bar.
+  // Nothing is known of the first piece's logits, so all of them are kept: it is one round of tiles, after which few are above a token's bar.  Where all are
+  // two rounds, or few bytes, there is one piece.  (Eight alternatives, f16, us, in one piece and in two: 512 tokens over 50257 entries 69, 72; 4096 over 5000
+  // 65, 72; 2.3 rounds, 640 over 50257, 94, 86.)
   int64_t rows = piece;
   if (out.top) {
     const int64_t tiles_n = (T + d.bn - 1) / d.bn, units = gensor_hw_mi355x()->compute_units;
-    if (piece * T * 4 > (int64_t)kHeadBytes) rows = std::min(piece, std::max<int64_t>(1, units / tiles_n) * d.bm);
+    if (piece * T * 4 > (int64_t)kHeadBytes && (piece + d.bm - 1) / d.bm * tiles_n > 2 * units) rows = std::min(piece, std::max<int64_t>(1, units / tiles_n) * d.bm);
     // The others are whole rounds, where that makes them no more: a launch's last round leaves units idle.  (3000 tokens over 50257 entries 265 us without, 246 with.)
     const int64_t whole = piece / d.bm * tiles_n / units * units / tiles_n * d.bm, rest = V - rows;
     if (whole > 0 && (rest + whole - 1) / whole == (rest + piece - 1) / piece) piece = whole;
