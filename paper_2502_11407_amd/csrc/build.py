@@ -154,7 +154,7 @@ def _compile(src):
     if "fused" in os.path.basename(src):
         deps += [os.path.join(HERE, "fused_kernel.hpp"), os.path.join(HERE, "fused_registry.hpp"), os.path.join(PKG, "..", "include", "gensor_fused.h")]
     if os.path.basename(src).startswith(("lm", "gated", "gensor_lm")):
-        deps += [os.path.join(HERE, f) for f in ("fused_kernel.hpp", "fused_registry.hpp", "lm_kernel.hpp", "lm_registry.hpp", "fused_host.hpp")]
+        deps += [os.path.join(HERE, f) for f in ("fused_kernel.hpp", "fused_registry.hpp", "lm_kernel.hpp", "lm_registry.hpp", "score_order.hpp", "fused_host.hpp")]
         deps += [os.path.join(PKG, "..", "include", f) for f in ("gensor_fused.h", "gensor_lm.h")]
     if os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps if os.path.exists(d)):
         return obj

@@ -13,6 +13,7 @@
 #include "../../include/gensor_lm.h"
 #include "fused_host.hpp"
 #include "lm_registry.hpp"
+#include "score_order.hpp"
 
 using namespace gensor;
 
@@ -237,17 +238,6 @@ struct AdvanceArgs {
   float *logprob, *lse, *entropy;
 };
 
-// A logit and its entry as one number, the larger the earlier it is among the largest: the value's order in front, then the lower entry.  0: none.
-__device__ inline uint64_t rank_key(float v, int entry) {
-  const uint32_t u = as_u32(v + 0.f);                                  // (minus zero is zero)
-  return (uint64_t)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (uint32_t)~entry;
-}
-__device__ inline float key_value(uint64_t key) {
-  const uint32_t u = (uint32_t)(key >> 32);
-  return as_f32(u & 0x80000000u ? u & 0x7fffffffu : ~u);
-}
-__device__ inline int key_entry(uint64_t key) { return (int)~(uint32_t)key; }
-
 // x of all lanes joined (by an operation whose operands may be swapped): all of them hold the result.  In registers, without LDS.
 template <typename Op>
 __device__ inline float over_lanes(float x, Op&& op) {
@@ -270,35 +260,25 @@ __device__ inline void join_lanes(float& top, float& sum, float& rest) {
   top = all;
 }
 
-// The smallest number above a number (NaN above infinity, which no number reaches)
-__device__ inline float next_above(float x) {
-  const uint32_t u = as_u32(x + 0.f);
-  return as_f32(u & 0x80000000u ? u - 1 : u + 1);
-}
-
-// A number that n of the lanes' values (COUNT each) reach, the largest with 20 bits (so a little below the n'th largest: an instruction or two a bit,
-// where counting for each value those above it takes three a lane)
+// A number that n of the lanes' values (COUNT each) reach (nth_reached: twenty ballots a value; counting for each value those above it takes three
+// instructions a lane)
 template <int COUNT>
 __device__ inline float nth_of_lanes(const float (&x)[COUNT], int n) {
   uint32_t key[COUNT];
 #pragma unroll
   for (int c = 0; c < COUNT; ++c) key[c] = (uint32_t)(rank_key(x[c], 0) >> 32);
-  uint32_t found = 0;
-#pragma unroll
-  for (int bit = 31; bit >= 12; --bit) {
-    const uint32_t higher = found | 1u << bit;
+  return nth_reached(n, [&](uint32_t least) __attribute__((always_inline)) {
     int reach = 0;
 #pragma unroll
-    for (int c = 0; c < COUNT; ++c) reach += (int)__popcll(__ballot(key[c] >= higher));
-    if (reach >= n) found = higher;
-  }
-  return found > 0x007fffffu ? key_value((uint64_t)found << 32) : -INFINITY;
+    for (int c = 0; c < COUNT; ++c) reach += (int)__popcll(__ballot(key[c] >= least));
+    return reach;
+  });
 }
 
 // WAVES waves per token join a piece's parts to what was joined before, and find the largest logits among the piece's and those so far.
 //
 // The search.  A bar that no more than a few logits reach is known before any is read: what the pieces so far say (the top'th largest, to be
-// exceeded), and the top'th largest of 64 maxima of disjoint groups of this piece's sets (to be reached; sought only where it is the higher one, mostly in the
+// exceeded), and the top'th largest of 64 maxima of disjoint groups of this piece's sets (to be reached; sought only where it may be the higher one, mostly in the
 // first two pieces: 4096 tokens' second 21 us without, 13 with).  Sets whose maximum does not reach it hold none of the largest; the logits of the others
 // that reach it, and the largest so far, are gathered in LDS, and each one's place is the number of those above it: no order in which anything is gathered
 // matters.  (Putting them into a sorted list, a lane each, one by one took 0.3 us apiece: 23 us for one token's five, 43 for the twenty of 301 tokens.)
@@ -449,18 +429,18 @@ __global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void advance_kernel(
   }
   if constexpr (!TOP) return;
 
-  // ---- sets that reach the bar
+  // ---- sets that reach the bar; all of them are stored (least_wanted)
   // (many are sought among more groups, of which fewer hold two of them)
-  float least = next_above(bar);
+  float least;
   if (a.top > 24) {
     int above = 0;
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) above += (int)__popcll(__ballot(most[g] > bar));
-    if (bar != bar || above >= a.top) least = nth_of_lanes(most, a.top);
+    least = least_wanted(bar, above >= a.top, [&]() { return nth_of_lanes(most, a.top); });
   } else {
 #pragma unroll
     for (int g = 1; g < GROUPS; ++g) most[0] = fmaxf(most[0], most[g]);
-    if (bar != bar || (int)__popcll(__ballot(most[0] > bar)) >= a.top) least = nth_of_lanes<1>({most[0]}, a.top);
+    least = least_wanted(bar, (int)__popcll(__ballot(most[0] > bar)) >= a.top, [&]() { return nth_of_lanes<1>({most[0]}, a.top); });
   }
   auto reaches = [&](float v) { return v >= least; };
   for (int s0 = 64 * part; s0 < a.sets; s0 += 64 * WAVES * AHEAD) {

@@ -9,6 +9,7 @@
 //   Teach      the same product again: C = scale * weight[token] * exp(logit - lse[token])
 #pragma once
 #include "fused_kernel.hpp"
+#include "score_order.hpp"
 
 namespace gensor {
 
@@ -33,7 +34,7 @@ struct ScoreArgs : KernelArgs {
   f32x4* parts;                            // [token][slab of C::WM rows]: maximum, sum, weighted sum
   float* set_max;                          // [token][set of rows]
   float* logits;                           // [token][set][rows of a set]: what is read of a token lies close together
-  const float* bar;                        // logits of sets whose maximum is not above a token's are not needed (NaN, or null: all are)
+  const float* bar;                        // logits of sets whose maximum is not above a token's are not needed, and not stored (NaN, or null: all are)
   float* at_target;
 };
 
@@ -532,10 +533,10 @@ struct Score {
     for (int bj = 0; bj < C::NBLK; ++bj) {
       const int token = p.n0 + p.col + bj * MB + frow;
       const bool there = token < a.N;
-      if (!__any(there && !(tops[bj] <= bar[bj]))) continue;
+      if (!__any(there && set_is_stored(tops[bj], bar[bj]))) continue;
 #pragma unroll
       for (int s = 0; s < SETS; ++s)
-        if (there && !(set_top[bj][s] <= bar[bj])) {
+        if (there && set_is_stored(set_top[bj][s], bar[bj])) {
           float* to = a.logits + ((int64_t)token * a.sets + slab * SETS + s) * SET + 4 * fgrp;
 #pragma unroll
           for (int b = 0; b < PER; ++b)
