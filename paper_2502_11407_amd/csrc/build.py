@@ -1,6 +1,8 @@
 """Build libgensor.so for gfx950: one translation unit per group of kernel instances
 (generated from lattice.py), the registry table, the constructor and the C ABI."""
+import functools
 import os
+import re
 import subprocess
 import sys
 from concurrent.futures import ThreadPoolExecutor
@@ -147,16 +149,29 @@ def generate_lm():
     return units + [path]
 
 
+@functools.lru_cache(maxsize=None)
+def _included(path, modified):
+    with open(path) as f:
+        return re.findall(r'^\s*#\s*include\s+"([^"]+)"', f.read(), re.M)
+
+
+def dependencies(src):
+    """The unit and every file of this repository that it includes, by itself or through others."""
+    found, todo = [], [os.path.abspath(src)]
+    while todo:
+        path = todo.pop()
+        if path in found:
+            continue
+        found.append(path)
+        for name in _included(path, os.stat(path).st_mtime_ns):
+            near = os.path.normpath(os.path.join(os.path.dirname(path), name))
+            todo.append(near if os.path.exists(near) else os.path.join(HERE, name))
+    return found
+
+
 def _compile(src):
     obj = os.path.join(GEN, os.path.basename(src).rsplit(".", 1)[0] + ".o")
-    deps = [src, os.path.join(HERE, "gemm_kernel.hpp"), os.path.join(HERE, "conv_kernel.hpp"), os.path.join(HERE, "conv_rows_kernel.hpp"), os.path.join(HERE, "registry.hpp"),
-            os.path.join(HERE, "host_common.hpp"), os.path.join(PKG, "..", "include", "gensor.h")]
-    if "fused" in os.path.basename(src):
-        deps += [os.path.join(HERE, "fused_kernel.hpp"), os.path.join(HERE, "fused_registry.hpp"), os.path.join(PKG, "..", "include", "gensor_fused.h")]
-    if os.path.basename(src).startswith(("lm", "gated", "gensor_lm")):
-        deps += [os.path.join(HERE, f) for f in ("fused_kernel.hpp", "fused_registry.hpp", "lm_kernel.hpp", "lm_registry.hpp", "score_order.hpp", "fused_host.hpp")]
-        deps += [os.path.join(PKG, "..", "include", f) for f in ("gensor_fused.h", "gensor_lm.h")]
-    if os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in deps if os.path.exists(d)):
+    if os.path.exists(obj) and all(os.path.getmtime(obj) >= os.path.getmtime(d) for d in dependencies(src)):
         return obj
     # host sources: no fused multiply-add contraction, so the constructor's double arithmetic
     # is the plain IEEE sequence its tests compare against
