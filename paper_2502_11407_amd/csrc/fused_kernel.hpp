@@ -514,10 +514,11 @@ struct Fused {
 #pragma unroll
         for (int v = 0; v < NACC; ++v) top = fmaxf(top, acc[bi][bj][v]);
       // exp(z - ref) in three operations: the product log2e * ref is rounded, which multiplies every term by the same factor 2^off; it is taken
-      // out of the sum, so that the maximum's own term is 1.  (Where that product would not be finite: four operations.  The column's own
-      // choice: a token's bits do not depend on what its neighbours hold.)
+      // out of the sum, so that the maximum's own term is 1.  (off is up to 2^-25 of the product.  Beyond 1e9, where it may exceed 64 and its power all
+      // numbers: four operations.  A stretch of the vocabulary that is shut off with large negative logits comes here, too.  The column's own choice: a
+      // token's bits do not depend on what its neighbours hold.)
       const float ref = lse_reference(top);
-      const bool far = fabsf(ref) > 1e37f;
+      const bool far = fabsf(ref) > 1e9f;
       const float base = far ? 0.f : -(log2e * ref), off = far ? 0.f : fmaf(log2e, ref, base);
       float sum = 0.f;
       if (__any(far)) {

@@ -452,12 +452,13 @@ struct Score {
         set_top[bj][s] = over_groups<MB>(t, larger);
         top = fmaxf(top, set_top[bj][s]);
       }
-      // exp(z - ref) = 2^y, y = log2(e) z - (log2(e) ref rounded), all terms off by one factor 2^off, which is taken out of the sums.  (Where the
-      // rounded product would not be finite the difference is taken first; the column's own choice, so that a token's bits do not depend
+      // exp(z - ref) = 2^y, y = log2(e) z - (log2(e) ref rounded), all terms off by one factor 2^off, which is taken out of the sums.  (off is up to 2^-25 of
+      // that product.  Beyond 1e6 the difference is taken first: from there on the weights would be mostly off, and beyond 1e9 its power may be no number; a
+      // stretch of the vocabulary that is shut off with large negative logits comes here, too.  The column's own choice, so that a token's bits do not depend
       // on its neighbours.)  The weight in the second sum is y itself; where a logit is minus infinity, or a row none, that is 0 times minus infinity,
       // and the sums are taken again with weights that are held above -1e4.
       const float ref = lse_reference(top);
-      const bool far = fabsf(ref) > 1e37f;
+      const bool far = fabsf(ref) > 1e6f;
       const float base = far ? 0.f : -(log2e * ref), off = far ? 0.f : fmaf(log2e, ref, base);
       float sum = 0.f, rest = 0.f;
       auto reduce = [&](auto weighted_tag, auto&& exponent, auto&& weight) {
