@@ -514,7 +514,7 @@ struct Fused {
 #pragma unroll
         for (int v = 0; v < NACC; ++v) top = fmaxf(top, acc[bi][bj][v]);
       // exp(z - ref) in three operations: the product log2e * ref is rounded, which multiplies every term by the same factor 2^off; it is taken
-      // out of the sum, so that the maximum's own term is 1.  (off is up to 2^-25 of the product.  Beyond 1e9, where it may exceed 64 and its power all
+      // out of the sum, so that the maximum's own term is 1.  (off is up to 2^-24 of the product.  Beyond 1e9, where it may exceed 64 and its power all
       // numbers: four operations.  A stretch of the vocabulary that is shut off with large negative logits comes here, too.  The column's own choice: a
       // token's bits do not depend on what its neighbours hold.)
       const float ref = lse_reference(top);
@@ -576,8 +576,9 @@ struct Fused {
     }
   }
 
-  // exp(z - lse), base = -log2(e) lse.  For 16-bit results, which round a thousand times coarser than the product and the exponent are rounded, in two
-  // operations; in fp32 the exponent's rounding (2^-24 of up to a hundred) is carried as a factor.
+  // exp(z - lse), base = -log2(e) lse.  For 16-bit results in two operations: base is rounded, up to an lse of 1024 by 2^-14, a factor within 2^-14
+  // of one, where the results are rounded by 2^-11 and 2^-8 (below_lse takes care of what lies beyond).  In fp32 the exponent's
+  // rounding (2^-24 of up to a hundred) is carried as a factor.
   template <typename C> static __device__ float probability(float z, float lse, float base) {
     constexpr float log2e = 1.44269504088896340736f;
     if constexpr (C::ES == 2) return __builtin_amdgcn_exp2f(fmaf(log2e, z, base));
@@ -585,6 +586,25 @@ struct Fused {
     const float r = fmaf(log2e, d, -t) + 1.92596299e-8f * d;           // (log2(e) - log2e)
     const float e = __builtin_amdgcn_exp2f(t);
     return d > -100.f ? fmaf(e, 0.69314718f * r, e) : e;                // (-inf: inf - inf)
+  }
+  // The `base` of a column's probabilities.  16-bit types, an lse beyond 1024: the logits become their differences from it, one operation more, and base 0.
+  // (Only of the waves that have such a token, and the token's own choice: with the rounded product a probability of one could be up to 2^64 at an lse of
+  // 1e9, and infinite from some 3e9 on.)
+  template <typename C, typename Acc>
+  static __device__ __attribute__((always_inline)) float below_lse(Acc (&acc)[C::MBLK][C::NBLK], int bj, float lse, bool counts) {
+    constexpr int NACC = C::MB * C::MB / 64;
+    if constexpr (C::ES == 2) {
+      const bool far = counts && fabsf(lse) > 1024.f;
+      if (__any(far)) {
+        const float off = far ? lse : 0.f;
+#pragma unroll
+        for (int bi = 0; bi < C::MBLK; ++bi)
+#pragma unroll
+          for (int v = 0; v < NACC; ++v) acc[bi][bj][v] -= off;
+      }
+      return far ? 0.f : -1.44269504088896340736f * lse;
+    }
+    return 0.f;
   }
 
   // ---- scale * dloss * (softmax - one at the target), in the input type, a product's operand next.  Columns beyond the tokens,
@@ -602,7 +622,7 @@ struct Fused {
       const bool there = token < a.tokens;
       const int64_t target = there ? a.targets[token] : -1;
       const bool counts = there && target != a.ignore && target >= 0 && target < a.vocab;
-      const float lse = counts ? a.lse[token] : INFINITY, base = -1.44269504088896340736f * lse, g = counts ? a.dloss[token] * scale : 0.f;
+      const float lse = counts ? a.lse[token] : INFINITY, base = below_lse<C>(acc, bj, lse, counts), g = counts ? a.dloss[token] * scale : 0.f;
       // (zero by choice, not by g = 0: the logits of a token that does not count may be infinite or NaN)
 #pragma unroll
       for (int bi = 0; bi < C::MBLK; ++bi)

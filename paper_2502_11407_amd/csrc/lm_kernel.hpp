@@ -452,7 +452,7 @@ struct Score {
         set_top[bj][s] = over_groups<MB>(t, larger);
         top = fmaxf(top, set_top[bj][s]);
       }
-      // exp(z - ref) = 2^y, y = log2(e) z - (log2(e) ref rounded), all terms off by one factor 2^off, which is taken out of the sums.  (off is up to 2^-25 of
+      // exp(z - ref) = 2^y, y = log2(e) z - (log2(e) ref rounded), all terms off by one factor 2^off, which is taken out of the sums.  (off is up to 2^-24 of
       // that product.  Beyond 1e6 the difference is taken first: from there on the weights would be mostly off, and beyond 1e9 its power may be no number; a
       // stretch of the vocabulary that is shut off with large negative logits comes here, too.  The column's own choice, so that a token's bits do not depend
       // on its neighbours.)  The weight in the second sum is y itself; where a logit is minus infinity, or a row none, that is 0 times minus infinity,
@@ -565,17 +565,25 @@ struct Teach {
     constexpr int MB = C::MB, NACC = MB * MB / 64;
     typedef Fused<END_LINEAR, MOVE_NONE> Plain;
     const float scale = a.scale ? *a.scale : 1.f;
+    if (a.alpha != 1.f) {
+#pragma unroll
+      for (int bi = 0; bi < C::MBLK; ++bi)
+#pragma unroll
+        for (int bj = 0; bj < C::NBLK; ++bj)
+#pragma unroll
+          for (int v = 0; v < NACC; ++v) acc[bi][bj][v] *= a.alpha;
+    }
 #pragma unroll
     for (int bj = 0; bj < C::NBLK; ++bj) {
       const int token = p.n0 + p.col + bj * MB + p.lane % MB;
       const bool there = token < a.tokens;
       const float weight = there ? a.dloss[token] * scale : 0.f;
       const bool counts = weight != 0.f;
-      const float lse = counts ? a.lse[token] : INFINITY, base = -1.44269504088896340736f * lse;
+      const float lse = counts ? a.lse[token] : INFINITY, base = Plain::template below_lse<C>(acc, bj, lse, counts);
 #pragma unroll
       for (int bi = 0; bi < C::MBLK; ++bi)
 #pragma unroll
-        for (int v = 0; v < NACC; ++v) acc[bi][bj][v] = counts ? weight * Plain::template probability<C>(a.alpha * acc[bi][bj][v], lse, base) : 0.f;
+        for (int v = 0; v < NACC; ++v) acc[bi][bj][v] = counts ? weight * Plain::template probability<C>(acc[bi][bj][v], lse, base) : 0.f;
     }
     Plain::template finish_linear<C, false>(a, acc, p);
   }
