@@ -52,7 +52,8 @@ gensor_status gensor_gated_act_grad(const gensor_problem* p, int32_t act, float 
  * wanted with logprob.  A NaN among a token's logits makes its log probabilities and entropy NaN; it is no alternative, and entry -1 stands where fewer than
  * `top` others are.  (An infinite largest logit: lse is that, what is a difference of infinities NaN.)
  * The workspace (256-byte aligned) holds, beside sums, the logits of a piece of the vocabulary that may be among the largest.
- * gensor_logprobs_workspace_bytes asks for what pieces of 384 MiB at most want, for any leading dimensions; with less the pieces are smaller.
+ * gensor_logprobs_workspace_bytes asks for what pieces of 384 MiB (or of one row of tiles, where many tokens make that more) want, for any leading
+ * dimensions; with less the pieces are smaller.  What it holds beforehand does not matter.
  * WORKSPACE if not even one row of tiles fits.
  */
 #define GENSOR_TOP_MAX 64
@@ -81,7 +82,8 @@ gensor_status gensor_distill_forward(gensor_dtype dtype, int64_t T, int64_t V, i
  *     dX = G * W,   dW = G^T * X
  * in `dtype`; dX or dW may be NULL.  G is zero for tokens whose loss is 0 for want of entries, whose loss is NaN for an entry out of range, and whose dloss is
  * zero, whatever their logits and lse are.  lse is the forward's, dloss (fp32, device) the gradient of each token's loss.  Pieces, G's scale in 16 bits
- * and room are as in gensor_xent_backward; gensor_distill_workspace_bytes(..., 1) asks for that and 8 T (k + 1) bytes more.
+ * (to which it is rounded, as the products' operand) and room are as in gensor_xent_backward; gensor_distill_workspace_bytes(..., 1) asks for that and
+ * T (8 k + 4) bytes more, rounded up to 256.
  */
 gensor_status gensor_distill_backward(gensor_dtype dtype, int64_t T, int64_t V, int64_t D, const void* X, int64_t ldx,
                                       const void* W, int64_t ldw, float scale, int32_t k, const int64_t* index, const float* teacher, int32_t normalize,

@@ -39,7 +39,10 @@ gensor_status remembered(const std::array<int64_t, 12>& key, int* out, F&& find)
 
 // The cheapest tile of two products at once: priced as one product of twice the columns, without the 192-column form, which such tiles do not have.
 // The 256x256 tile's price is that of its products alone; with its epilogue it takes 1.13 times that beside a 256x128 tile's (bf16, us, 256x256 and
-// 256x128, W [N][K]: 2048 x 5632 x 2048 88 and 82, 3000 x 5400 x 2048 133 and 114, 8192 x 2048 x 768 46 and 53, 20000 x 688 x 256 25 and 28).
+// 256x128, W [N][K]: 2048 x 5632 x 2048 88 and 82, 3000 x 5400 x 2048 133 and 114, 8192 x 2048 x 768 46 and 53, 20000 x 688 x 256 25 and 28).  The factor is
+// taken for every activation, type of C and with G and U kept, too.  All tiles timed beside the chosen one, us: it is the fastest of those four shapes,
+// 1024 x 4096 x 4096 and 4096 x 1024 x 512 with silu and G and U kept, none, relu alone, bf16 and fp32 results but for 20000 x 688 x 256 to fp32 (28.4, 24.0 with
+// 256x256; kept 44.0, 39.0); of 500 x 2048 x 768 it is up to 1.14 times the fastest (13.2, 11.6 with 64x64; fp32 33.9, 30.0).
 gensor_status choose_gated(const GemmView& v, bool vec_ok, const LeadingDims& ld, int64_t strideB, int* out) {
   return remembered({0, v.in_dtype, v.out_dtype, v.bsrc, vec_ok, v.M, v.N, v.K, ld.a, ld.b, ld.c, strideB}, out, [&]() {
     GemmView both = v;
@@ -65,6 +68,9 @@ gensor_status choose_gated(const GemmView& v, bool vec_ok, const LeadingDims& ld
 // The tile of a gradient, whose epilogue takes longer than its products: two values read and two or three stored, an exponential, a reciprocal and some
 // thirty operations each, 24 us a round of 256x256 tiles and 0.33 ns an element and unit of smaller ones.  (bf16, us, 256x256, 256x128 and 128x128:
 // 8192 x 2048 x 768 49, 56, 65; 3000 x 5400 x 2048 132, 117, 125; 2048 x 5632 x 2048 62, 75, 75; 8192 x 4096 x 4096 254, 297, 364; 1024 x 4096 x 4096 92, 54, 44.
+// The prices are those of silu with H in 16 bits, and taken for all.  All tiles timed beside the chosen one: without H and with relu or none within 10 % of
+// the fastest as with silu, but for 20000 x 688 x 256 (35.9, 30.3 with 256x256; silu 42.0, 37.0); fp32 operands within 4 %; fp32 results of bf16 operands within 12 %,
+// but for 20000 x 688 x 256 (104, 77 with 64x64; relu without H 48, 39).
 // Lines of G and U requested under the products did not help: 8192 x 2048 x 768 56, and 69 against 63 among the gradient's other products.)
 gensor_status choose_gated_grad(const GemmView& v, bool vec_ok, const LeadingDims& ld, int* out) {
   return remembered({1, v.in_dtype, v.out_dtype, v.bsrc, vec_ok, v.M, v.N, v.K, ld.a, ld.b, ld.c, 0}, out, [&]() {

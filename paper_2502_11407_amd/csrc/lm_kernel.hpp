@@ -390,10 +390,10 @@ __device__ __attribute__((always_inline)) inline float over_groups(float x, Op&&
 }
 
 // The logits' reduction of END_LSE with one more sum, and, for the largest entries, the maxima of sets of 32 rows and the logits of the sets whose
-// maximum is above the token's bar (a set in 70 behind the first piece).  Sums and maxima of a token lie side by side for the wave that joins them.
+// maximum is above the token's bar (46 of 768 in the second of three pieces, 6 of 675 in the third).  Sums and maxima of a token lie side by side for the wave that joins them.
 // Bound by the products under the power limit (16 of a tile's 21 to 24 us), then by the vector unit.  4096 tokens over 50257 entries of width 768, f16, us
 // with the join: lse 268 (1.18 PFLOP/s), with entropy 277, with the log probabilities of targets 278, with eight alternatives 311, all together 333 (three
-// pieces; matrix units busy 45 %); one token 17.4, which is reading W at 4.4 TB/s.
+// pieces; matrix units busy 45 %; 316 to 352 over boxes); one token 17.4, which is reading W at 4.4 TB/s.
 struct Score {
   typedef ScoreArgs Args;
   static constexpr int MOVES = PLACE_ALL;
@@ -551,7 +551,8 @@ struct Score {
   }
 };
 
-// Weights of zero are a choice, not a factor: the logits of a token that teaches nothing may be infinite or NaN.  Bound as END_PROB is: 4096 tokens over
+// Weights of zero are a choice, not a factor: the logits of a token that teaches nothing may be infinite or NaN.  G is rounded to the type because it is an
+// operand of two products, which run at nine times fp32's rate so (bf16: dX and dW 0.0023 from 64 bits, 0.0017 with fp32 throughout).  Bound as END_PROB is: 4096 tokens over
 // 50257 entries of width 768, bf16, 186 and 122 us of two pieces (1.03 PFLOP/s, matrix units busy 45 %, 412 MB written).
 struct Teach {
   typedef FusedArgs Args;
