@@ -393,7 +393,7 @@ __device__ __attribute__((always_inline)) inline float over_groups(float x, Op&&
 // maximum is above the token's bar (46 of 768 in the second of three pieces, 6 of 675 in the third).  Sums and maxima of a token lie side by side for the wave that joins them.
 // Bound by the products under the power limit (16 of a tile's 21 to 24 us), then by the vector unit.  4096 tokens over 50257 entries of width 768, f16, us
 // with the join: lse 268 (1.18 PFLOP/s), with entropy 277, with the log probabilities of targets 278, with eight alternatives 311, all together 333 (three
-// pieces; matrix units busy 45 %; 316 to 352 over boxes); one token 17.4, which is reading W at 4.4 TB/s.
+// pieces; matrix units busy 45 %; 316 to 352 from card to card); one token 17.4, which is reading W at 4.4 TB/s.
 struct Score {
   typedef ScoreArgs Args;
   static constexpr int MOVES = PLACE_ALL;
